@@ -19,12 +19,18 @@
  *                   example's gather with caller weights and its reduction
  *                   over the k neighbours (App. B);
  *   snls_aggregate_static  snls_aggregate without a caller workspace, for
- *                   callers that cannot allocate.
+ *                   callers that cannot allocate;
+ *   snls_bias, snls_bias_backward, snls_backward_scores  a learned bias of the
+ *                   neighbours' relative position and its training;
+ *   snls_cache_store, snls_cache_attend, snls_cache_attend_points  past frames
+ *                   held in 8 bits and attention over their whole windows, for
+ *                   programs that see a video frame by frame.
  *
  * Conventions shared by every call
  * --------------------------------
  *  - Pointers named as device buffers must point to device memory of the
- *    current HIP device; all are fp32, dense, C-contiguous, 4-byte aligned.
+ *    current HIP device; all are fp32 (unless the call says otherwise), dense,
+ *    C-contiguous, 4-byte aligned.
  *    The caller owns every buffer; the library keeps no pointer and no state
  *    between calls (apart from the scratch array of snls_aggregate_static),
  *    so concurrent calls on different streams are safe when their output
@@ -308,12 +314,149 @@ snls_status snls_gather_reduce(const float* v, const float* weights, const float
                                const snls_params* p, int32_t cout, float* out, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/* ---- learned position bias ------------------------------------------------
+ * Each component x of a neighbour's displacement falls into one of 2E+1
+ * buckets: j = the number of edges e_i with |x| >= e_i, bucket E + j for
+ * x >= 0, E - j for x < 0; its frame step frame - t, clamped to -radius ..
+ * radius, is bucket step + radius.  The table holds one learned number per
+ * head and bucket triple, (HD, 2*radius+1, 2E+1, 2E+1): frame step, row
+ * displacement, column displacement.  struct_size must be
+ * sizeof(snls_bias_params); edges[0 .. n_edges-1] are finite, > 0 and strictly
+ * ascending. */
+#define SNLS_BIAS_MAX_EDGES 16
+#define SNLS_BIAS_MAX_BUCKETS 4096 /* largest (2*radius+1) * (2E+1)^2 */
+typedef struct {
+  uint32_t struct_size;
+  int32_t radius;  /* 0 .. 63 */
+  int32_t n_edges; /* E, 0 .. SNLS_BIAS_MAX_EDGES */
+  float edges[SNLS_BIAS_MAX_EDGES];
+} snls_bias_params;
+
+/* snls_bias -- scores plus the bias of their position: out = dists + table
+ * (inner product) or dists - table (squared L2, where smaller is better), so
+ * that a larger entry always means more weight.  snls_aggregate, the other
+ * aggregations and snls_backward_scores then take out in place of dists.  A
+ * score that is not finite, and the score of a neighbour that contributes
+ * nothing to the aggregation (frame not an integer in [0,T), displacement not
+ * finite or 1e6 or more), is copied as it is.
+ *   dists   device, (B, HD, T, nH, nW, k); for p->k == 0 every candidate's, (..., (2wt+1)*ws*ws)
+ *   inds    device, (..., 3)
+ *   table   device, (HD, 2*radius+1, 2E+1, 2E+1)
+ *   out     device out, as dists; may be dists itself
+ * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for more buckets per head
+ * than SNLS_BIAS_MAX_BUCKETS or more than 2^40 scores; SNLS_ERR_HIP. */
+snls_status snls_bias(const float* dists, const float* inds, const float* table, const snls_params* p,
+                      const snls_bias_params* bias, float* out, void* stream);
+
+/* snls_bias_backward -- gradient of the table from the gradient of the biased
+ * scores (that of the scores themselves is the same): grad_table[hd, bucket] =
+ * the sum of +grad_scores (inner product) or -grad_scores (squared L2) over the
+ * neighbours that snls_bias adds this entry to.
+ *   grad_scores  device, as dists (snls_backward_scores returns it)
+ *   dists        device, the scores or the biased scores (which ones are finite)
+ *   inds         device, (..., 3)
+ *   grad_table   device out, (HD, 2*radius+1, 2E+1, 2E+1), fully overwritten
+ *   workspace    device scratch of at least
+ *                snls_workspace_size(SNLS_OP_BIAS_BACKWARD, p) bytes, 256-byte
+ *                aligned
+ * The result does not depend on scheduling: it is bit-identical between runs.
+ * Errors: as snls_bias; SNLS_ERR_WORKSPACE. */
+snls_status snls_bias_backward(const float* grad_scores, const float* dists, const float* inds, const snls_params* p,
+                               const snls_bias_params* bias, float* grad_table, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* snls_backward_scores -- snls_backward that also returns grad_scores
+ * (B,HD,T,nH,nW,k), dL/d dists of the loss through the aggregation plus
+ * grad_dists: what the gradient of anything added to the scores starts from
+ * (0 for neighbours that contribute nothing).  With biased scores as dists the
+ * gradients of q, k, v and the flows are those of the biased layer.  Every
+ * other argument, the workspace (SNLS_OP_BACKWARD) and the errors are those of
+ * snls_backward; grad_scores must not be NULL. */
+snls_status snls_backward_scores(const float* q, const float* k, const float* v, const float* flows,
+                                 const float* dists, const float* inds, const float* grad_out,
+                                 const float* grad_dists, const snls_params* p, float scale, float* grad_q,
+                                 float* grad_k, float* grad_v, float* grad_flows, float* grad_scores,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- frames held in 8 bits ------------------------------------------------
+ * A cache keeps keys and values of `slots` past frames per video of the batch,
+ * for programs that see one frame at a time.  It is four buffers of the caller,
+ * codes and scales of the keys and of the values:
+ *   codes   (B, slots, HD, H, W, Cp) bytes, OCP e4m3 (4 exponent, 3 mantissa
+ *           bits), 16-byte aligned; Cp is C/HD rounded up to a multiple of 16,
+ *           the channels past C/HD hold 0
+ *   scales  (B, slots, HD, ceil(H/block), ceil(W/block)) fp32, powers of two
+ * and stands for code * scale.  struct_size must be sizeof(snls_cache_params).
+ * Limits (SNLS_ERR_UNSUPPORTED): block 8 or 16, C/HD <= 256, H and W below
+ * 1,000,000, H*W*Cp below 2^31. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t B, slots, C, H, W, HD;
+  int32_t block; /* side in pixels of the blocks that share a scale (per head) */
+} snls_cache_params;
+
+/* snls_cache_store -- one frame of keys and values into the cache.  The scale
+ * of a block is the smallest power of two (2^-126 or more) with which its
+ * largest finite magnitude fits e4m3 (448); a value is its quotient by the scale, rounded to the
+ * nearest code, ties to even.  Infinities are held as +-448 * scale, NaN as NaN;
+ * a block of zeros has scale 1.
+ *   k, v     device, (B, C, H, W)
+ *   slots    device, int32 (B): the slot video b's frame goes to; a value
+ *            outside [0, cp->slots) leaves that video's cache as it is
+ *   k_codes, k_scales, v_codes, v_scales  device, in place: only the named
+ *            slots are written
+ * Errors: SNLS_ERR_INVALID_ARG (sizes, NULL buffers, misaligned codes),
+ * SNLS_ERR_UNSUPPORTED (limits above), SNLS_ERR_HIP. */
+snls_status snls_cache_store(const float* k, const float* v, const int32_t* slots, const snls_cache_params* cp,
+                             void* k_codes, float* k_scales, void* v_codes, float* v_scales, void* stream);
+
+/* snls_cache_attend -- attention of every pixel of a frame over its shifted
+ * windows in all cached frames, with no top-k: for pixel (h,w), head and slot s,
+ * the ws x ws candidates at displacement F + (d - ws/2), F the flow to the
+ * slot's frame, read bilinearly (taps outside the frame read 0).  A candidate
+ * counts if the slot holds a frame (age >= 0), |F| < 1e6 and its centre lies in
+ * [0,H-1] x [0,W-1]; its logit is scale * (q.k~ + table entry), its bucket that
+ * of the frame step -age and of the fp32 displacement; a logit that is not
+ * finite does not count.  out = sum of softmax(logits) * v~ over the candidates
+ * of all slots, 0 where none counts; v~'s taps of weight 0 are not read.
+ *   q        device, (B, C, H, W)
+ *   flows    device, (B, slots, 2, H, W), or NULL for offsets of 0
+ *   ages     device, int32 (B, slots): frames since the slot's, negative for
+ *            a slot that holds none (its codes may be anything)
+ *   table, bias  the position bias (device; host), or both NULL
+ *   ws       window side, 1 .. 15 (SNLS_ERR_UNSUPPORTED above)
+ *   scale    finite
+ *   out      device out, (B, C, H, W), fully overwritten
+ * The result does not depend on scheduling.  Errors: SNLS_ERR_INVALID_ARG,
+ * SNLS_ERR_UNSUPPORTED (limits of the cache and of the bias, 2^31 pixels and
+ * heads in all), SNLS_ERR_HIP. */
+snls_status snls_cache_attend(const float* q, const float* flows, const int32_t* ages, const void* k_codes,
+                              const float* k_scales, const void* v_codes, const float* v_scales,
+                              const float* table, const snls_cache_params* cp, const snls_bias_params* bias,
+                              int32_t ws, float scale, float* out, void* stream);
+
+/* snls_cache_attend_points -- the same for a list of n single pixels (tracked
+ * points, one token at a time; strided queries).
+ *   q        device, (n, C)
+ *   points   device, int32 (n, 3): video of the batch, row, column; a point
+ *            outside the batch or the frame gets a row of zeros
+ *   flows    device, (n, slots, 2), or NULL for offsets of 0
+ *   out      device out, (n, C), fully overwritten; nothing is touched when
+ *            n == 0
+ * Everything else as in snls_cache_attend; n < 0 is SNLS_ERR_INVALID_ARG. */
+snls_status snls_cache_attend_points(const float* q, const int32_t* points, int64_t n, const float* flows,
+                                     const int32_t* ages, const void* k_codes, const float* k_scales,
+                                     const void* v_codes, const float* v_scales, const float* table,
+                                     const snls_cache_params* cp, const snls_bias_params* bias, int32_t ws,
+                                     float scale, float* out, void* stream);
+
 #define SNLS_OP_SEARCH 0
 #define SNLS_OP_AGGREGATE 1
 #define SNLS_OP_BACKWARD 2
 #define SNLS_OP_AGGREGATE_STACKED 3
 #define SNLS_OP_GATHER_STACKED 4
 #define SNLS_OP_GATHER_REDUCE 5
+#define SNLS_OP_BIAS_BACKWARD 6
 
 /* Device workspace in bytes that operation op needs for parameters p
  * (0 when none is needed; (size_t)-1 for invalid arguments). */

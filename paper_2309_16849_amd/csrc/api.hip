@@ -32,6 +32,48 @@ size_t search_ws_bytes(const Geo& g, size_t have) {
   return r == SearchRoute::TileVector || r == SearchRoute::P1Scored ? tile_base_bytes(g) : 0;
 }
 
+snls_status backward_call(const float* q, const float* k, const float* v, const float* dists, const float* inds,
+                          const float* grad_out, const float* grad_dists, const snls_params* p, float scale,
+                          float* grad_q, float* grad_k, float* grad_v, float* grad_flows, float* grad_scores,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  Geo g;
+  snls_status st = check_params(p, true, &g);
+  if (st != SNLS_OK) return st;
+  if (!q || !k || !v || !dists || !inds || !grad_out || !grad_q || !grad_k || !grad_v) return SNLS_ERR_INVALID_ARG;
+  if (g.wt > 0 && !grad_flows) return SNLS_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return SNLS_ERR_INVALID_ARG;
+  size_t need = backward_ws_bytes(g);
+  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return SNLS_ERR_WORKSPACE;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_backward(q, k, v, dists, inds, grad_out, grad_dists, g, scale, grad_q, grad_k, grad_v, grad_flows,
+                         grad_scores, static_cast<float*>(workspace), as_stream(stream));
+}
+
+snls_status check_bias_call(const snls_params* p, const snls_bias_params* bias, Geo* g, Bias* b) {
+  snls_status st = check_params(p, false, g);
+  if (st != SNLS_OK) return st;
+  if ((st = check_bias(bias, b)) != SNLS_OK) return st;
+  if ((double)g->rows * (g->k > 0 ? g->k : g->ncand) > 1099511627776.0) return SNLS_ERR_UNSUPPORTED;
+  return SNLS_OK;
+}
+
+bool codes_ok(const void* codes) { return codes && !(reinterpret_cast<uintptr_t>(codes) & 15); }
+
+snls_status check_attend(const float* q, const int32_t* ages, const void* k_codes, const float* k_scales,
+                         const void* v_codes, const float* v_scales, const float* table,
+                         const snls_cache_params* cp, const snls_bias_params* bias, int32_t ws, float scale,
+                         const float* out, CacheGeo* c, Bias* b) {
+  snls_status st = check_cache(cp, c);
+  if (st != SNLS_OK) return st;
+  if (!q || !ages || !codes_ok(k_codes) || !k_scales || !codes_ok(v_codes) || !v_scales || !out)
+    return SNLS_ERR_INVALID_ARG;
+  if (ws < 1 || !std::isfinite(scale) || !table != !bias) return SNLS_ERR_INVALID_ARG;
+  if (ws > kMaxAttendWs) return SNLS_ERR_UNSUPPORTED;
+  *b = Bias{};
+  return bias ? check_bias(bias, b) : SNLS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -60,6 +102,7 @@ size_t snls_workspace_size(int op, const snls_params* p) {
   if (op == SNLS_OP_GATHER_STACKED) return check_params(p, true, &g) == SNLS_OK ? gather_ws_bytes(g) : (size_t)-1;
   if (op == SNLS_OP_GATHER_REDUCE)
     return check_params(p, true, &g) == SNLS_OK ? (size_t)g.B * g.T * g.C * g.HW * sizeof(float) : (size_t)-1;
+  if (op == SNLS_OP_BIAS_BACKWARD) return check_params(p, false, &g) == SNLS_OK ? bias_backward_ws_bytes(g) : (size_t)-1;
   return (size_t)-1;
 }
 
@@ -167,19 +210,90 @@ snls_status snls_backward(const float* q, const float* k, const float* v, const 
                           const float* inds, const float* grad_out, const float* grad_dists, const snls_params* p,
                           float scale, float* grad_q, float* grad_k, float* grad_v, float* grad_flows,
                           void* workspace, size_t workspace_bytes, void* stream) {
-  Geo g;
-  snls_status st = check_params(p, true, &g);
-  if (st != SNLS_OK) return st;
   (void)flows;  // positions come from inds; d disp / d flow = 1
-  if (!q || !k || !v || !dists || !inds || !grad_out || !grad_q || !grad_k || !grad_v) return SNLS_ERR_INVALID_ARG;
-  if (g.wt > 0 && !grad_flows) return SNLS_ERR_INVALID_ARG;
-  if (!std::isfinite(scale)) return SNLS_ERR_INVALID_ARG;
-  size_t need = backward_ws_bytes(g);
-  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+  return backward_call(q, k, v, dists, inds, grad_out, grad_dists, p, scale, grad_q, grad_k, grad_v, grad_flows,
+                       nullptr, workspace, workspace_bytes, stream);
+}
+
+snls_status snls_backward_scores(const float* q, const float* k, const float* v, const float* flows,
+                                 const float* dists, const float* inds, const float* grad_out,
+                                 const float* grad_dists, const snls_params* p, float scale, float* grad_q,
+                                 float* grad_k, float* grad_v, float* grad_flows, float* grad_scores,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  (void)flows;
+  if (!grad_scores) return SNLS_ERR_INVALID_ARG;
+  return backward_call(q, k, v, dists, inds, grad_out, grad_dists, p, scale, grad_q, grad_k, grad_v, grad_flows,
+                       grad_scores, workspace, workspace_bytes, stream);
+}
+
+snls_status snls_bias(const float* dists, const float* inds, const float* table, const snls_params* p,
+                      const snls_bias_params* bias, float* out, void* stream) {
+  Geo g;
+  Bias b;
+  snls_status st = check_bias_call(p, bias, &g, &b);
+  if (st != SNLS_OK) return st;
+  if (!dists || !inds || !table || !out) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_bias(dists, inds, table, g, b, out, as_stream(stream));
+}
+
+snls_status snls_bias_backward(const float* grad_scores, const float* dists, const float* inds, const snls_params* p,
+                               const snls_bias_params* bias, float* grad_table, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  Geo g;
+  Bias b;
+  snls_status st = check_bias_call(p, bias, &g, &b);
+  if (st != SNLS_OK) return st;
+  if (!grad_scores || !dists || !inds || !grad_table) return SNLS_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < bias_backward_ws_bytes(g) || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return SNLS_ERR_WORKSPACE;
   if ((st = device_ready()) != SNLS_OK) return st;
-  return launch_backward(q, k, v, dists, inds, grad_out, grad_dists, g, scale, grad_q, grad_k, grad_v, grad_flows,
-                         static_cast<float*>(workspace), as_stream(stream));
+  return launch_bias_backward(grad_scores, dists, inds, g, b, grad_table, static_cast<float*>(workspace),
+                              as_stream(stream));
+}
+
+snls_status snls_cache_store(const float* k, const float* v, const int32_t* slots, const snls_cache_params* cp,
+                             void* k_codes, float* k_scales, void* v_codes, float* v_scales, void* stream) {
+  CacheGeo c;
+  snls_status st = check_cache(cp, &c);
+  if (st != SNLS_OK) return st;
+  if (!k || !v || !slots || !codes_ok(k_codes) || !k_scales || !codes_ok(v_codes) || !v_scales)
+    return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_cache_store(k, v, slots, c, static_cast<uint8_t*>(k_codes), k_scales, static_cast<uint8_t*>(v_codes),
+                            v_scales, as_stream(stream));
+}
+
+snls_status snls_cache_attend(const float* q, const float* flows, const int32_t* ages, const void* k_codes,
+                              const float* k_scales, const void* v_codes, const float* v_scales,
+                              const float* table, const snls_cache_params* cp, const snls_bias_params* bias,
+                              int32_t ws, float scale, float* out, void* stream) {
+  CacheGeo c;
+  Bias b;
+  snls_status st = check_attend(q, ages, k_codes, k_scales, v_codes, v_scales, table, cp, bias, ws, scale, out, &c, &b);
+  if (st != SNLS_OK) return st;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_cache_attend(q, nullptr, (long long)c.B * c.H * c.W, flows, ages, static_cast<const uint8_t*>(k_codes),
+                             k_scales, static_cast<const uint8_t*>(v_codes), v_scales, table, c, b, ws, scale, out,
+                             as_stream(stream));
+}
+
+snls_status snls_cache_attend_points(const float* q, const int32_t* points, int64_t n, const float* flows,
+                                     const int32_t* ages, const void* k_codes, const float* k_scales,
+                                     const void* v_codes, const float* v_scales, const float* table,
+                                     const snls_cache_params* cp, const snls_bias_params* bias, int32_t ws,
+                                     float scale, float* out, void* stream) {
+  CacheGeo c;
+  Bias b;
+  snls_status st = check_attend(q, ages, k_codes, k_scales, v_codes, v_scales, table, cp, bias, ws, scale, out, &c, &b);
+  if (st != SNLS_OK) return st;
+  if (!points || n < 0) return SNLS_ERR_INVALID_ARG;
+  if ((double)n * c.HD >= 2147483648.0) return SNLS_ERR_UNSUPPORTED;
+  if (n == 0) return SNLS_OK;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_cache_attend(q, points, n, flows, ages, static_cast<const uint8_t*>(k_codes), k_scales,
+                             static_cast<const uint8_t*>(v_codes), v_scales, table, c, b, ws, scale, out,
+                             as_stream(stream));
 }
 
 }  // extern "C"

@@ -293,7 +293,8 @@ __global__ void __launch_bounds__(256) backward_search_kernel(const float* __res
                                                               const float* __restrict__ grad_dists, Geo g,
                                                               float scale, const float* __restrict__ Gws,
                                                               float* __restrict__ dqcl, float* __restrict__ dkcl,
-                                                              float* __restrict__ grad_flows) {
+                                                              float* __restrict__ grad_flows,
+                                                              float* __restrict__ dd_out) {
   const int lane = threadIdx.x & 63;
   const long long row = (long long)blockIdx.x * bwd::WAVES + (threadIdx.x >> 6);
   if (row >= g.rows) return;  // whole wave
@@ -314,11 +315,14 @@ __global__ void __launch_bounds__(256) backward_search_kernel(const float* __res
   for (int l = 0; l < g.k; ++l) {
     int t2, ny, nx;
     float ay, ax;
-    if (!isfinite(drow[l]) || !neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax)) continue;
+    const bool ok = isfinite(drow[l]) && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
     float dd = 0.f;
-    if (z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
-    if (grad_dists) dd += grad_dists[row * g.k + l];
-    if (dd == 0.f) continue;
+    if (ok) {
+      if (z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
+      if (grad_dists) dd += grad_dists[row * g.k + l];
+    }
+    if (dd_out && lane == 0) dd_out[row * g.k + l] = dd;
+    if (!ok || dd == 0.f) continue;
     const long long fbase = ((long long)rp.b * g.T + t2) * g.HW;
     float fh = 0.f, fw = 0.f;
     for (int c0 = 0; c0 < g.Ch; c0 += 64) {
@@ -1047,8 +1051,8 @@ static void zero(float* p, long long n, hipStream_t s) {
 
 snls_status launch_backward(const float* q, const float* k, const float* v, const float* dists, const float* inds,
                             const float* grad_out, const float* grad_dists, const Geo& g, float scale,
-                            float* grad_q, float* grad_k, float* grad_v, float* grad_flows, float* ws,
-                            hipStream_t s) {
+                            float* grad_q, float* grad_k, float* grad_v, float* grad_flows, float* grad_scores,
+                            float* ws, hipStream_t s) {
   const long long nvid = (long long)g.B * g.T * g.C * g.HW;
   const long long nflow = (long long)g.B * g.T * g.nslot * 2 * g.HW;
   const long long pairs = g.rows * (long long)g.k;
@@ -1074,7 +1078,7 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
   float* scratch = nullptr;
   if (binned) {
     const size_t nbb = align256((size_t)nbins * sizeof(unsigned));
-    ddws = reinterpret_cast<float*>(base);
+    ddws = grad_scores ? grad_scores : reinterpret_cast<float*>(base);  // dd_l is dL/d score
     base += pb;
     wlws = reinterpret_cast<float*>(base);
     base += pb;
@@ -1168,7 +1172,7 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
       hipLaunchKernelGGL(backward_agg_kernel, grid, block, 0, s, vcl, dists, inds, gocl, g, scale, dvcl, grad_flows,
                          Gws);
       hipLaunchKernelGGL(backward_search_kernel, grid, block, 0, s, qcl, kcl, dists, inds, grad_dists, g, scale,
-                         Gws, dqcl, dkcl, grad_flows);
+                         Gws, dqcl, dkcl, grad_flows, grad_scores);
     }
   }
   if (nvid > 0) {

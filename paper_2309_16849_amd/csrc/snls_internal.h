@@ -36,10 +36,26 @@ struct Geo {
 // kernels.
 constexpr float kFarDisp = 1.0e6f;
 
+// The position bias of a call, passed to kernels by value: the buckets of one
+// component are counted over `edges`, padded with +inf.
+struct Bias {
+  int radius, nE, nb, buckets;  // nb = 2*nE + 1, buckets = (2*radius + 1) * nb * nb
+  float edges[SNLS_BIAS_MAX_EDGES];
+};
+
+// The 8-bit frame cache of a call.  Cp: channels per head padded to 16; nv =
+// Cp / 16 16-byte vectors a token; sh: log2 of the block side.
+struct CacheGeo {
+  int B, S, C, HD, H, W, Ch, Cp, nv, sh, nby, nbx;
+};
+constexpr int kMaxAttendWs = 15;  // largest window side of the attention over it
+
 // Host-side checks (validate.cpp).  Return SNLS_OK or an error code; they
 // never touch the GPU.
 snls_status check_params(const snls_params* p, bool need_k, Geo* g);
 snls_status check_topk_args(int64_t rows, int32_t n_cand, int32_t k, int32_t dist_type);
+snls_status check_bias(const snls_bias_params* b, Bias* out);
+snls_status check_cache(const snls_cache_params* c, CacheGeo* out);
 
 // Device workspace of snls_aggregate: softmax weights (rows x k) then a
 // channels-last copy of V, 256-byte aligned.
@@ -56,6 +72,10 @@ size_t aggregate_stacked_ws_bytes(const Geo& g);
 bool gather_tile_supported(const Geo& g);
 bool reduce_supported(const Geo& g, int cout);
 size_t gather_ws_bytes(const Geo& g);
+
+// Device workspace of snls_bias_backward: one partial table per slice of the
+// scores.
+size_t bias_backward_ws_bytes(const Geo& g);
 
 // The tiled search path (any S_Q, P <= 7, Ws <= 9, at P = 7 Ws <= 15, S_K <= 1;
 // either distance) and its workspace without the matrix cores' operands: the
@@ -128,8 +148,21 @@ snls_status launch_gather_reduce(const float* v, const float* weights, const flo
                                  const Geo& g, int cout, float* out, void* ws, hipStream_t s);
 snls_status launch_backward(const float* q, const float* k, const float* v, const float* dists, const float* inds,
                             const float* grad_out, const float* grad_dists, const Geo& g, float scale,
-                            float* grad_q, float* grad_k, float* grad_v, float* grad_flows, float* Gws,
-                            hipStream_t s);
+                            float* grad_q, float* grad_k, float* grad_v, float* grad_flows, float* grad_scores,
+                            float* Gws, hipStream_t s);
+// k = 0: every candidate's score
+snls_status launch_bias(const float* dists, const float* inds, const float* table, const Geo& g, const Bias& bias,
+                        float* out, hipStream_t s);
+snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
+                                 const Bias& bias, float* grad_table, float* ws, hipStream_t s);
+snls_status launch_cache_store(const float* k, const float* v, const int32_t* slots, const CacheGeo& c,
+                               uint8_t* k_codes, float* k_scales, uint8_t* v_codes, float* v_scales, hipStream_t s);
+// points == nullptr: every pixel of a frame (q and out (B, C, H, W), flows
+// (B, S, 2, H, W)), else n listed pixels.
+snls_status launch_cache_attend(const float* q, const int32_t* points, long long n, const float* flows,
+                                const int32_t* ages, const uint8_t* k_codes, const float* k_scales,
+                                const uint8_t* v_codes, const float* v_scales, const float* table,
+                                const CacheGeo& c, const Bias& bias, int ws, float scale, float* out, hipStream_t s);
 
 // ---------------------------------------------------------------- device --
 

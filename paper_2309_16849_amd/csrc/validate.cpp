@@ -53,4 +53,44 @@ snls_status check_topk_args(int64_t rows, int32_t n_cand, int32_t k, int32_t dis
   return SNLS_OK;
 }
 
+snls_status check_bias(const snls_bias_params* b, Bias* out) {
+  if (!b || b->struct_size != sizeof(snls_bias_params)) return SNLS_ERR_INVALID_ARG;
+  if (b->radius < 0 || b->n_edges < 0) return SNLS_ERR_INVALID_ARG;
+  if (b->radius > 63 || b->n_edges > SNLS_BIAS_MAX_EDGES) return SNLS_ERR_UNSUPPORTED;
+  for (int i = 0; i < b->n_edges; ++i)
+    if (!isfinite(b->edges[i]) || !(b->edges[i] > (i ? b->edges[i - 1] : 0.f))) return SNLS_ERR_INVALID_ARG;
+  const int nb = 2 * b->n_edges + 1;
+  if ((2 * b->radius + 1) * nb * nb > SNLS_BIAS_MAX_BUCKETS) return SNLS_ERR_UNSUPPORTED;
+  out->radius = b->radius;
+  out->nE = b->n_edges;
+  out->nb = nb;
+  out->buckets = (2 * b->radius + 1) * nb * nb;
+  for (int i = 0; i < SNLS_BIAS_MAX_EDGES; ++i) out->edges[i] = i < b->n_edges ? b->edges[i] : INFINITY;
+  return SNLS_OK;
+}
+
+snls_status check_cache(const snls_cache_params* c, CacheGeo* out) {
+  if (!c || c->struct_size != sizeof(snls_cache_params)) return SNLS_ERR_INVALID_ARG;
+  if (c->B < 1 || c->slots < 1 || c->C < 1 || c->H < 1 || c->W < 1 || c->HD < 1 || c->block < 1)
+    return SNLS_ERR_INVALID_ARG;
+  if (c->C % c->HD != 0) return SNLS_ERR_INVALID_ARG;
+  const int Ch = c->C / c->HD;
+  if ((c->block != 8 && c->block != 16) || Ch > 256) return SNLS_ERR_UNSUPPORTED;
+  if (c->H >= (long long)kFarDisp || c->W >= (long long)kFarDisp) return SNLS_ERR_UNSUPPORTED;
+  const int Cp = (Ch + 15) / 16 * 16;
+  // a token's byte offset inside its plane is 32-bit; planes are found with 64 bits
+  if ((long long)c->H * c->W * Cp >= 1LL << 31) return SNLS_ERR_UNSUPPORTED;
+  // workgroups: one per head and some pixels at most
+  if ((double)c->B * c->HD * c->H * c->W >= 2147483648.0 || (double)c->B * c->slots >= 2147483648.0)
+    return SNLS_ERR_UNSUPPORTED;
+  out->B = c->B; out->S = c->slots; out->C = c->C; out->HD = c->HD; out->H = c->H; out->W = c->W;
+  out->Ch = Ch;
+  out->Cp = Cp;
+  out->nv = Cp / 16;
+  out->sh = c->block == 8 ? 3 : 4;
+  out->nby = (c->H + c->block - 1) / c->block;
+  out->nbx = (c->W + c->block - 1) / c->block;
+  return SNLS_OK;
+}
+
 }  // namespace snls

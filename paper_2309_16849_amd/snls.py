@@ -7,10 +7,15 @@ call raises.
 
 Functions carry the C names: snls_search, snls_topk, snls_aggregate,
 snls_backward, snls_aggregate_stacked, snls_chain_flows, snls_aggregate_static,
-snls_gather_stacked, snls_stacked_reduce, snls_gather_reduce, snls_workspace_size,
-snls_status_string, snls_abi_version.
+snls_gather_stacked, snls_stacked_reduce, snls_gather_reduce, snls_bias,
+snls_bias_backward, snls_backward_scores, snls_cache_store, snls_cache_attend,
+snls_cache_attend_points, snls_workspace_size, snls_status_string,
+snls_abi_version.
 Parameters are plain dicts with keys B, T, C, H, W, HD, ws, wt, ps, stride0,
-stride1, k, dist_type (see ``params_from_dict``).
+stride1, k, dist_type (see ``params_from_dict``); the position bias's with keys
+radius and edges (a list), a cache's with keys B, slots, C, H, W, HD, block.
+A cache is the tuple (k_codes, k_scales, v_codes, v_scales) that ``cache_alloc``
+returns.
 """
 from __future__ import annotations
 
@@ -26,11 +31,15 @@ SNLS_OK, SNLS_ERR_INVALID_ARG, SNLS_ERR_UNSUPPORTED, SNLS_ERR_HIP, SNLS_ERR_WORK
 SNLS_DIST_PROD, SNLS_DIST_L2 = 0, 1
 SNLS_OP_SEARCH, SNLS_OP_AGGREGATE, SNLS_OP_BACKWARD, SNLS_OP_AGGREGATE_STACKED = 0, 1, 2, 3
 SNLS_OP_GATHER_STACKED, SNLS_OP_GATHER_REDUCE = 4, 5
+SNLS_OP_BIAS_BACKWARD = 6
 SNLS_MAX_K = 128
+SNLS_BIAS_MAX_EDGES, SNLS_BIAS_MAX_BUCKETS = 16, 4096
 SNLS_STATIC_SCRATCH_BYTES = 64 << 20
 SYMBOLS = ("snls_search", "snls_topk", "snls_aggregate", "snls_backward", "snls_workspace_size",
            "snls_status_string", "snls_abi_version", "snls_aggregate_stacked", "snls_chain_flows",
-           "snls_aggregate_static", "snls_gather_stacked", "snls_stacked_reduce", "snls_gather_reduce")
+           "snls_aggregate_static", "snls_gather_stacked", "snls_stacked_reduce", "snls_gather_reduce",
+           "snls_bias", "snls_bias_backward", "snls_backward_scores", "snls_cache_store", "snls_cache_attend",
+           "snls_cache_attend_points")
 
 
 class SnlsParams(ctypes.Structure):
@@ -38,6 +47,18 @@ class SnlsParams(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32)] + [
         (n, ctypes.c_int32) for n in ("B", "T", "C", "H", "W", "HD", "ws", "wt", "ps", "stride0")
     ] + [("stride1", ctypes.c_float), ("k", ctypes.c_int32), ("dist_type", ctypes.c_int32)]
+
+
+class SnlsBiasParams(ctypes.Structure):
+    """Mirror of the C struct snls_bias_params."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("radius", ctypes.c_int32), ("n_edges", ctypes.c_int32),
+                ("edges", ctypes.c_float * SNLS_BIAS_MAX_EDGES)]
+
+
+class SnlsCacheParams(ctypes.Structure):
+    """Mirror of the C struct snls_cache_params."""
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("B", "slots", "C", "H", "W", "HD", "block")]
 
 
 class SnlsError(RuntimeError):
@@ -68,6 +89,13 @@ def load_library():
         lib.snls_gather_stacked.argtypes = [P, P, P, PP, P, P, SZ, P]
         lib.snls_stacked_reduce.argtypes = [P, P, PP, I32, P, P]
         lib.snls_gather_reduce.argtypes = [P, P, P, P, PP, I32, P, P, SZ, P]
+        PB, PC = ctypes.POINTER(SnlsBiasParams), ctypes.POINTER(SnlsCacheParams)
+        lib.snls_bias.argtypes = [P, P, P, PP, PB, P, P]
+        lib.snls_bias_backward.argtypes = [P, P, P, PP, PB, P, P, SZ, P]
+        lib.snls_backward_scores.argtypes = [P] * 8 + [PP, F32, P, P, P, P, P, P, SZ, P]
+        lib.snls_cache_store.argtypes = [P, P, P, PC, P, P, P, P, P]
+        lib.snls_cache_attend.argtypes = [P] * 8 + [PC, PB, I32, F32, P, P]
+        lib.snls_cache_attend_points.argtypes = [P, P, I64] + [P] * 7 + [PC, PB, I32, F32, P, P]
         lib.snls_workspace_size.argtypes = [ctypes.c_int, PP]
         lib.snls_workspace_size.restype = SZ
         lib.snls_status_string.argtypes = [ctypes.c_int]
@@ -75,7 +103,8 @@ def load_library():
         lib.snls_abi_version.argtypes = []
         for f in ("snls_search", "snls_topk", "snls_aggregate", "snls_backward", "snls_abi_version",
                   "snls_aggregate_stacked", "snls_chain_flows", "snls_aggregate_static", "snls_gather_stacked",
-                  "snls_stacked_reduce", "snls_gather_reduce"):
+                  "snls_stacked_reduce", "snls_gather_reduce", "snls_bias", "snls_bias_backward",
+                  "snls_backward_scores", "snls_cache_store", "snls_cache_attend", "snls_cache_attend_points"):
             getattr(lib, f).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -350,4 +379,211 @@ def snls_gather_reduce(v, weights, inds, proj, p: dict, out=None, workspace=None
     prm = params_from_dict(p)
     _check(lib.snls_gather_reduce(_ptr(v), _ptr(weights), _ptr(inds), _ptr(proj), ctypes.byref(prm), cout, _ptr(out),
                                   _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_gather_reduce")
+    return out
+
+
+# ------------------------------------------------------- learned position bias --
+
+def bias_from_dict(bias: dict) -> SnlsBiasParams:
+    s = SnlsBiasParams()
+    s.struct_size = ctypes.sizeof(SnlsBiasParams)
+    s.radius = int(bias["radius"])
+    edges = bias["edges"]
+    s.n_edges = len(edges)
+    if len(edges) <= SNLS_BIAS_MAX_EDGES:  # a longer list is refused by the library
+        for i, e in enumerate(edges):
+            s.edges[i] = e
+    return s
+
+
+def bias_table_shape(bias: dict, heads: int):
+    nb = 2 * len(bias["edges"]) + 1
+    return (heads, 2 * bias["radius"] + 1, nb, nb)
+
+
+def _here(*tensors):
+    """Every given tensor is on the current device, where the call will run."""
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != cur:
+            raise ValueError("tensors are on %s, the current device is cuda:%d" % (t.device, cur))
+
+
+def snls_bias(dists, inds, table, p: dict, bias: dict, out=None, stream=None):
+    """Scores plus the learned bias of their position; out may be dists."""
+    lib = load_library()
+    shp = out_shape(p)
+    _dev(dists, "dists", shp)
+    _dev(inds, "inds", shp + (3,))
+    _dev(table, "table", bias_table_shape(bias, p["HD"]))
+    if out is None:
+        out = torch.empty(shp, device=dists.device, dtype=torch.float32)
+    _dev(out, "out", shp)
+    _here(dists, inds, table, out)
+    prm, bprm = params_from_dict(p), bias_from_dict(bias)
+    _check(lib.snls_bias(_ptr(dists), _ptr(inds), _ptr(table), ctypes.byref(prm), ctypes.byref(bprm), _ptr(out),
+                         _stream(stream)), "snls_bias")
+    return out
+
+
+def snls_bias_backward(grad_scores, dists, inds, p: dict, bias: dict, grad_table=None, workspace=None, stream=None):
+    """Gradient of the bias table from the gradient of the (biased) scores."""
+    lib = load_library()
+    shp = out_shape(p)
+    _dev(grad_scores, "grad_scores", shp)
+    _dev(dists, "dists", shp)
+    _dev(inds, "inds", shp + (3,))
+    if grad_table is None:
+        grad_table = torch.empty(bias_table_shape(bias, p["HD"]), device=dists.device, dtype=torch.float32)
+    _dev(grad_table, "grad_table", bias_table_shape(bias, p["HD"]))
+    if workspace is None:
+        workspace = workspace_for(SNLS_OP_BIAS_BACKWARD, p, dists.device)
+    _here(grad_scores, dists, inds, grad_table, workspace)
+    prm, bprm = params_from_dict(p), bias_from_dict(bias)
+    _check(lib.snls_bias_backward(_ptr(grad_scores), _ptr(dists), _ptr(inds), ctypes.byref(prm), ctypes.byref(bprm),
+                                  _ptr(grad_table), _ptr(workspace), workspace.numel() * 4, _stream(stream)),
+           "snls_bias_backward")
+    return grad_table
+
+
+def snls_backward_scores(q, k, v, flows, dists, inds, grad_out, p: dict, scale: float = 1.0, grad_dists=None,
+                         workspace=None, stream=None):
+    """snls_backward's gradients and that of the scores: (grad_q, grad_k, grad_v, grad_flows, grad_scores)."""
+    lib = load_library()
+    vs, shp = video_shape(p), out_shape(p)
+    for t, n in ((q, "q"), (k, "k"), (v, "v"), (grad_out, "grad_out")):
+        _dev(t, n, vs)
+    _dev(dists, "dists", shp)
+    _dev(inds, "inds", shp + (3,))
+    if grad_dists is not None:
+        _dev(grad_dists, "grad_dists", shp)
+    if p["wt"] > 0 or flows is not None:
+        _dev(flows, "flows", flow_shape(p))
+    gq, gk, gv = (torch.empty(vs, device=q.device, dtype=torch.float32) for _ in range(3))
+    gf = torch.empty(flow_shape(p), device=q.device, dtype=torch.float32)
+    gs = torch.empty(shp, device=q.device, dtype=torch.float32)
+    if workspace is None:
+        workspace = workspace_for(SNLS_OP_BACKWARD, p, q.device)
+    _here(q, k, v, dists, inds, grad_out, grad_dists, flows, workspace)
+    prm = params_from_dict(p)
+    _check(lib.snls_backward_scores(_ptr(q), _ptr(k), _ptr(v), _ptr(flows), _ptr(dists), _ptr(inds), _ptr(grad_out),
+                                    _ptr(grad_dists), ctypes.byref(prm), float(scale), _ptr(gq), _ptr(gk), _ptr(gv),
+                                    _ptr(gf), _ptr(gs), _ptr(workspace), workspace.numel() * 4, _stream(stream)),
+           "snls_backward_scores")
+    return gq, gk, gv, gf, gs
+
+
+# ------------------------------------------------------- frames held in 8 bits --
+
+def cache_from_dict(cp: dict) -> SnlsCacheParams:
+    s = SnlsCacheParams()
+    s.struct_size = ctypes.sizeof(SnlsCacheParams)
+    for n in ("B", "slots", "C", "H", "W", "HD", "block"):
+        setattr(s, n, int(cp[n]))
+    return s
+
+
+def cache_shapes(cp: dict):
+    """Shapes of a cache's codes and of its scales."""
+    padded = (cp["C"] // cp["HD"] + 15) // 16 * 16
+    lead = (cp["B"], cp["slots"], cp["HD"])
+    return lead + (cp["H"], cp["W"], padded), lead + (-(-cp["H"] // cp["block"]), -(-cp["W"] // cp["block"]))
+
+
+def cache_alloc(cp: dict, device):
+    """The four buffers of an empty cache: (k_codes, k_scales, v_codes, v_scales)."""
+    codes, scales = cache_shapes(cp)
+
+    def one():
+        return (torch.zeros(codes, device=device, dtype=torch.uint8).view(torch.float8_e4m3fn),
+                torch.ones(scales, device=device, dtype=torch.float32))
+
+    return one() + one()
+
+
+def _dev_as(t, name, shape, dtypes):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous tensor of %s on the GPU" % (name, " or ".join(map(str, dtypes))))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t
+
+
+def _cache_ptrs(cache, cp):
+    codes, scales = cache_shapes(cp)
+    if len(cache) != 4:
+        raise ValueError("a cache is (k_codes, k_scales, v_codes, v_scales)")
+    for t, n in ((cache[0], "k_codes"), (cache[2], "v_codes")):
+        _dev_as(t, n, codes, (torch.float8_e4m3fn, torch.uint8))
+    _dev(cache[1], "k_scales", scales)
+    _dev(cache[3], "v_scales", scales)
+    return tuple(_ptr(t) for t in cache)
+
+
+def snls_cache_store(k, v, slots, cp: dict, cache, stream=None):
+    """One frame of keys and values (B, C, H, W) into the cache's slots (int32, one a video); returns the cache."""
+    lib = load_library()
+    shp = (cp["B"], cp["C"], cp["H"], cp["W"])
+    _dev(k, "k", shp)
+    _dev(v, "v", shp)
+    _dev_as(slots, "slots", (cp["B"],), (torch.int32,))
+    ptrs = _cache_ptrs(cache, cp)
+    _here(k, v, slots, *cache)
+    prm = cache_from_dict(cp)
+    _check(lib.snls_cache_store(_ptr(k), _ptr(v), _ptr(slots), ctypes.byref(prm), *ptrs, _stream(stream)),
+           "snls_cache_store")
+    return cache
+
+
+def _attend_common(cp, ages, cache, table, bias):
+    _dev_as(ages, "ages", (cp["B"], cp["slots"]), (torch.int32,))
+    if (table is None) != (bias is None):
+        raise ValueError("table and bias go together")
+    if table is not None:
+        _dev(table, "table", bias_table_shape(bias, cp["HD"]))
+    return _cache_ptrs(cache, cp), ctypes.byref(bias_from_dict(bias)) if bias is not None else None
+
+
+def snls_cache_attend(q, flows, ages, cache, cp: dict, ws: int, scale: float = 1.0, table=None, bias=None, out=None,
+                      stream=None):
+    """Every pixel of a frame q (B, C, H, W) attends its shifted windows in all cached frames; returns (B, C, H, W).
+    flows (B, slots, 2, H, W) or None; ages int32 (B, slots), negative for a slot that holds no frame."""
+    lib = load_library()
+    shp = (cp["B"], cp["C"], cp["H"], cp["W"])
+    _dev(q, "q", shp)
+    if flows is not None:
+        _dev(flows, "flows", (cp["B"], cp["slots"], 2, cp["H"], cp["W"]))
+    ptrs, bp = _attend_common(cp, ages, cache, table, bias)
+    if out is None:
+        out = torch.empty(shp, device=q.device, dtype=torch.float32)
+    _dev(out, "out", shp)
+    _here(q, flows, ages, table, out, *cache)
+    prm = cache_from_dict(cp)
+    _check(lib.snls_cache_attend(_ptr(q), _ptr(flows), _ptr(ages), *ptrs, _ptr(table), ctypes.byref(prm), bp, int(ws),
+                                 float(scale), _ptr(out), _stream(stream)), "snls_cache_attend")
+    return out
+
+
+def snls_cache_attend_points(q, points, flows, ages, cache, cp: dict, ws: int, scale: float = 1.0, table=None,
+                             bias=None, out=None, stream=None):
+    """Single pixels attend the cached frames: q (n, C), points int32 (n, 3) = video, row, column, flows
+    (n, slots, 2) or None; returns (n, C)."""
+    lib = load_library()
+    _dev(q, "q")
+    n = q.shape[0]
+    _dev(q, "q", (n, cp["C"]))
+    _dev_as(points, "points", (n, 3), (torch.int32,))
+    if flows is not None:
+        _dev(flows, "flows", (n, cp["slots"], 2))
+    ptrs, bp = _attend_common(cp, ages, cache, table, bias)
+    if out is None:
+        out = torch.empty((n, cp["C"]), device=q.device, dtype=torch.float32)
+    _dev(out, "out", (n, cp["C"]))
+    if n == 0:
+        return out
+    _here(q, points, flows, ages, table, out, *cache)
+    prm = cache_from_dict(cp)
+    _check(lib.snls_cache_attend_points(_ptr(q), _ptr(points), n, _ptr(flows), _ptr(ages), *ptrs, _ptr(table),
+                                        ctypes.byref(prm), bp, int(ws), float(scale), _ptr(out), _stream(stream)),
+           "snls_cache_attend_points")
     return out
