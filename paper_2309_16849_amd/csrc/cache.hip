@@ -121,9 +121,8 @@ struct AttendArgs {
   float* out;
 };
 
-// acc += dot of 16 codes with q (or, in spread16, acc[i] += w * code i).
-SNLS_DEV float dot16(uint4 t, const float* q) {
-  float s = 0.f;
+// s plus the dot product of 16 codes with q; spread16: acc[i] += wgt * code i.
+SNLS_DEV float dot16(uint4 t, const float* q, float s) {
   const unsigned w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -151,7 +150,7 @@ SNLS_DEV void spread16(uint4 t, float wgt, float* acc) {
 // [0, n-1].
 SNLS_DEV bool cell_ok(int y, bool frac, int n) { return y >= 0 && (frac ? y < n - 1 : y < n); }
 
-// One query and head, SPLIT waves: wave i takes the slots i, i + SPLIT, ...;
+// One listed query and head, SPLIT waves: wave i takes the slots i, i + SPLIT, ...;
 // the waves' maxima, sums and outputs are joined in LDS.  Within a wave G
 // lanes hold the channels of a token (16 each), 64 / G tokens are read at a
 // time.
@@ -171,18 +170,8 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
   const int ws = a.ws, nt = ws + 1, r = ws / 2, pitch = ws + 2;
   float* taps = taps_[wv];
   float* cells = cells_[wv];
-  int b, h, w;
+  const int b = a.points[3 * qi], h = a.points[3 * qi + 1], w = a.points[3 * qi + 2];
   const long long HW = (long long)c.H * c.W;
-  if (a.points) {
-    b = a.points[3 * qi];
-    h = a.points[3 * qi + 1];
-    w = a.points[3 * qi + 2];
-  } else {
-    b = (int)(qi / HW);
-    const int pix = (int)(qi - b * HW);
-    h = pix / c.W;
-    w = pix - h * c.W;
-  }
   const bool inb = b >= 0 && b < c.B && h >= 0 && h < c.H && w >= 0 && w < c.W;
   const int vec = lane & (G - 1), tok = lane / G;
   const bool vlive = vec < c.nv;
@@ -192,11 +181,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
     const int ch = vec * 16 + i;
     q[i] = 0.f;
     acc[i] = 0.f;
-    if (inb && ch < c.Ch) {
-      const long long at = a.points ? qi * c.C + hd * c.Ch + ch
-                                    : ((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w;
-      q[i] = a.q[at];
-    }
+    if (inb && ch < c.Ch) q[i] = a.q[qi * c.C + hd * c.Ch + ch];
   }
   for (int i = lane; i < (ws + 2) * (ws + 2); i += 64) cells[i] = 0.f;
   float m = -INFINITY, z = 0.f;  // running maximum (of the wave) and this lane's sum
@@ -206,9 +191,8 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
       if (age < 0) continue;
       float Fh = 0.f, Fw = 0.f;
       if (a.flows) {
-        const long long at = a.points ? (qi * c.S + s) * 2 : (((long long)b * c.S + s) * 2 * HW + (long long)h * c.W + w);
-        Fh = a.flows[at];
-        Fw = a.flows[at + (a.points ? 1 : HW)];
+        Fh = a.flows[(qi * c.S + s) * 2];
+        Fw = a.flows[(qi * c.S + s) * 2 + 1];
       }
       if (!(fabsf(Fh) < kFarDisp && fabsf(Fw) < kFarDisp)) continue;
       int nh, nw;
@@ -228,7 +212,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
         const bool in = t < nt * nt && y >= 0 && y < c.H && x >= 0 && x < c.W;
         float d = 0.f;
         if (in && vlive) {
-          d = dot16(*reinterpret_cast<const uint4*>(kp + (unsigned)((y * c.W + x) * c.Cp + vec * 16)), q);
+          d = dot16(*reinterpret_cast<const uint4*>(kp + (unsigned)((y * c.W + x) * c.Cp + vec * 16)), q, 0.f);
           d *= ksp[(y >> c.sh) * c.nbx + (x >> c.sh)];
         }
 #pragma unroll
@@ -327,9 +311,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
           Z += f * join_mz[i][1];
           o += f * join_acc[i][ch];
         }
-    const long long at = a.points ? qi * c.C + hd * c.Ch + ch
-                                  : ((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w;
-    a.out[at] = Z > 0.f ? o / Z : 0.f;
+    a.out[qi * c.C + hd * c.Ch + ch] = Z > 0.f ? o / Z : 0.f;
   }
 }
 
@@ -348,15 +330,406 @@ static void run_attend_wave(const AttendArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((attend_wave_kernel<16, SPLIT>), grid, block, 0, s, a);
 }
 
+// --- four lanes per query ---
+//
+// Sixteen queries per wave.  The four lanes of a query read 64 consecutive
+// bytes of a tap row at a time: R lanes hold the channels of a token, 16 * V
+// each, and 4 / R tokens are read at once.  Whatever R, lane l ends up with
+// the scores of the tap columns l, l + 4, ... and computes the cells of these
+// columns; neighbouring columns are exchanged through DPP.  The rows of taps
+// stream by: key row i completes cell row i - 1, whose weights complete the
+// taps of value row i - 1; the softmax's maximum is a running one, so nothing
+// but two rows is kept.
+//
+// Logits are held in base 2 (q and the table are multiplied by scale * log2 e
+// as they are read).  The maximum follows the logits only in steps of more
+// than kSlack, so that the outputs are rescaled once or twice per frame, not
+// per row: weights are then at most 2^kSlack, far from fp32's limits.
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kSlack = 12.f;
+// Loads of a tap row (K * R * V) up to which the values' are issued beside the
+// keys', a row's arithmetic ahead of their use: 4 heads of 16 channels at 256 x
+// 256 0.74 -> 0.70 ms, 64 channels at 480 x 854 1.53 -> 1.41 ms; above it the
+// registers would halve the waves.
+constexpr int kAhead = 12;
+
+// Keeps a loaded value from being read again, later, inside a branch.
+SNLS_DEV void pin(uint4& t) { asm volatile("" : "+v"(t.x), "+v"(t.y), "+v"(t.z), "+v"(t.w)); }
+
+// Lane i of each quad gets the value of lane P_i.
+template <int P0, int P1, int P2, int P3>
+SNLS_DEV float quad(float v) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(
+      0, (int)__float_as_uint(v), P0 | (P1 << 2) | (P2 << 4) | (P3 << 6), 0xf, 0xf, true));
+}
+
+// A finite table entry stays finite in base 2 (a mask of the lowest value is
+// no mask of -inf).
+SNLS_DEV float table_base2(float t, float scale) {
+  const float x = t * scale;
+  return fabsf(x) < INFINITY ? fminf(fmaxf(x * kLog2e, -3.402823466e38f), 3.402823466e38f) : x;
+}
+
+// The loads of a tap row stand together, with no branch between them, so that
+// they are under way at the same time: CT columns of taps are read whatever ws
+// is (those past the window at the clamped address, unused).
+//
+// split (1, 2 or 4) waves share 16 queries, each takes every split-th slot,
+// and the first joins their maxima, sums and outputs through LDS: for calls
+// whose queries alone are too few waves for the chip.
+template <int CT, int R, int V, bool POINTS>
+__global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
+  constexpr int K = (CT + 3) / 4;
+  extern __shared__ float lds[];  // row buckets of the four waves' queries, then the head's bias table
+  const CacheGeo& c = a.c;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int l = lane & 3, sub = lane >> 2;
+  const int groups = 4 / split, group = wv / split, part_of = wv % split;  // of 16 queries; of the slots
+  const int ws = a.ws, r = ws / 2;
+  const long long HW = (long long)c.H * c.W;
+  // the wave's queries: 8 x 2 pixels of the workgroup's tile, or 16 listed points
+  int b, hd, h, w;
+  long long qi = 0;
+  bool live;
+  if constexpr (POINTS) {
+    const long long blocks = (a.n + groups * 16 - 1) / (groups * 16);
+    hd = (int)(blockIdx.x / blocks);
+    qi = (blockIdx.x - hd * blocks) * (groups * 16) + group * 16 + sub;
+    live = qi < a.n;
+    if (!live) qi = a.n - 1;
+    b = a.points[3 * qi];
+    h = a.points[3 * qi + 1];
+    w = a.points[3 * qi + 2];
+  } else {
+    // consecutive workgroups land on different XCDs: each XCD takes a
+    // contiguous run of tiles, ordered in strips of 8 tiles, whose windows fit its L2
+    const int tiles = tiles_x * tiles_y, total = tiles * c.B * c.HD, per = (total + 7) / 8;
+    const int id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if (id >= total || (int)(blockIdx.x >> 3) >= per) return;  // the whole workgroup
+    const int img = id / tiles, tile = id % tiles;
+    b = img / c.HD;
+    hd = img % c.HD;
+    const int strip = tile / (8 * tiles_y), rest = tile % (8 * tiles_y), width = min(8, tiles_x - strip * 8);
+    h = (rest / width * groups + group) * 2 + (sub >> 3);
+    w = (strip * 8 + rest % width) * 8 + (sub & 7);
+    live = h < c.H && w < c.W;
+  }
+  const bool stored = live;  // has a row of out
+  if constexpr (POINTS) {
+    live = live && b >= 0 && b < c.B && h >= 0 && h < c.H && w >= 0 && w < c.W;
+    if (!live) b = 0;  // (without points b is uniform, and so are the addresses of the planes)
+  }
+  if (!live) h = w = 0;
+  int* rowb = reinterpret_cast<int*>(lds) + threadIdx.x / 4 * 16;  // of this query: table row per tap row
+  float* tab = lds + 64 * 16;
+  for (int i = threadIdx.x; i < max(a.bias.buckets, 1); i += 256)
+    tab[i] = a.table ? table_base2(a.table[(long long)hd * a.bias.buckets + i], a.scale) : 0.f;
+  __syncthreads();
+  const int lr = l & (R - 1);  // this lane's part of a token
+  float q[V][16], acc[V][16];
+  int voff[V];  // byte offset of the lane's vector v from its first
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    voff[v] = v * R + lr < c.nv ? v * R * 16 : 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int ch = (v * R + lr) * 16 + i;
+      acc[v][i] = 0.f;
+      q[v][i] = 0.f;
+      if (live && ch < c.Ch)
+        q[v][i] = (a.scale * kLog2e) * (POINTS ? a.q[qi * c.C + hd * c.Ch + ch]
+                                               : a.q[((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w]);
+    }
+  }
+  const int lane0 = min(lr, c.nv - 1) * 16, rowbytes = c.W * c.Cp;
+  float m = -INFINITY, z = 0.f;
+  for (int s = part_of; s < c.S; s += split) {
+    const int age = a.ages[(long long)b * c.S + s];
+    if (!POINTS && age < 0) continue;
+    float Fh = 0.f, Fw = 0.f;
+    if (a.flows) {
+      const long long at = POINTS ? (qi * c.S + s) * 2 : (((long long)b * c.S + s) * 2 * HW + (long long)h * c.W + w);
+      Fh = a.flows[at];
+      Fw = a.flows[at + (POINTS ? 1 : HW)];
+    }
+    const bool on = live && age >= 0 && fabsf(Fh) < kFarDisp && fabsf(Fw) < kFarDisp;
+    if (!__any(on)) continue;
+    if (!on) Fh = Fw = 0.f;
+    int nh, nw;
+    float ay, ax;
+    split_disp(Fh, &nh, &ay);
+    split_disp(Fw, &nw, &ax);
+    const int y0 = h + nh - r, x0 = w + nw - r;
+    const long long img = ((long long)b * c.S + s) * c.HD + hd;
+    const uint8_t* kp = a.kc + img * HW * c.Cp;
+    const uint8_t* vp = a.vc + img * HW * c.Cp;
+    const float* ksp = a.ks + img * c.nby * c.nbx;
+    const float* vsp = a.vs + img * c.nby * c.nbx;
+    // byte offsets of the tap columns this lane reads; its own columns' scales
+    // (a window meets at most three rows of blocks), validity and buckets
+    int xoff[K][R];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int col = R == 1 ? 4 * k + l : R == 2 ? 4 * k + (l & 2) + i : 4 * k + i;
+        xoff[k][i] = (int)__umul24((unsigned)min(max(x0 + col, 0), c.W - 1), (unsigned)c.Cp) + lane0;
+      }
+    float ksc[3][K], vsc[3][K];
+    int cb[K];
+    bool cok[K], tin[K];
+    const int yb0 = y0 >> c.sh;
+    // table index of (step, row bucket 0 ..) plus the column's; rows are looked up in LDS
+    const int bt = bias_step_bucket(-age, a.bias) * a.bias.nb * a.bias.nb;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int col = 4 * k + l, x = x0 + col;
+      tin[k] = x >= 0 && x < c.W && col <= ws;
+      cok[k] = on && col < ws && cell_ok(x, ax != 0.f, c.W);
+      const int xb = min(max(x, 0), c.W - 1) >> c.sh;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const unsigned at = (unsigned)(min(max(yb0 + i, 0), c.nby - 1) * c.nbx + xb);
+        ksc[i][k] = ksp[at];
+        vsc[i][k] = vsp[at];
+      }
+      cb[k] = bt + bias_bucket(Fw + (float)(col - r), a.bias);
+      rowb[col] = bias_bucket(Fh + (float)(col - 1 - r), a.bias) * a.bias.nb;  // for tap row col: cell row col - 1
+    }
+    wave_lds_sync();
+    const bool fy = ay != 0.f;
+    float hprev[K], pprev[K], p[K], vsk[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) hprev[k] = pprev[k] = p[k] = vsk[k] = 0.f;
+    int yov = 0;  // byte offset of the value row
+    auto load_row = [&](const uint8_t* plane, int yoff, uint4* to) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (4 * k + (R == 1 ? 0 : i) < CT)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+              to[(k * R + i) * V + v] = *reinterpret_cast<const uint4*>(plane + (unsigned)(yoff + xoff[k][i] + (v ? voff[v] : 0)));
+    };
+    for (int row = 0; row <= ws + 1; ++row) {
+      const int y = y0 + row;
+      const bool yin = (unsigned)y < (unsigned)c.H;
+      const int yo = min(max(y, 0), c.H - 1) * rowbytes;
+      const int dyb = (y >> c.sh) - yb0;
+      uint4 kb[K * R * V], vb[K * R * V];
+      if (row <= ws) load_row(kp, yo, kb);
+      if constexpr (K * R * V <= kAhead) load_row(vp, yov, vb);
+      float sc[K + 1];
+#pragma unroll
+      for (int k = 0; k <= K; ++k) sc[k] = 0.f;
+      const int rb = rowb[min(row, 4 * K - 1)];
+      if (row <= ws) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          float part[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            part[i] = 0.f;
+            if (4 * k + (R == 1 ? 0 : i) < CT)
+#pragma unroll
+              for (int v = 0; v < V; ++v) part[i] = dot16(kb[(k * R + i) * V + v], q[v], part[i]);
+          }
+          float d;
+          if constexpr (R == 1) {
+            d = part[0];
+          } else if constexpr (R == 2) {
+            part[0] += quad<1, 0, 3, 2>(part[0]);
+            part[1] += quad<1, 0, 3, 2>(part[1]);
+            d = (l & 1) ? part[1] : part[0];
+          } else {  // lane l keeps the sum of part l
+            const float u0 = ((l & 1) ? part[1] : part[0]) + quad<1, 0, 3, 2>((l & 1) ? part[0] : part[1]);
+            const float u1 = ((l & 1) ? part[3] : part[2]) + quad<1, 0, 3, 2>((l & 1) ? part[2] : part[3]);
+            d = ((l & 2) ? u1 : u0) + quad<2, 3, 0, 1>((l & 2) ? u0 : u1);
+          }
+          const float sk = dyb <= 0 ? ksc[0][k] : dyb == 1 ? ksc[1][k] : ksc[2][k];
+          sc[k] = yin && tin[k] ? d * sk : 0.f;
+        }
+      }
+      const bool rok = (unsigned)(row - 1) < (unsigned)ws && cell_ok(y - 1, fy, c.H);
+      float lg[K], top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const float right = quad<1, 2, 3, 0>(l == 0 ? sc[k + 1] : sc[k]);  // column + 1
+        const float hrow = fmaf(ax, right - sc[k], sc[k]);
+        const float x = fmaf(ay, hrow - hprev[k], hprev[k]) + tab[rb + cb[k]];
+        lg[k] = rok && cok[k] && fabsf(x) < INFINITY ? x : -INFINITY;
+        top = fmaxf(top, lg[k]);
+        hprev[k] = hrow;
+      }
+      top = fmaxf(top, quad<1, 0, 3, 2>(top));
+      top = fmaxf(top, quad<2, 3, 0, 1>(top));
+      const bool lift = top > m + kSlack;  // also from -inf
+      if (__any(lift)) {
+        const float m2 = lift ? top : m, f = lift ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+        m = m2;
+        z *= f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) pprev[k] *= f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[v][i] *= f;
+      }
+      const float mm = fmaxf(m, -3.402823466e38f);  // nothing counted yet: weights 2^-inf
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        p[k] = __builtin_amdgcn_exp2f(lg[k] - mm);
+        z += p[k];
+      }
+      if (row > 0) {  // values of the row above (its scales and validity were found with its keys)
+        if constexpr (K * R * V > kAhead) load_row(vp, yov, vb);
+#pragma unroll
+        for (int n = 0; n < K * R * V; ++n)
+          if (4 * (n / (R * V)) + (R == 1 ? 0 : n / V % R) < CT) pin(vb[n]);
+        float g[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) g[k] = fmaf(ay, pprev[k] - p[k], p[k]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const float left = quad<3, 0, 1, 2>(l == 3 ? (k ? g[k ? k - 1 : 0] : 0.f) : g[k]);  // column - 1
+          const float wgt = fmaf(ax, left - g[k], g[k]) * vsk[k];
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const float wi = R == 1 ? wgt
+                             : R == 2 ? (i == 0 ? quad<0, 0, 2, 2>(wgt) : quad<1, 1, 3, 3>(wgt))
+                                      : (i == 0   ? quad<0, 0, 0, 0>(wgt)
+                                         : i == 1 ? quad<1, 1, 1, 1>(wgt)
+                                         : i == 2 ? quad<2, 2, 2, 2>(wgt)
+                                                  : quad<3, 3, 3, 3>(wgt));
+            if (4 * k + (R == 1 ? 0 : i) < CT && wi != 0.f)
+#pragma unroll
+              for (int v = 0; v < V; ++v) spread16(vb[(k * R + i) * V + v], wi, acc[v]);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        pprev[k] = p[k];
+        const float sv = dyb <= 0 ? vsc[0][k] : dyb == 1 ? vsc[1][k] : vsc[2][k];
+        vsk[k] = yin && tin[k] ? sv : 0.f;
+      }
+      yov = yo;
+    }
+    wave_lds_sync();
+  }
+  // the waves that share the queries, one after the other
+  if (split > 1) {
+    float* buf = lds + group * (64 * (2 + 16 * V)) + lane;  // (over the buckets and the table)
+    for (int j = 1; j < split; ++j) {
+      __syncthreads();
+      if (part_of == j) {
+        buf[0] = m;
+        buf[64] = z;
+#pragma unroll
+        for (int i = 0; i < 16 * V; ++i) buf[(2 + i) * 64] = acc[i / 16][i % 16];
+      }
+      __syncthreads();
+      if (part_of == 0) {
+        const float mj = buf[0], top = fmaxf(m, mj);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float fj = mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - top);
+        m = top;
+        z = z * f + buf[64] * fj;
+#pragma unroll
+        for (int i = 0; i < 16 * V; ++i) acc[i / 16][i % 16] = acc[i / 16][i % 16] * f + buf[(2 + i) * 64] * fj;
+      }
+    }
+    if (part_of != 0) return;
+  }
+  // sums over the quad: the weights' sum, and the outputs of lanes that hold the same channels
+  z += quad<1, 0, 3, 2>(z);
+  z += quad<2, 3, 0, 1>(z);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (R == 1) acc[v][i] += quad<1, 0, 3, 2>(acc[v][i]);
+      if constexpr (R <= 2) acc[v][i] += quad<2, 3, 0, 1>(acc[v][i]);
+    }
+  if (!stored) return;
+  const float inv = z > 0.f ? 1.f / z : 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int ch = (v * R + lr) * 16 + i;
+      if (i / (4 * R) != l / R || ch >= c.Ch) continue;  // each lane stores its share
+      const float o = z > 0.f ? acc[v][i] * inv : 0.f;
+      if constexpr (POINTS)
+        a.out[qi * c.C + hd * c.Ch + ch] = o;
+      else
+        a.out[((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w] = o;
+    }
+}
+
+template <int CT, bool POINTS>
+static void run_attend_quad(const AttendArgs& a, int split, hipStream_t s) {
+  const CacheGeo& c = a.c;
+  const int groups = 4 / split, tx = (c.W + 7) / 8, ty = (c.H + 2 * groups - 1) / (2 * groups);
+  const long long blocks = POINTS ? (a.n + groups * 16 - 1) / (groups * 16) : (long long)c.B * tx * ty;
+  const dim3 grid((unsigned)(POINTS ? blocks * c.HD : (blocks * c.HD + 7) / 8 * 8)), block(256);
+  size_t lds = (64 * 16 + (a.table ? a.bias.buckets : 1)) * sizeof(float);
+  auto room = [&](int V) {
+    const size_t join = split > 1 ? (size_t)groups * 64 * (2 + 16 * V) * sizeof(float) : 0;
+    return join > lds ? join : lds;
+  };
+#define SNLS_QUAD(R, V) \
+  hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, POINTS>), grid, block, room(V), s, a, tx, ty, split)
+  switch (c.nv) {
+    case 1: SNLS_QUAD(1, 1); break;
+    case 2: SNLS_QUAD(2, 1); break;
+    case 3: SNLS_QUAD(1, 3); break;
+    case 4: SNLS_QUAD(4, 1); break;
+    case 6: SNLS_QUAD(2, 3); break;
+    case 5: case 7: case 8: SNLS_QUAD(4, 2); break;
+    case 9: case 10: case 11: case 12: SNLS_QUAD(4, 3); break;
+    default: SNLS_QUAD(4, 4); break;
+  }
+#undef SNLS_QUAD
+}
+
+template <bool POINTS>
+static void run_attend(const AttendArgs& a, hipStream_t s) {
+  const CacheGeo& c = a.c;
+  // waves per 16 queries: the chip has 1,024 places for a wave.  Split by 1 / 2 / 4 (4 slots, ws = 9): 4 heads of
+  // 16 channels 46 / 25 / 17 us at 48 x 48 (576 waves), 46 / 32 / 34 us at 64 x 64 (1,024), 71 / 61 us at 96 x 96
+  // (2,304), 97 / 93 us at 128 x 128 (4,096)
+  const long long waves = (a.n + 15) / 16 * c.HD;
+  int split = waves >= 4096 ? 1 : waves >= 1024 ? 2 : 4;
+  while (split > c.S) split /= 2;
+  if (a.ws <= 3)
+    run_attend_quad<4, POINTS>(a, split, s);
+  else if (a.ws <= 5)
+    run_attend_quad<6, POINTS>(a, split, s);
+  else if (a.ws <= 7)
+    run_attend_quad<8, POINTS>(a, split, s);
+  else if (a.ws <= 9)
+    run_attend_quad<10, POINTS>(a, split, s);
+  else if (a.ws <= 11)
+    run_attend_quad<12, POINTS>(a, split, s);
+  else
+    run_attend_quad<16, POINTS>(a, split, s);
+}
+
 snls_status launch_cache_attend(const float* q, const int32_t* points, long long n, const float* flows,
                                 const int32_t* ages, const uint8_t* k_codes, const float* k_scales,
                                 const uint8_t* v_codes, const float* v_scales, const float* table,
                                 const CacheGeo& c, const Bias& bias, int ws, float scale, float* out, hipStream_t s) {
   const AttendArgs a{q, points, n, flows, ages, k_codes, k_scales, v_codes, v_scales, table, c, bias, ws, scale, out};
-  if (points)
+  // few points: a wave each for the shortest way through one query.  Wave / quads (6 slots, ws = 9): one head of 64
+  // channels 30 / 51 us for 1,024 points, 56 / 52 us for 2,048; 4 heads of 16 29 / 32 us for 512, 51 / 33 us for 1,024
+  if (points && n * c.HD <= 2048)
     run_attend_wave<4>(a, s);
+  else if (points)
+    run_attend<true>(a, s);
   else
-    run_attend_wave<1>(a, s);
+    run_attend<false>(a, s);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 

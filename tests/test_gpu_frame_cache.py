@@ -390,3 +390,38 @@ def test_side_stream_and_two_calls(dev):
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("C,HD,ws,slots", [(16, 1, 2, 5), (24, 1, 4, 1), (40, 1, 6, 2), (64, 1, 10, 4), (70, 1, 3, 3),
+                                           (96, 1, 12, 2), (130, 1, 9, 2), (250, 1, 5, 4), (48, 3, 9, 3),
+                                           (112, 1, 15, 2)], ids=str)
+def test_long_lists_of_points(dev, C, HD, ws, slots):
+    """Lists long enough for four lanes a point, for every grouping of channels and window width: the same as the dense
+    form, sampled against 64 bits, with points outside the frame among them."""
+    cp = _cp(B=2, C=C, HD=HD, H=47, W=45, slots=slots)
+    g = torch.Generator().manual_seed(21)
+    cache, kv, vv = _filled(cp, dev)
+    bias = dict(radius=2, edges=[0.5, 2.0, 5.0])
+    table = torch.randn(B.bias_table_shape(bias, HD), generator=g)
+    ages = torch.randint(-1, 4, (2, slots), generator=g).to(torch.int32)
+    ages[:, 0] = 1
+    q = 2 * torch.randn(2, C, 47, 45, generator=g)
+    fl = 3 * torch.randn(2, slots, 2, 47, 45, generator=g)
+    scale = 1.0 / (C // HD) ** 0.5
+    print("points", cp, ws, flush=True)
+    a, b, qa, allp, fa = _both(dev, cp, ws, q, fl, ages, cache, scale, table, bias)
+    pick = torch.randint(0, qa.shape[0], (24,), generator=g)
+    ref, big = R.attend(qa[pick], allp[pick], fa[pick], ages, kv, vv, cp, ws, scale, table, bias)
+    tol = _tol(qa, kv, vv, cp, ws, scale, big, table)
+    assert float((a[pick].double() - ref).abs().max()) <= tol
+    assert float((b[pick].double() - ref).abs().max()) <= tol
+    assert float((a - b).abs().max()) <= 2 * tol
+    bad = allp.clone()
+    bad[5::7, 0] = 2
+    bad[6::7, 1] = -3
+    to = lambda x: x.to(dev)  # noqa: E731
+    got = B.snls_cache_attend_points(to(qa), to(bad), to(fa), to(ages), cache, cp, ws, scale, table=to(table), bias=bias)
+    got = got.cpu()
+    keep = torch.ones(len(bad), dtype=torch.bool)
+    keep[5::7] = keep[6::7] = False
+    assert bool((got[~keep] == 0).all()) and torch.equal(got[keep], b[keep])
