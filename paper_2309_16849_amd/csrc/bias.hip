@@ -3,133 +3,212 @@
 //
 // A neighbour's entry is table[hd, step, bucket(dh), bucket(dw)].  Both
 // directions read 16 or 20 bytes a neighbour and write 4 or (almost) nothing,
-// so memory bandwidth bounds them.
+// so memory bandwidth bounds them.  The scores of one image -- one head of one
+// query frame, nH * nW * k of them -- lie together and share the query frame
+// and the head's table; they are walked in chunks of 256 per wave, four
+// consecutive neighbours a lane, in 16-byte reads.
 #include "position_bias.h"
 
 namespace snls {
 
-// Scores of one image (one head of one query frame: nH * nW * k of them lie
-// together, with one frame index and one table) per group of workgroups.
+constexpr int kChunk = 256;  // neighbours a wave takes at a time
+
 struct BiasRows {
   long long per_image;  // scores of an image
-  int T, HD;
+  long long chunks;     // of an image
+  int B, T, HD;
 };
 
 static BiasRows bias_rows(const Geo& g) {
-  return {(long long)g.nH * g.nW * (g.k > 0 ? g.k : g.ncand), g.T, g.HD};
+  const long long n = (long long)g.nH * g.nW * (g.k > 0 ? g.k : g.ncand);
+  return {n, (n + kChunk - 1) / kChunk, g.B, g.T, g.HD};
 }
 
-// Flat bucket of a neighbour of query frame t, or -1 when it contributes
-// nothing to the aggregation.
-SNLS_DEV int neighbour_bucket(float frame, float dh, float dw, int t, int T, const Bias& b) {
-  const bool ok = frame >= 0.f && frame < (float)T && frame == floorf(frame) && fabsf(dh) < kFarDisp &&
-                  fabsf(dw) < kFarDisp;
-  if (!ok) return -1;
-  return (bias_step_bucket((int)frame - t, b) * b.nb + bias_bucket(dh, b)) * b.nb + bias_bucket(dw, b);
+// Four floats at any 4-byte address.
+struct __attribute__((packed, aligned(4))) Float4 {
+  float x, y, z, w;
+};
+
+// A lane's four neighbours: flat buckets, -1 for one that contributes nothing
+// to the aggregation.  cnt: how many of them there are (4 but at an image's
+// end, where they are read one by one).
+struct Quartet {
+  float ind[12];
+  SNLS_DEV void load(const float* __restrict__ inds, int cnt) {
+    if (cnt == 4) {
+      const Float4* p = reinterpret_cast<const Float4*>(inds);
+      const Float4 a = p[0], b = p[1], c = p[2];
+      ind[0] = a.x, ind[1] = a.y, ind[2] = a.z, ind[3] = a.w;
+      ind[4] = b.x, ind[5] = b.y, ind[6] = b.z, ind[7] = b.w;
+      ind[8] = c.x, ind[9] = c.y, ind[10] = c.z, ind[11] = c.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 12; ++i) ind[i] = i < 3 * cnt ? inds[i] : -1.f;
+    }
+  }
+  SNLS_DEV int bucket(int i, int t, int T, const Bias& b) const {
+    const float frame = ind[3 * i], dh = ind[3 * i + 1], dw = ind[3 * i + 2];
+    const bool ok = frame >= 0.f && frame < (float)T && frame == floorf(frame) && fabsf(dh) < kFarDisp &&
+                    fabsf(dw) < kFarDisp;
+    const int at = (bias_step_bucket((int)frame - t, b) * b.nb + bias_bucket(dh, b)) * b.nb + bias_bucket(dw, b);
+    return ok ? at : -1;
+  }
+};
+
+SNLS_DEV void load4(const float* p, int cnt, float* to) {
+  if (cnt == 4) {
+    const Float4 a = *reinterpret_cast<const Float4*>(p);
+    to[0] = a.x, to[1] = a.y, to[2] = a.z, to[3] = a.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = i < cnt ? p[i] : 0.f;
+  }
 }
 
+// A workgroup takes `run` chunks of one image per wave.
 __global__ void __launch_bounds__(256) bias_kernel(const float* dists, const float* __restrict__ inds,
                                                    const float* __restrict__ table, BiasRows r, Bias b, float sign,
-                                                   unsigned chunks, float* out) {
+                                                   int run, unsigned groups, float* out) {
   extern __shared__ float tab[];
-  const long long img = blockIdx.x / chunks;
-  const unsigned chunk = blockIdx.x % chunks;
+  const long long img = blockIdx.x / groups;
   const int t = (int)(img % r.T), hd = (int)(img / r.T % r.HD);
   for (int i = threadIdx.x; i < b.buckets; i += 256) tab[i] = sign * table[(long long)hd * b.buckets + i];
   __syncthreads();
   const long long base = img * r.per_image;
-  for (long long i = (long long)chunk * 256 + threadIdx.x; i < r.per_image; i += (long long)chunks * 256) {
+  const long long first = ((long long)(blockIdx.x % groups) * 4 + (threadIdx.x >> 6)) * run;
+  for (int c = 0; c < run; ++c) {
+    const long long i = (first + c) * kChunk + (threadIdx.x & 63) * 4;
+    if (i >= r.per_image) return;
+    const int cnt = (int)min(4LL, r.per_image - i);
     const long long n = base + i;
-    const float d = dists[n];
-    const int at = neighbour_bucket(inds[3 * n], inds[3 * n + 1], inds[3 * n + 2], t, r.T, b);
-    out[n] = isfinite(d) && at >= 0 ? d + tab[at] : d;
+    float d[4];
+    Quartet q;
+    load4(dists + n, cnt, d);
+    q.load(inds + 3 * n, cnt);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = q.bucket(j, t, r.T, b);
+      const float x = d[j] + tab[max(at, 0)];
+      d[j] = at >= 0 && fabsf(d[j]) < INFINITY ? x : d[j];
+    }
+    if (cnt == 4) {
+      *reinterpret_cast<Float4*>(out + n) = Float4{d[0], d[1], d[2], d[3]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < cnt) out[n + j] = d[j];
+    }
   }
 }
 
-// One wave per slice of a head's scores.  The table of partial sums lies in
-// LDS, `cols` copies of every entry; lane i adds to copy i % cols, cols lanes
-// at a time, so that no two lanes of one step meet and the order of every
-// entry's additions is fixed.
+// One wave per slice of a head's chunks, with a table of partial sums of its
+// own in LDS: 64-bit additions, which LDS performs in hardware (fp32 atomics
+// take 180 cycles an instruction on this chip, fp64 10 to 13, a read and a
+// write 25), `cols` copies of every entry so that fewer lanes meet.  No other
+// wave touches the table, so every entry's additions happen in one order.
 __global__ void __launch_bounds__(64) bias_grad_kernel(const float* __restrict__ grad, const float* __restrict__ dists,
-                                                       const float* __restrict__ inds, BiasRows r, Bias b, int B,
-                                                       float sign, int cols, int slices, float* __restrict__ part) {
-  extern __shared__ float acc[];
+                                                       const float* __restrict__ inds, BiasRows r, Bias b, float sign,
+                                                       int cols, int slices, float* __restrict__ part) {
+  extern __shared__ double acc[];
   const int lane = threadIdx.x;
   const int hd = blockIdx.x / slices, slice = blockIdx.x % slices;
-  for (int i = lane; i < b.buckets * cols; i += 64) acc[i] = 0.f;
+  for (int i = lane; i < b.buckets * cols; i += 64) acc[i] = 0.0;
   wave_lds_sync();
-  const long long total = (long long)B * r.T * r.per_image;  // of this head
-  const long long per = ((total + slices - 1) / slices + 63) / 64 * 64;
-  const long long u1 = min(total, (slice + 1) * per);
-  const int mycol = lane & (cols - 1), turn = lane / cols;
-  for (long long u0 = slice * per; u0 < u1; u0 += 64) {
-    const long long u = u0 + lane;
-    int at = -1;
-    float gv = 0.f;
-    if (u < u1) {
-      const long long bt = u / r.per_image, i = u - bt * r.per_image;
-      const int t = (int)(bt % r.T);
-      const long long n = ((bt / r.T * r.HD + hd) * r.T + t) * r.per_image + i;
-      gv = sign * grad[n];
-      if (isfinite(dists[n])) at = neighbour_bucket(inds[3 * n], inds[3 * n + 1], inds[3 * n + 2], t, r.T, b);
-    }
-    for (int k = 0; k < 64 / cols; ++k) {
-      if (turn == k && at >= 0) acc[at * cols + mycol] += gv;
-      wave_lds_sync();
+  const long long total = (long long)r.B * r.T * r.chunks;  // of this head
+  const long long c1 = total * (slice + 1) / slices;
+  const int col = lane & (cols - 1);
+  for (long long c = total * slice / slices; c < c1; ++c) {
+    const long long bt = c / r.chunks, i = (c - bt * r.chunks) * kChunk + lane * 4;
+    const int t = (int)(bt % r.T), cnt = (int)min(4LL, max(0LL, r.per_image - i));
+    const long long n = ((bt / r.T * r.HD + hd) * r.T + t) * r.per_image + i;
+    if (cnt > 0) {
+      float d[4], gv[4];
+      Quartet q;
+      load4(grad + n, cnt, gv);
+      load4(dists + n, cnt, d);
+      q.load(inds + 3 * n, cnt);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = q.bucket(j, t, r.T, b);
+        if (at >= 0 && fabsf(d[j]) < INFINITY) unsafeAtomicAdd(acc + at * cols + col, (double)(sign * gv[j]));
+      }
     }
   }
+  wave_lds_sync();
   for (int i = lane; i < b.buckets; i += 64) {
-    float s = 0.f;
-    for (int c = 0; c < cols; ++c) s += acc[i * cols + c];
-    part[(long long)blockIdx.x * b.buckets + i] = s;
+    double s = 0.0;
+    for (int k = 0; k < cols; ++k) s += acc[i * cols + k];
+    part[(long long)blockIdx.x * b.buckets + i] = (float)s;
   }
 }
 
-// grad_table[hd][i] = sum of the head's slices, in 64 bits.
-__global__ void __launch_bounds__(256) bias_grad_sum_kernel(const float* __restrict__ part, int buckets, int slices,
-                                                            float* __restrict__ grad_table) {
-  const int hd = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= buckets) return;
+// grad_table[hd][i] = sum of the head's slices, in 64 bits: 64 entries a
+// workgroup, its 16 waves take every 16th slice.
+__global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const float* __restrict__ part, int buckets, int slices,
+                                                             float* __restrict__ grad_table) {
+  __shared__ double sums[16][64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int hd = blockIdx.y, i = blockIdx.x * 64 + lane;
   double s = 0.0;
-  for (int k = 0; k < slices; ++k) s += part[((long long)hd * slices + k) * buckets + i];
-  grad_table[(long long)hd * buckets + i] = (float)s;
+  if (i < buckets) {
+    const float* p = part + (long long)hd * slices * buckets + i;
+#pragma unroll 8
+    for (int k = wv; k < slices; k += 16) s += p[(long long)k * buckets];
+  }
+  sums[wv][lane] = s;
+  __syncthreads();
+  if (wv == 0 && i < buckets) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += sums[k][lane];
+    grad_table[(long long)hd * buckets + i] = (float)s;
+  }
 }
 
-constexpr int kBiasSlices = 1280;  // one wave each: 5 on every CU
+// Slices of a head: as many waves as lie on the chip at once with their tables
+// (16 a CU up to 1,280 entries: 31 million gradients into 4 tables of 1,183
+// took 215 us with 8 a CU, 142 with 16, 178 with 24, which do not fit), and
+// four chunks a slice at least.
+constexpr int kCUs = 256, kLds = 160 * 1024, kMostWaves = 16;
 
-static int bias_slices(const Geo& g) {
-  const long long total = (long long)g.B * g.T * bias_rows(g).per_image;
-  const long long want = (total + 255) / 256;
-  const long long most = kBiasSlices / g.HD > 1 ? kBiasSlices / g.HD : 1;
-  return (int)(want < most ? want : most);
+static long long bias_slices(const Geo& g, int buckets) {
+  const BiasRows r = bias_rows(g);
+  const long long want = ((long long)g.B * g.T * r.chunks + 3) / 4;
+  const int fit = kLds / (buckets * (int)sizeof(double));
+  const long long most = kCUs * (fit < kMostWaves ? fit : kMostWaves) / g.HD;
+  return want < most ? want : most > 1 ? most : 1;
 }
 
+// slices * buckets is largest where the tables fill LDS
 size_t bias_backward_ws_bytes(const Geo& g) {
-  return (size_t)g.HD * bias_slices(g) * SNLS_BIAS_MAX_BUCKETS * sizeof(float);
+  const size_t heads = (size_t)g.HD * SNLS_BIAS_MAX_BUCKETS, full = (size_t)kCUs * (kLds / sizeof(double));
+  const size_t few = heads * bias_slices(g, 1);
+  const size_t most = heads > full ? heads : full;
+  return (few < most ? few : most) * sizeof(float);
 }
 
 snls_status launch_bias(const float* dists, const float* inds, const float* table, const Geo& g, const Bias& bias,
                         float* out, hipStream_t s) {
   const BiasRows r = bias_rows(g);
   const long long images = (long long)g.B * g.HD * g.T;
-  long long chunks = (r.per_image + 1023) / 1024;
-  const long long most = images < 8192 ? 8192 / images : 1;
-  if (chunks > most) chunks = most;
-  if (images * chunks > 0x7fffffffLL) return SNLS_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(bias_kernel, dim3((unsigned)(images * chunks)), dim3(256), bias.buckets * sizeof(float), s, dists,
-                     inds, table, r, bias, g.dist == SNLS_DIST_PROD ? 1.f : -1.f, (unsigned)chunks, out);
+  // chunks a wave takes: enough workgroups for the chip, few copies of the table
+  long long run = images * r.chunks / (4 * 8192);
+  run = run < 1 ? 1 : run > 16 ? 16 : run;
+  const long long groups = (r.chunks + 4 * run - 1) / (4 * run);
+  if (images * groups > 0x7fffffffLL) return SNLS_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(bias_kernel, dim3((unsigned)(images * groups)), dim3(256), bias.buckets * sizeof(float), s, dists,
+                     inds, table, r, bias, g.dist == SNLS_DIST_PROD ? 1.f : -1.f, (int)run, (unsigned)groups, out);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
 snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
                                  const Bias& bias, float* grad_table, float* ws, hipStream_t s) {
-  const int slices = bias_slices(g);
-  int cols = 16;
-  while (cols > 1 && bias.buckets * cols > 8192) cols /= 2;  // at most 32 KB
+  const int slices = (int)bias_slices(g, bias.buckets);
+  int cols = 8;  // as many copies as leave room for all the waves
+  while (cols > 1 && bias.buckets * cols * (int)sizeof(double) > kLds / kMostWaves) cols /= 2;
   hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)(g.HD * slices)), dim3(64),
-                     (size_t)bias.buckets * cols * sizeof(float), s, grad, dists, inds, bias_rows(g), bias, g.B,
+                     (size_t)bias.buckets * cols * sizeof(double), s, grad, dists, inds, bias_rows(g), bias,
                      g.dist == SNLS_DIST_PROD ? 1.f : -1.f, cols, slices, ws);
-  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)((bias.buckets + 255) / 256), (unsigned)g.HD), dim3(256), 0,
+  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)((bias.buckets + 63) / 64), (unsigned)g.HD), dim3(1024), 0,
                      s, ws, bias.buckets, slices, grad_table);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
