@@ -41,9 +41,11 @@ SNLS_DEV unsigned encode4(float a, float b, float c, float d, float inv) {
 }
 
 // One workgroup = 256 pixels of one (video, head): a 16 x 16 block, or four
-// 8 x 8 blocks side by side; one thread per pixel, its channels 16 at a time
-// (read twice: for the largest magnitude, then for the codes).  blockIdx.y = 0
+// 8 x 8 blocks side by side; one thread per pixel.  Up to NV * 16 channels stay
+// in registers between the largest magnitude and the codes; NV = 0: heads of
+// more channels are read twice (the second time from L2).  blockIdx.y = 0
 // stores keys, 1 values.
+template <int NV>
 __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restrict__ k, const float* __restrict__ v,
                                                           const int32_t* __restrict__ slots, CacheGeo c,
                                                           uint8_t* __restrict__ kc, float* __restrict__ ks,
@@ -55,39 +57,58 @@ __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restric
   const int b = bh / c.HD, hd = bh % c.HD;
   const int slot = slots[b];
   if (slot < 0 || slot >= c.S) return;  // the whole workgroup
-  const float* src = (blockIdx.y ? v : k) + ((long long)b * c.C + (long long)hd * c.Ch) * c.H * c.W;
+  const long long HW = (long long)c.H * c.W;
+  const float* src = (blockIdx.y ? v : k) + ((long long)b * c.C + (long long)hd * c.Ch) * HW;
   const long long img = ((long long)b * c.S + slot) * c.HD + hd;
-  uint8_t* codes = (blockIdx.y ? vc : kc) + img * c.H * c.W * c.Cp;
+  uint8_t* codes = (blockIdx.y ? vc : kc) + img * HW * c.Cp;
   float* scales = (blockIdx.y ? vs : ks) + img * c.nby * c.nbx;
   const int tw = c.sh == 3 ? 32 : 16, th = 256 / tw;
   const int ly = threadIdx.x / tw, lx = threadIdx.x % tw;
   const int y = tile / tiles_x * th + ly, x = tile % tiles_x * tw + lx;
-  const int sub = lx >> c.sh;  // block of this pixel within the workgroup
   const bool in = y < c.H && x < c.W;
   if (threadIdx.x < 4) top[threadIdx.x] = 0u;
   __syncthreads();
-  const long long HW = (long long)c.H * c.W;
   const float* px = src + (in ? (long long)y * c.W + x : 0);
+  float val[NV ? NV * 16 : 1];
   float amax = 0.f;
-  if (in)
-    for (int ch = 0; ch < c.Ch; ++ch) {
-      const float m = fabsf(px[ch * HW]);
-      if (m < INFINITY) amax = fmaxf(amax, m);
-    }
-  atomicMax(&top[sub], __float_as_uint(amax));  // magnitudes order like their bits
+  auto grow = [&](float t) {
+    const float m = fabsf(t);
+    amax = m < INFINITY ? fmaxf(amax, m) : amax;
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int ch = 0; ch < NV * 16; ++ch) val[ch] = in && ch < c.Ch ? px[ch * HW] : 0.f;
+#pragma unroll
+    for (int ch = 0; ch < NV * 16; ++ch) grow(val[ch]);
+  } else if (in) {
+#pragma unroll 16
+    for (int ch = 0; ch < c.Ch; ++ch) grow(px[ch * HW]);
+  }
+  // over the block's row in this wave, then over the workgroup (magnitudes order like their bits)
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+  if ((lx & 7) == 0) atomicMax(&top[lx >> c.sh], __float_as_uint(amax));
   __syncthreads();
-  const float scale = block_scale(__uint_as_float(top[sub]));
+  const float scale = block_scale(__uint_as_float(top[lx >> c.sh]));
   if (!in) return;
   const float inv = 1.f / scale;  // exact; at most 2^126
-  if ((ly & ((1 << c.sh) - 1)) == 0 && (lx & ((1 << c.sh) - 1)) == 0)
-    scales[(y >> c.sh) * c.nbx + (x >> c.sh)] = scale;
+  const int mask = (1 << c.sh) - 1;
+  if ((ly & mask) == 0 && (lx & mask) == 0) scales[(y >> c.sh) * c.nbx + (x >> c.sh)] = scale;
   uint4* dst = reinterpret_cast<uint4*>(codes + ((long long)y * c.W + x) * c.Cp);
-  for (int j = 0; j < c.nv; ++j) {
-    float f[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = j * 16 + i < c.Ch ? px[(j * 16 + i) * HW] : 0.f;
+  auto put = [&](int j, const float* f) {
     dst[j] = make_uint4(encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv),
                         encode4(f[8], f[9], f[10], f[11], inv), encode4(f[12], f[13], f[14], f[15], inv));
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) put(j, val + 16 * j);
+  } else {
+    for (int j = 0; j < c.nv; ++j) {
+      float f[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = j * 16 + i < c.Ch ? px[(j * 16 + i) * HW] : 0.f;
+      put(j, f);
+    }
   }
 }
 
@@ -96,8 +117,18 @@ snls_status launch_cache_store(const float* k, const float* v, const int32_t* sl
   const int tw = c.sh == 3 ? 32 : 16, th = 256 / tw;
   const int tx = (c.W + tw - 1) / tw, ty = (c.H + th - 1) / th;
   // (fewer workgroups than pixels and heads, which fit 31 bits)
-  hipLaunchKernelGGL(cache_store_kernel, dim3((unsigned)(c.B * c.HD * tx * ty), 2), dim3(256), 0, s, k, v, slots, c,
-                     k_codes, k_scales, v_codes, v_scales, tx, ty);
+  const dim3 grid((unsigned)(c.B * c.HD * tx * ty), 2);
+#define SNLS_STORE(NV)                                                                                        \
+  hipLaunchKernelGGL(cache_store_kernel<NV>, grid, dim3(256), 0, s, k, v, slots, c, k_codes, k_scales, v_codes, \
+                     v_scales, tx, ty)
+  switch (c.nv) {
+    case 1: SNLS_STORE(1); break;
+    case 2: SNLS_STORE(2); break;
+    case 3: SNLS_STORE(3); break;
+    case 4: SNLS_STORE(4); break;
+    default: SNLS_STORE(0); break;
+  }
+#undef SNLS_STORE
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
