@@ -69,6 +69,22 @@ SNLS_DEV float wave_sum_dpp(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// Sum over groups of LW lanes (16, 32 or 64), in the last lane of each.
+template <int LW>
+SNLS_DEV float group_sum_dpp(float v) {
+  static_assert(LW == 16 || LW == 32 || LW == 64, "lanes per group");
+#define SNLS_DPP_ADD(CTRL, MASK) \
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, MASK, 0xf, false))
+  SNLS_DPP_ADD(0x111, 0xf);
+  SNLS_DPP_ADD(0x112, 0xf);
+  SNLS_DPP_ADD(0x114, 0xf);
+  SNLS_DPP_ADD(0x118, 0xf);
+  if constexpr (LW >= 32) SNLS_DPP_ADD(0x142, 0xa);
+  if constexpr (LW == 64) SNLS_DPP_ADD(0x143, 0xc);
+#undef SNLS_DPP_ADD
+  return v;
+}
+
 SNLS_DEV float wave_max(float v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
@@ -400,7 +416,12 @@ SNLS_DEV long long bwd_row() {
 // the flow gradients, dQ (summed over all k neighbours of the row and added
 // once per patch pixel) -- and store the pair scalars w_l and dd_l; the dK and
 // dV terms on the key blocks are summed per key tile further below.
-template <int P>
+//
+// A head of at most 32 or 16 channels takes LW = 32 or 16 lanes: the wave's
+// 64 / LW groups of lanes go through the row's neighbours side by side (one
+// lane per channel and wave left 48 of 64 lanes idle at 16 channels), and dQ is
+// summed over the groups at the end.
+template <int P, int LW>
 __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __restrict__ vcl,
                                                                  const float* __restrict__ dists,
                                                                  const float* __restrict__ inds,
@@ -408,7 +429,9 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
                                                                  float scale, float* __restrict__ grad_flows,
                                                                  float* __restrict__ Gws, float* __restrict__ wl_out) {
   constexpr int PB = P + 1;
-  const int lane = threadIdx.x & 63;
+  constexpr int NG = 64 / LW;
+  const int lane = threadIdx.x & 63, cl = lane % LW;  // channel of the head
+  const bool last = cl == LW - 1;                      // the lane with the group's sums
   const long long row = bwd_row();
   if (row >= g.rows) return;  // whole wave
   const RowPos rp = row_pos(row, g);
@@ -417,8 +440,8 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
   const float sscale = (g.dist == SNLS_DIST_PROD ? 1.f : -1.f) * scale;
   float m, z;
   softmax_stats(drow, g.k, sscale, lane, &m, &z);
-  const bool act = lane < g.Ch;
-  const unsigned ch4 = act ? (unsigned)(rp.hd * g.Ch + lane) * 4u : kOOB2;
+  const bool act = cl < g.Ch;
+  const unsigned ch4 = act ? (unsigned)(rp.hd * g.Ch + cl) * 4u : kOOB2;
   const int lo = -(P / 2);
   const ClView gv_ = cl_view(gs, g), vv = cl_view(vcl, g);
   // g~ = grad_out / count of the patch pixels (gs holds it; 0 outside the frame)
@@ -436,18 +459,17 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
 #pragma unroll
       for (int pw = 0; pw < P; ++pw) gg[ph * P + pw] = gv_.ld(ro[ph] + co[pw] + ch4);
   }
-  for (int l = 0; l < g.k; ++l) {
-    int t2, ny, nx;
-    float ay, ax;
-    if (!isfinite(drow[l]) || !(z > 0.f) || !neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax)) {
-      if (lane == 0) {
-        Gws[row * g.k + l] = 0.f;
-        wl_out[row * g.k + l] = 0.f;
-      }
-      continue;
+  for (int l0 = 0; l0 < g.k; l0 += NG) {
+    const int l = NG == 1 ? l0 : l0 + lane / LW;
+    int t2 = 0, ny = 0, nx = 0;
+    float ay = 0.f, ax = 0.f;
+    const bool ok = l < g.k && isfinite(drow[l]) && z > 0.f && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
+    if (!ok && last && l < g.k) {
+      Gws[row * g.k + l] = 0.f;
+      wl_out[row * g.k + l] = 0.f;
     }
-    const float wl = expf(sscale * drow[l] - m) / z;
-    if (lane == 0) wl_out[row * g.k + l] = wl;
+    if (NG == 1 ? !ok : !__any(ok)) continue;
+    const float wl = ok ? expf(sscale * drow[l] - m) / z : 0.f;
     const int Y0 = rp.h + lo + ny, X0 = rp.w + lo + nx;  // block origin
     // the block of V values (0 outside the frame)
     float vb[PB * PB];
@@ -456,7 +478,7 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
         const int Y = Y0 + i, X = X0 + i;
-        kr[i] = Y >= 0 && Y < g.H ? (unsigned)((rp.b * g.T + t2) * g.H + Y) * vv.rowb : kOOB;
+        kr[i] = ok && Y >= 0 && Y < g.H ? (unsigned)((rp.b * g.T + t2) * g.H + Y) * vv.rowb : kOOB;
         kc[i] = X >= 0 && X < g.W ? (unsigned)X * vv.colb : kOOB;
       }
 #pragma unroll
@@ -483,18 +505,19 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
         fh = fmaf(gv, (1.f - ax) * (v10 - v00) + ax * (v11 - v01), fh);
         fw = fmaf(gv, (1.f - ay) * (v01 - v00) + ay * (v11 - v10), fw);
       }
-    Gl = wave_sum_dpp(Gl);
-    fh = wave_sum_dpp(fh);
-    fw = wave_sum_dpp(fw);
-    if (lane == 0) {
+    Gl = group_sum_dpp<LW>(Gl);
+    fh = group_sum_dpp<LW>(fh);
+    fw = group_sum_dpp<LW>(fw);
+    if (last && ok) {
       Gws[row * g.k + l] = Gl;
+      wl_out[row * g.k + l] = wl;
       add_flow_grad(grad_flows, g, rp, t2, wl * fh, wl * fw);
     }
   }
 }
 
 // IP: inner product (else squared L2).
-template <int P, bool IP>
+template <int P, bool IP, int LW>
 __global__ void __launch_bounds__(256) backward_search_block_kernel(const float* __restrict__ qcl,
                                                                     const float* __restrict__ kcl,
                                                                     const float* __restrict__ dists,
@@ -505,7 +528,9 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
                                                                     float* __restrict__ grad_flows,
                                                                     float* __restrict__ dd_out) {
   constexpr int PB = P + 1;
-  const int lane = threadIdx.x & 63;
+  constexpr int NG = 64 / LW;
+  const int lane = threadIdx.x & 63, cl = lane % LW;
+  const bool last = cl == LW - 1;
   const long long row = bwd_row();
   if (row >= g.rows) return;  // whole wave
   const RowPos rp = row_pos(row, g);
@@ -522,8 +547,8 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
       if (isfinite(drow[l])) wg += expf(sscale * drow[l] - m) / z * Grow[l];
   wg = wave_sum(wg);
   const long long qbase = ((long long)rp.b * g.T + rp.t) * g.HW;
-  const bool act = lane < g.Ch;
-  const int cc = rp.hd * g.Ch + (act ? lane : 0);  // a channel of the head for every lane
+  const bool act = cl < g.Ch;
+  const int cc = rp.hd * g.Ch + (act ? cl : 0);  // a channel of the head for every lane
   const unsigned ch4 = act ? (unsigned)cc * 4u : kOOB2;
   const int lo = -(P / 2);
   const ClView qv_ = cl_view(qcl, g), kv_ = cl_view(kcl, g);
@@ -545,17 +570,18 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
         dq[ph * P + pw] = 0.f;
       }
   }
-  for (int l = 0; l < g.k; ++l) {
-    int t2, ny, nx;
-    float ay, ax;
-    const bool ok = isfinite(drow[l]) && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
+  for (int l0 = 0; l0 < g.k; l0 += NG) {
+    const int l = NG == 1 ? l0 : l0 + lane / LW;
+    int t2 = 0, ny = 0, nx = 0;
+    float ay = 0.f, ax = 0.f;
+    const bool ok = l < g.k && isfinite(drow[l]) && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
     float dd = 0.f;
     if (ok) {
       if (z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
       if (grad_dists) dd += grad_dists[row * g.k + l];
     }
-    if (lane == 0) dd_out[row * g.k + l] = dd;
-    if (!ok || dd == 0.f) continue;
+    if (last && l < g.k) dd_out[row * g.k + l] = dd;
+    if (NG == 1 ? dd == 0.f : !__any(dd != 0.f)) continue;  // (dd is 0 where not ok)
     const int Y0 = rp.h + lo + ny, X0 = rp.w + lo + nx;
     float kb[PB * PB];
     {
@@ -563,7 +589,7 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
         const int Y = Y0 + i, X = X0 + i;
-        kr[i] = Y >= 0 && Y < g.H ? (unsigned)((rp.b * g.T + t2) * g.H + Y) * kv_.rowb : kOOB;
+        kr[i] = dd != 0.f && Y >= 0 && Y < g.H ? (unsigned)((rp.b * g.T + t2) * g.H + Y) * kv_.rowb : kOOB;
         kc[i] = X >= 0 && X < g.W ? (unsigned)X * kv_.colb : kOOB;
       }
 #pragma unroll
@@ -608,16 +634,18 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
         }
       }
     }
-    fh = wave_sum_dpp(fh);
-    fw = wave_sum_dpp(fw);
-    if (lane == 0) add_flow_grad(grad_flows, g, rp, t2, fh, fw);
+    fh = group_sum_dpp<LW>(fh);
+    fw = group_sum_dpp<LW>(fw);
+    if (last && dd != 0.f) add_flow_grad(grad_flows, g, rp, t2, fh, fw);
   }
 #pragma unroll
   for (int ph = 0; ph < P; ++ph)
 #pragma unroll
     for (int pw = 0; pw < P; ++pw) {
       const int y = rp.h + lo + ph, x = rp.w + lo + pw;
-      if (act && y >= 0 && y < g.H && x >= 0 && x < g.W && dq[ph * P + pw] != 0.f)
+#pragma unroll
+      for (int o = LW; o < 64; o <<= 1) dq[ph * P + pw] += __shfl_xor(dq[ph * P + pw], o);
+      if (act && lane < LW && y >= 0 && y < g.H && x >= 0 && x < g.W && dq[ph * P + pw] != 0.f)
         atomicAdd(dqcl + (qbase + (long long)y * g.W + x) * g.C + cc, dq[ph * P + pw]);
     }
 }
@@ -650,24 +678,24 @@ struct alignas(32) PairRec {
 constexpr unsigned kNoBin = 0xffffffffu;
 
 // Adds, for every lane with `has`, one to cnt[key] -- one atomic per distinct
-// key of the wave -- and returns the lane's slot: the counter's previous value
-// plus the number of lower lanes with the same key.
+// key of the wave, all of them in one instruction -- and returns the lane's
+// slot: the counter's previous value plus the number of lower lanes with the
+// same key.
 SNLS_DEV unsigned wave_count_add(unsigned* cnt, bool has, unsigned key) {
   const int lane = (int)__lane_id();
   unsigned long long pend = __ballot(has);
-  unsigned slot = 0;
+  unsigned long long same = 0;  // lanes with this lane's key
   while (pend) {
-    const int leader = (int)__builtin_ctzll(pend);
-    const unsigned lk = (unsigned)__builtin_amdgcn_readlane((int)key, leader);
-    const bool mine = ((pend >> lane) & 1ull) && key == lk;
-    const unsigned long long same = __ballot(mine);
-    unsigned base = 0;
-    if (lane == leader) base = atomicAdd(cnt + lk, (unsigned)__popcll(same));
-    base = (unsigned)__builtin_amdgcn_readlane((int)base, leader);
-    if (mine) slot = base + (unsigned)lanes_below(same);
-    pend &= ~same;
+    const unsigned lk = (unsigned)__builtin_amdgcn_readlane((int)key, (int)__builtin_ctzll(pend));
+    const unsigned long long eq = __ballot(((pend >> lane) & 1ull) && key == lk);
+    if ((eq >> lane) & 1ull) same = eq;
+    pend &= ~eq;
   }
-  return slot;
+  const int leader = same ? (int)__builtin_ctzll(same) : lane;
+  unsigned base = 0;
+  if (has && lane == leader) base = atomicAdd(cnt + key, (unsigned)__popcll(same));
+  base = __shfl(base, leader);
+  return base + (unsigned)lanes_below(same);
 }
 
 // Per pair (one thread each, pair indices below 2^29): decode the row and the
@@ -774,8 +802,10 @@ __global__ void __launch_bounds__(bin::SORT_THREADS) bin_fill_kernel(const unsig
 // whose offset is pushed past the buffer (reads 0) for pixels outside the
 // frame.  The region goes to scratch (all of it, every tile: the merge reads
 // no stale value).  gs is grad_out already divided by the cover count of its
-// pixel.
-template <int P, bool L2K>
+// pixel.  Heads of at most LW = 32 or 16 channels: every group of LW lanes
+// takes entries of its own into its own copy of the region, and the copies are
+// summed as the region is written.
+template <int P, bool L2K, int LW>
 __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restrict__ qcl,
                                                             const float* __restrict__ kcl,
                                                             const float* __restrict__ gs,
@@ -789,7 +819,8 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
   constexpr int lo = -(P / 2);
   constexpr int RH = TH + P, RW = TW + P, RPIX = RH * RW;
   __shared__ float acc[RPIX * 64];
-  const int lane = threadIdx.x;
+  constexpr int NG = 64 / LW;
+  const int lane = threadIdx.x, cl = lane % LW;
   const int term = (int)blockIdx.y + term0;
   const bool is_v = term == 1;
   const int nbins = (int)gridDim.x;
@@ -798,7 +829,7 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
   const int f = bn / (ntx * nty);
   const int t2 = f % g.T, hd = (f / g.T) % g.HD, b = f / (g.T * g.HD);
   const int ry0 = ty * TH - P, rx0 = tx * TW - P;  // region origin
-  const int ch = hd * g.Ch + (lane < g.Ch ? lane : 0);  // a channel of the head for every lane
+  const int ch = hd * g.Ch + (cl < g.Ch ? cl : 0);  // a channel of the head for every lane
   const unsigned ch4 = (unsigned)ch * 4u;
   constexpr bool l2k = L2K;  // the dK pass of the L2 distance (reads the key block too)
   const int H = g.H, W = g.W;
@@ -845,11 +876,13 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
     en.sc = s;
     return en;
   };
-  // entry i of the batch, from lane i
+  // entry i of the batch, from lane i (the same for the lanes of a group)
   auto get = [&](const Ent& v, int i) {
     Ent en;
-    auto rd = [&](unsigned x) { return (unsigned)__builtin_amdgcn_readlane((int)x, i); };
-    auto rdf = [&](float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i)); };
+    auto rd = [&](unsigned x) {
+      return NG == 1 ? (unsigned)__builtin_amdgcn_readlane((int)x, i) : (unsigned)__shfl((int)x, i);
+    };
+    auto rdf = [&](float x) { return __uint_as_float(rd(__float_as_uint(x))); };
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       en.ro[j] = rd(v.ro[j]);
@@ -937,7 +970,7 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
     auto fetch = [&](int step, Ent (&e)[2], float (&t)[2][P * P], float (&kk)[2][PB * PB]) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int idx = 2 * step + u;
+        const int idx = NG == 1 ? 2 * step + u : (2 * step + u) * NG + lane / LW;
         e[u] = get(vb, idx & 63);
         if (idx >= n) e[u].sc = 0.f;
         if (e[u].sc != 0.f) load(e[u], t[u], kk[u]);
@@ -945,7 +978,7 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
     };
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) fetch(d, es[d], ts[d], ks[d]);
-    for (int st = 0; 2 * st < n; st += D) {
+    for (int st = 0; 2 * st * NG < n; st += D) {
 #pragma unroll
       for (int d = 0; d < D; ++d) {
         const int nd = (d + D - 1) % D;
@@ -958,21 +991,28 @@ __global__ void __launch_bounds__(64) bin_accumulate_kernel(const float* __restr
   }
   float* dst = scratch + ((long long)term * nbins + bn) * (RPIX * 64) + lane;
 #pragma unroll
-  for (int px = 0; px < RPIX; ++px) dst[px * 64] = acc[px * 64 + lane];
+  for (int px = 0; px < RPIX; ++px) {
+    float v = acc[px * 64 + lane];
+#pragma unroll
+    for (int o = LW; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    dst[px * 64] = v;
+  }
 }
 
 // Key pixel (Y, X) of frame (b, hd, t2) sums the copies of the regions of
 // tiles ty in [Y / TH, (Y + P) / TH], tx in [X / TW, (X + P) / TW] (those
-// that exist), in that order, into the channels-last accumulator.  One wave
-// per pixel, lanes over the head's channels; blockIdx.y + term0 picks dK / dV.
+// that exist), in that order, into the channels-last accumulator.  LW lanes
+// per pixel, over the head's channels; blockIdx.y + term0 picks dK / dV.
+template <int LW>
 __global__ void __launch_bounds__(256) bin_merge_kernel(const float* __restrict__ scratch, Geo g, int nty, int ntx,
                                                         int term0, float* __restrict__ dkcl,
                                                         float* __restrict__ dvcl) {
   using namespace bin;
-  const long long pid = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const long long pid = (long long)blockIdx.x * (256 / LW) +
+                        (LW == 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : (int)threadIdx.x / LW);
   const long long npix = (long long)g.B * g.HD * g.T * g.HW;
-  if (pid >= npix) return;  // whole wave
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x % LW;
+  if (pid >= npix || lane >= g.Ch) return;
   const int term = (int)blockIdx.y + term0;
   const int P = g.ps, RH = TH + P, RW = TW + P;
   const long long nbins = (long long)g.B * g.HD * g.T * nty * ntx;
@@ -987,8 +1027,7 @@ __global__ void __launch_bounds__(256) bin_merge_kernel(const float* __restrict_
       const int px = (Y - (ty * TH - P)) * RW + (X - (tx * TW - P));
       v += scratch[((term * nbins + bn) * (RH * RW) + px) * 64 + lane];
     }
-  if (lane < g.Ch)
-    (term == 1 ? dvcl : dkcl)[(((long long)b * g.T + t2) * g.HW + (long long)Y * g.W + X) * g.C + hd * g.Ch + lane] = v;
+  (term == 1 ? dvcl : dkcl)[(((long long)b * g.T + t2) * g.HW + (long long)Y * g.W + X) * g.C + hd * g.Ch + lane] = v;
 }
 
 // grad_out (channels-last) divided in place by the number of query patches
@@ -1110,19 +1149,28 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
     const unsigned blocks = (unsigned)((g.rows + bwd::WAVES - 1) / bwd::WAVES);
     const dim3 grid(blocks), block(64 * bwd::WAVES);
     if (binned) {
+      const int lw = g.Ch <= 16 ? 16 : g.Ch <= 32 ? 32 : 64;  // lanes a neighbour or entry
       const unsigned pix = (unsigned)((g.B * g.T * g.HW + 3) / 4);
       hipLaunchKernelGGL(scale_by_cover_kernel, dim3(pix), dim3(256), 0, s, gocl, g, g.lo, g.ps);
       switch (g.ps) {
-#define SNLS_BWD_ROWS_CASE(P)                                                                                     \
-  case P:                                                                                                         \
-    hipLaunchKernelGGL(backward_agg_block_kernel<P>, grid, block, 0, s, vcl, dists, inds, gocl, g, scale,          \
-                       grad_flows, Gws, wlws);                                                                    \
-    if (g.dist == SNLS_DIST_PROD)                                                                                 \
-      hipLaunchKernelGGL((backward_search_block_kernel<P, true>), grid, block, 0, s, qcl, kcl, dists, inds,       \
-                         grad_dists, g, scale, Gws, dqcl, grad_flows, ddws);                                      \
-    else                                                                                                          \
-      hipLaunchKernelGGL((backward_search_block_kernel<P, false>), grid, block, 0, s, qcl, kcl, dists, inds,      \
-                         grad_dists, g, scale, Gws, dqcl, grad_flows, ddws);                                      \
+#define SNLS_BWD_ROWS(P, LW)                                                                                        \
+  hipLaunchKernelGGL((backward_agg_block_kernel<P, LW>), grid, block, 0, s, vcl, dists, inds, gocl, g, scale,       \
+                     grad_flows, Gws, wlws);                                                                        \
+  if (g.dist == SNLS_DIST_PROD)                                                                                     \
+    hipLaunchKernelGGL((backward_search_block_kernel<P, true, LW>), grid, block, 0, s, qcl, kcl, dists, inds,       \
+                       grad_dists, g, scale, Gws, dqcl, grad_flows, ddws);                                          \
+  else                                                                                                              \
+    hipLaunchKernelGGL((backward_search_block_kernel<P, false, LW>), grid, block, 0, s, qcl, kcl, dists, inds,      \
+                       grad_dists, g, scale, Gws, dqcl, grad_flows, ddws)
+#define SNLS_BWD_ROWS_CASE(P)  \
+  case P:                      \
+    if (lw == 16) {            \
+      SNLS_BWD_ROWS(P, 16);    \
+    } else if (lw == 32) {     \
+      SNLS_BWD_ROWS(P, 32);    \
+    } else {                   \
+      SNLS_BWD_ROWS(P, 64);    \
+    }                          \
     break;
         SNLS_BWD_ROWS_CASE(1)
         SNLS_BWD_ROWS_CASE(2)
@@ -1132,6 +1180,7 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
         SNLS_BWD_ROWS_CASE(6)
         SNLS_BWD_ROWS_CASE(7)
 #undef SNLS_BWD_ROWS_CASE
+#undef SNLS_BWD_ROWS
       }
       const unsigned sblocks = (unsigned)((pairs + bin::SORT_THREADS - 1) / bin::SORT_THREADS);
       hipLaunchKernelGGL(bin_count_kernel, dim3(sblocks), dim3(bin::SORT_THREADS), 0, s, dists, inds, ddws, g, nty,
@@ -1144,17 +1193,25 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
       const bool l2 = g.dist != SNLS_DIST_PROD;
       const dim3 agrid((unsigned)nbins, l2 ? 1 : 2), ablock(64);
       switch (g.ps) {
-#define SNLS_BWD_ACC_CASE(P)                                                                                        \
-  case P:                                                                                                           \
-    if (l2) {                                                                                                       \
-      hipLaunchKernelGGL((bin_accumulate_kernel<P, true>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws, offsets, \
-                         entries, g, nty, ntx, 0, scratch);                                                         \
-      hipLaunchKernelGGL((bin_accumulate_kernel<P, false>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws,        \
-                         offsets, entries, g, nty, ntx, 1, scratch);                                                \
-    } else {                                                                                                        \
-      hipLaunchKernelGGL((bin_accumulate_kernel<P, false>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws,        \
-                         offsets, entries, g, nty, ntx, 0, scratch);                                                \
-    }                                                                                                               \
+#define SNLS_BWD_ACC(P, LW)                                                                                         \
+  if (l2) {                                                                                                         \
+    hipLaunchKernelGGL((bin_accumulate_kernel<P, true, LW>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws,       \
+                       offsets, entries, g, nty, ntx, 0, scratch);                                                  \
+    hipLaunchKernelGGL((bin_accumulate_kernel<P, false, LW>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws,      \
+                       offsets, entries, g, nty, ntx, 1, scratch);                                                  \
+  } else {                                                                                                          \
+    hipLaunchKernelGGL((bin_accumulate_kernel<P, false, LW>), agrid, ablock, 0, s, qcl, kcl, gocl, recs, wlws,      \
+                       offsets, entries, g, nty, ntx, 0, scratch);                                                  \
+  }
+#define SNLS_BWD_ACC_CASE(P)  \
+  case P:                     \
+    if (lw == 16) {           \
+      SNLS_BWD_ACC(P, 16)     \
+    } else if (lw == 32) {    \
+      SNLS_BWD_ACC(P, 32)     \
+    } else {                  \
+      SNLS_BWD_ACC(P, 64)     \
+    }                         \
     break;
         SNLS_BWD_ACC_CASE(1)
         SNLS_BWD_ACC_CASE(2)
@@ -1164,10 +1221,16 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
         SNLS_BWD_ACC_CASE(6)
         SNLS_BWD_ACC_CASE(7)
 #undef SNLS_BWD_ACC_CASE
+#undef SNLS_BWD_ACC
       }
       const long long npix = (long long)g.B * g.HD * g.T * g.HW;
-      hipLaunchKernelGGL(bin_merge_kernel, dim3((unsigned)((npix + 3) / 4), 2), dim3(256), 0, s, scratch, g, nty, ntx,
-                         0, dkcl, dvcl);
+      const dim3 mgrid((unsigned)((npix * lw + 255) / 256), 2);
+      if (lw == 16)
+        hipLaunchKernelGGL(bin_merge_kernel<16>, mgrid, dim3(256), 0, s, scratch, g, nty, ntx, 0, dkcl, dvcl);
+      else if (lw == 32)
+        hipLaunchKernelGGL(bin_merge_kernel<32>, mgrid, dim3(256), 0, s, scratch, g, nty, ntx, 0, dkcl, dvcl);
+      else
+        hipLaunchKernelGGL(bin_merge_kernel<64>, mgrid, dim3(256), 0, s, scratch, g, nty, ntx, 0, dkcl, dvcl);
     } else {
       hipLaunchKernelGGL(backward_agg_kernel, grid, block, 0, s, vcl, dists, inds, gocl, g, scale, dvcl, grad_flows,
                          Gws);

@@ -121,6 +121,11 @@ LAYERS = [  # binned backward pass, its atomic form (wide head), squared L2, hea
     dict(T=3, C=6, H=9, W=10, ws=5, wt=1, ps=2, k=6, dist_type=1, stride0=2),
     dict(T=2, C=70, H=6, W=7, ws=3, wt=1, ps=3, k=3, dist_type=1),
     dict(B=2, T=3, C=16, H=9, W=7, HD=4, ws=5, wt=2, ps=1, k=20),
+    # the channels at which a neighbour's lanes change, numbers of neighbours that fill no group of lanes
+    dict(T=2, C=16, H=9, W=8, ws=5, wt=1, ps=3, k=7), dict(T=2, C=17, H=8, W=9, ws=5, wt=1, ps=2, k=5, dist_type=1),
+    dict(T=2, C=64, H=7, W=9, HD=2, ws=5, wt=1, ps=1, k=9, stride0=2),
+    dict(T=2, C=32, H=8, W=8, ws=3, wt=1, ps=7, k=3, dist_type=1), dict(T=2, C=33, H=8, W=8, ws=5, wt=1, ps=3, k=6),
+    dict(T=2, C=32, H=9, W=12, HD=2, ws=3, wt=1, ps=5, k=1),
 ]
 
 
