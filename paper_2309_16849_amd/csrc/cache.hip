@@ -383,6 +383,11 @@ constexpr float kSlack = 12.f;
 // 256 0.74 -> 0.70 ms, 64 channels at 480 x 854 1.53 -> 1.41 ms; above it the
 // registers would halve the waves.
 constexpr int kAhead = 12;
+// ... and up to which a row's loads stand together at all; wider heads issue
+// those of one column group (R * V) at a time (96 channels at 160 x 160 with 3
+// slots 308 -> 193 us), and above 128 channels two waves a SIMD are worth some
+// spilled registers (192 channels 440 -> 276 us).
+constexpr int kTogether = 12;
 
 // Keeps a loaded value from being read again, later, inside a branch.
 SNLS_DEV void pin(uint4& t) { asm volatile("" : "+v"(t.x), "+v"(t.y), "+v"(t.z), "+v"(t.w)); }
@@ -409,7 +414,7 @@ SNLS_DEV float table_base2(float t, float scale) {
 // and the first joins their maxima, sums and outputs through LDS: for calls
 // whose queries alone are too few waves for the chip.
 template <int CT, int R, int V, bool POINTS>
-__global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
+__global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
   constexpr int K = (CT + 3) / 4;
   extern __shared__ float lds[];  // row buckets of the four waves' queries, then the head's bias table
   const CacheGeo& c = a.c;
@@ -533,23 +538,27 @@ __global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tile
 #pragma unroll
     for (int k = 0; k < K; ++k) hprev[k] = pprev[k] = p[k] = vsk[k] = 0.f;
     int yov = 0;  // byte offset of the value row
+    constexpr bool kRow = K * R * V <= kTogether;
+    constexpr int kBuf = kRow ? K * R * V : R * V;
+    auto load_group = [&](const uint8_t* plane, int yoff, int k, uint4* to) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (4 * k + (R == 1 ? 0 : i) < CT)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            to[i * V + v] = *reinterpret_cast<const uint4*>(plane + (unsigned)(yoff + xoff[k][i] + (v ? voff[v] : 0)));
+    };
     auto load_row = [&](const uint8_t* plane, int yoff, uint4* to) {
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-          if (4 * k + (R == 1 ? 0 : i) < CT)
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-              to[(k * R + i) * V + v] = *reinterpret_cast<const uint4*>(plane + (unsigned)(yoff + xoff[k][i] + (v ? voff[v] : 0)));
+      for (int k = 0; k < K; ++k) load_group(plane, yoff, k, to + k * R * V);
     };
     for (int row = 0; row <= ws + 1; ++row) {
       const int y = y0 + row;
       const bool yin = (unsigned)y < (unsigned)c.H;
       const int yo = min(max(y, 0), c.H - 1) * rowbytes;
       const int dyb = (y >> c.sh) - yb0;
-      uint4 kb[K * R * V], vb[K * R * V];
-      if (row <= ws) load_row(kp, yo, kb);
+      uint4 kb[kBuf], vb[kBuf];
+      if (kRow && row <= ws) load_row(kp, yo, kb);
       if constexpr (K * R * V <= kAhead) load_row(vp, yov, vb);
       float sc[K + 1];
 #pragma unroll
@@ -558,13 +567,15 @@ __global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tile
       if (row <= ws) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
+          uint4* kk = kRow ? kb + k * R * V : kb;
+          if constexpr (!kRow) load_group(kp, yo, k, kk);
           float part[R];
 #pragma unroll
           for (int i = 0; i < R; ++i) {
             part[i] = 0.f;
             if (4 * k + (R == 1 ? 0 : i) < CT)
 #pragma unroll
-              for (int v = 0; v < V; ++v) part[i] = dot16(kb[(k * R + i) * V + v], q[v], part[i]);
+              for (int v = 0; v < V; ++v) part[i] = dot16(kk[i * V + v], q[v], part[i]);
           }
           float d;
           if constexpr (R == 1) {
@@ -614,15 +625,26 @@ __global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tile
         z += p[k];
       }
       if (row > 0) {  // values of the row above (its scales and validity were found with its keys)
-        if constexpr (K * R * V > kAhead) load_row(vp, yov, vb);
+        auto pin_group = [&](int k, uint4* t) {
 #pragma unroll
-        for (int n = 0; n < K * R * V; ++n)
-          if (4 * (n / (R * V)) + (R == 1 ? 0 : n / V % R) < CT) pin(vb[n]);
+          for (int n = 0; n < R * V; ++n)
+            if (4 * k + (R == 1 ? 0 : n / V) < CT) pin(t[n]);
+        };
+        if constexpr (kRow) {
+          if constexpr (K * R * V > kAhead) load_row(vp, yov, vb);
+#pragma unroll
+          for (int k = 0; k < K; ++k) pin_group(k, vb + k * R * V);
+        }
         float g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) g[k] = fmaf(ay, pprev[k] - p[k], p[k]);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
+          uint4* vk = kRow ? vb + k * R * V : vb;
+          if constexpr (!kRow) {
+            load_group(vp, yov, k, vk);
+            pin_group(k, vk);
+          }
           const float left = quad<3, 0, 1, 2>(l == 3 ? (k ? g[k ? k - 1 : 0] : 0.f) : g[k]);  // column - 1
           const float wgt = fmaf(ax, left - g[k], g[k]) * vsk[k];
 #pragma unroll
@@ -635,7 +657,7 @@ __global__ void __launch_bounds__(256) attend_quad_kernel(AttendArgs a, int tile
                                                   : quad<3, 3, 3, 3>(wgt));
             if (4 * k + (R == 1 ? 0 : i) < CT && wi != 0.f)
 #pragma unroll
-              for (int v = 0; v < V; ++v) spread16(vb[(k * R + i) * V + v], wi, acc[v]);
+              for (int v = 0; v < V; ++v) spread16(vk[i * V + v], wi, acc[v]);
           }
         }
       }
@@ -753,14 +775,23 @@ snls_status launch_cache_attend(const float* q, const int32_t* points, long long
                                 const uint8_t* v_codes, const float* v_scales, const float* table,
                                 const CacheGeo& c, const Bias& bias, int ws, float scale, float* out, hipStream_t s) {
   const AttendArgs a{q, points, n, flows, ages, k_codes, k_scales, v_codes, v_scales, table, c, bias, ws, scale, out};
-  // few points: a wave each for the shortest way through one query.  Wave / quads (6 slots, ws = 9): one head of 64
-  // channels 30 / 51 us for 1,024 points, 56 / 52 us for 2,048; 4 heads of 16 29 / 32 us for 512, 51 / 33 us for 1,024
-  if (points && n * c.HD <= 2048)
-    run_attend_wave<4>(a, s);
-  else if (points)
+  // few points: 4, 8 or 16 waves each, which share its slots, for the shortest way through one query.  4 waves / quads
+  // (6 slots, ws = 9): one head of 64 channels 30 / 51 us for 1,024 points, 56 / 52 us for 2,048; 4 heads of 16
+  // channels 29 / 32 us for 512, 51 / 33 us for 1,024.  4 / 16 waves (16 slots): 12 heads 20.0 / 17.3 us for 16
+  // points, 27 / 37 us for 64, where 4,096 waves are passed
+  const long long single = n * c.HD;
+  if (points && single <= 2048) {
+    if (c.S > 8 && single * 16 <= 4096)
+      run_attend_wave<16>(a, s);
+    else if (c.S > 4 && single * 8 <= 4096)
+      run_attend_wave<8>(a, s);
+    else
+      run_attend_wave<4>(a, s);
+  } else if (points) {
     run_attend<true>(a, s);
-  else
+  } else {
     run_attend<false>(a, s);
+  }
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 

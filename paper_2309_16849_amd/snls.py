@@ -110,13 +110,13 @@ def load_library():
     return _lib
 
 
+_PARAMS_SIZE = ctypes.sizeof(SnlsParams)
+
+
 def params_from_dict(p: dict) -> SnlsParams:
-    s = SnlsParams()
-    s.struct_size = ctypes.sizeof(SnlsParams)
-    for n in ("B", "T", "C", "H", "W", "HD", "ws", "wt", "ps", "stride0", "k", "dist_type"):
-        setattr(s, n, int(p[n]))
-    s.stride1 = float(p["stride1"])
-    return s
+    return SnlsParams(_PARAMS_SIZE, int(p["B"]), int(p["T"]), int(p["C"]), int(p["H"]), int(p["W"]), int(p["HD"]),
+                      int(p["ws"]), int(p["wt"]), int(p["ps"]), int(p["stride0"]), float(p["stride1"]), int(p["k"]),
+                      int(p["dist_type"]))
 
 
 def grid(p: dict):
@@ -128,20 +128,25 @@ def n_cand(p: dict) -> int:
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else None
+    return t.data_ptr() if t is not None else None
 
 
 def _dev(t, name, shape=None):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()):
         raise ValueError("%s must be a contiguous float32 tensor on the GPU" % name)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != tuple(shape):
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     return t
 
 
+# the current stream's handle without a Stream object around it (3 us a call)
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None and _current_raw is not None:
+        return _current_raw(torch.cuda.current_device())
+    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
 
 
 def _check(status, where):
@@ -384,16 +389,12 @@ def snls_gather_reduce(v, weights, inds, proj, p: dict, out=None, workspace=None
 
 # ------------------------------------------------------- learned position bias --
 
+_BIAS_SIZE, _Edges = ctypes.sizeof(SnlsBiasParams), ctypes.c_float * SNLS_BIAS_MAX_EDGES
+
+
 def bias_from_dict(bias: dict) -> SnlsBiasParams:
-    s = SnlsBiasParams()
-    s.struct_size = ctypes.sizeof(SnlsBiasParams)
-    s.radius = int(bias["radius"])
-    edges = bias["edges"]
-    s.n_edges = len(edges)
-    if len(edges) <= SNLS_BIAS_MAX_EDGES:  # a longer list is refused by the library
-        for i, e in enumerate(edges):
-            s.edges[i] = e
-    return s
+    edges = bias["edges"]  # (a list longer than the library takes is refused there)
+    return SnlsBiasParams(_BIAS_SIZE, int(bias["radius"]), len(edges), _Edges(*edges[:SNLS_BIAS_MAX_EDGES]))
 
 
 def bias_table_shape(bias: dict, heads: int):
@@ -405,7 +406,7 @@ def _here(*tensors):
     """Every given tensor is on the current device, where the call will run."""
     cur = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != cur:
+        if t is not None and t.get_device() != cur:
             raise ValueError("tensors are on %s, the current device is cuda:%d" % (t.device, cur))
 
 
@@ -475,12 +476,12 @@ def snls_backward_scores(q, k, v, flows, dists, inds, grad_out, p: dict, scale: 
 
 # ------------------------------------------------------- frames held in 8 bits --
 
+_CACHE_SIZE = ctypes.sizeof(SnlsCacheParams)
+
+
 def cache_from_dict(cp: dict) -> SnlsCacheParams:
-    s = SnlsCacheParams()
-    s.struct_size = ctypes.sizeof(SnlsCacheParams)
-    for n in ("B", "slots", "C", "H", "W", "HD", "block"):
-        setattr(s, n, int(cp[n]))
-    return s
+    return SnlsCacheParams(_CACHE_SIZE, int(cp["B"]), int(cp["slots"]), int(cp["C"]), int(cp["H"]), int(cp["W"]),
+                           int(cp["HD"]), int(cp["block"]))
 
 
 def cache_shapes(cp: dict):
@@ -504,7 +505,7 @@ def cache_alloc(cp: dict, device):
 def _dev_as(t, name, shape, dtypes):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.is_contiguous()):
         raise ValueError("%s must be a contiguous tensor of %s on the GPU" % (name, " or ".join(map(str, dtypes))))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     return t
 
