@@ -15,6 +15,9 @@
 namespace snls {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------------------------ store --
 
@@ -406,6 +409,32 @@ SNLS_DEV float table_base2(float t, float scale) {
   return fabsf(x) < INFINITY ? fminf(fmaxf(x * kLog2e, -3.402823466e38f), 3.402823466e38f) : x;
 }
 
+// MX: scores from the matrix cores (heads of 17 channels and more; 64 channels
+// at 480 x 854 1.45 -> 1.08 ms, two heads of 32 at 256 x 256 0.32 -> 0.27).  The
+// windows of a wave's 16 queries overlap, so the box around them in a slot's
+// frame is walked in tiles of 16 tokens, v_mfma_f32_16x16x32_f16 with tokens as
+// rows and queries as columns, and each query's own taps of the product go to
+// LDS, from where the rows of taps are read.  Codes are exact in fp16; q is
+// split in two fp16 parts that hold 22 bits of a query's largest channel
+// (scaled by a power of two per query).  A box is some four times a window
+// (offsets carry an error of pixels), the matrix cores 30 times as fast as the
+// vector units on such a product.  Where the box would be larger than the 16
+// windows are together (offsets that differ by tens of pixels between
+// neighbours), every window is a box of its own.
+template <int CT>
+constexpr int kBoxPitch = CT + 6;  // a row of taps with the three beside it that a group of four tokens may bring
+template <int CT>
+constexpr int kBoxQuery = CT * kBoxPitch<CT> + 1;  // floats of a query (odd: queries fall on different banks)
+
+// 8 codes as fp16.
+SNLS_DEV half8_t codes_f16(unsigned a, unsigned b) {
+  const half2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.f, false);
+  const half2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.f, true);
+  const half2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.f, false);
+  const half2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.f, true);
+  return half8_t{p0.x, p0.y, p1.x, p1.y, p2.x, p2.y, p3.x, p3.y};
+}
+
 // The loads of a tap row stand together, with no branch between them, so that
 // they are under way at the same time: CT columns of taps are read whatever ws
 // is (those past the window at the clamped address, unused).
@@ -413,10 +442,19 @@ SNLS_DEV float table_base2(float t, float scale) {
 // split (1, 2 or 4) waves share 16 queries, each takes every split-th slot,
 // and the first joins their maxima, sums and outputs through LDS: for calls
 // whose queries alone are too few waves for the chip.
-template <int CT, int R, int V, bool POINTS>
-__global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
+// Waves a SIMD that the registers are held to (160 x 160 to 480 x 854, ws = 9):
+// with the matrix cores 3 for heads up to 64 channels (64 channels 1.32 -> 1.08
+// ms at 480 x 854, 48 channels 151 -> 132 us at 200 x 240; 4 spill), without
+// them what the compiler takes (3 at 16 channels; 4 cost 1 to 7%).
+constexpr int attend_waves(int CT, int R, int V, bool MX) {
+  if (MX && (V == 1 || (R == 1 && CT <= 10))) return 3;
+  return V >= 3 || (MX && V >= 2) ? 2 : 1;
+}
+template <int CT, int R, int V, bool POINTS, bool MX>
+__global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
+  static_assert(!(MX && POINTS), "boxes lie around neighbouring pixels");
   constexpr int K = (CT + 3) / 4;
-  extern __shared__ float lds[];  // row buckets of the four waves' queries, then the head's bias table
+  extern __shared__ float lds[];  // row buckets of the four waves' queries, the head's bias table, the boxes' scores
   const CacheGeo& c = a.c;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int l = lane & 3, sub = lane >> 2;
@@ -424,7 +462,7 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
   const int ws = a.ws, r = ws / 2;
   const long long HW = (long long)c.H * c.W;
   // the wave's queries: 8 x 2 pixels of the workgroup's tile, or 16 listed points
-  int b, hd, h, w;
+  int b, hd, h, w, h0 = 0, w0 = 0;
   long long qi = 0;
   bool live;
   if constexpr (POINTS) {
@@ -446,8 +484,10 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
     b = img / c.HD;
     hd = img % c.HD;
     const int strip = tile / (8 * tiles_y), rest = tile % (8 * tiles_y), width = min(8, tiles_x - strip * 8);
-    h = (rest / width * groups + group) * 2 + (sub >> 3);
-    w = (strip * 8 + rest % width) * 8 + (sub & 7);
+    h0 = (rest / width * groups + group) * 2;
+    w0 = (strip * 8 + rest % width) * 8;
+    h = h0 + (sub >> 3);
+    w = w0 + (sub & 7);
     live = h < c.H && w < c.W;
   }
   const bool stored = live;  // has a row of out
@@ -462,7 +502,7 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
     tab[i] = a.table ? table_base2(a.table[(long long)hd * a.bias.buckets + i], a.scale) : 0.f;
   __syncthreads();
   const int lr = l & (R - 1);  // this lane's part of a token
-  float q[V][16], acc[V][16];
+  float q[MX ? 1 : V][16], acc[V][16];
   int voff[V];  // byte offset of the lane's vector v from its first
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -471,13 +511,56 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
     for (int i = 0; i < 16; ++i) {
       const int ch = (v * R + lr) * 16 + i;
       acc[v][i] = 0.f;
-      q[v][i] = 0.f;
-      if (live && ch < c.Ch)
-        q[v][i] = (a.scale * kLog2e) * (POINTS ? a.q[qi * c.C + hd * c.Ch + ch]
+      if constexpr (!MX) q[v][i] = 0.f;
+      if (!MX && live && ch < c.Ch)
+        q[MX ? 0 : v][i] = (a.scale * kLog2e) * (POINTS ? a.q[qi * c.C + hd * c.Ch + ch]
                                                : a.q[((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w]);
     }
   }
   const int lane0 = min(lr, c.nv - 1) * 16, rowbytes = c.W * c.Cp;
+  // Matrix-core operand of query lane % 16: lanes of group lane / 16 hold the
+  // channels of vector 4 j + group, its first and its second eight; with two
+  // vectors the upper groups hold the low parts of the same channels instead.
+  constexpr bool kPack = R * V == 2;
+  constexpr int J = (R * V + 3) / 4;
+  half8_t qh[MX ? J : 1][2], ql[MX && !kPack ? J : 1][2];
+  float qback = 0.f;  // undoes the query's power of two
+  const int n16 = lane & 15, g4 = lane >> 4;
+  float* const stab = tab + max(a.bias.buckets, 1) + wv * 16 * kBoxQuery<CT>;
+  if constexpr (MX) {
+    const int hn = h0 + (n16 >> 3), wn = w0 + (n16 & 7);
+    const bool inq = hn < c.H && wn < c.W;
+    const float* qp = a.q + ((long long)b * c.C + hd * c.Ch) * HW + (inq ? (long long)hn * c.W + wn : 0);
+    float x[J][16], most = 0.f;
+#pragma unroll
+    for (int jj = 0; jj < J; ++jj)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int ch = (kPack ? (g4 & 1) : 4 * jj + g4) * 16 + i;
+        x[jj][i] = inq && ch < c.Ch ? (a.scale * kLog2e) * qp[ch * HW] : 0.f;
+        const float t = fabsf(x[jj][i]);
+        most = t < INFINITY ? fmaxf(most, t) : most;
+      }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    // the largest channel to 2^14 .. 2^15, just below fp16's end: channels 2^-15 of it still have all of both parts
+    const int e = max((int)(__float_as_uint(most) >> 23) - 127, -110) - 14;
+    const float up = __uint_as_float((unsigned)(127 - e) << 23);
+    qback = __uint_as_float((unsigned)(127 + e) << 23);
+#pragma unroll
+    for (int jj = 0; jj < J; ++jj)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float t = x[jj][i] * up;
+        const _Float16 hi = (_Float16)t, lo = (_Float16)(t - (float)hi);
+        if constexpr (kPack) {
+          qh[jj][i / 8][i % 8] = g4 < 2 ? hi : lo;
+        } else {
+          qh[jj][i / 8][i % 8] = hi;
+          ql[jj][i / 8][i % 8] = lo;
+        }
+      }
+  }
   float m = -INFINITY, z = 0.f;
   for (int s = part_of; s < c.S; s += split) {
     const int age = a.ages[(long long)b * c.S + s];
@@ -501,6 +584,102 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
     const uint8_t* vp = a.vc + img * HW * c.Cp;
     const float* ksp = a.ks + img * c.nby * c.nbx;
     const float* vsp = a.vs + img * c.nby * c.nbx;
+    if constexpr (MX) {
+      int ymin = on ? y0 : INT_MAX, ymax = on ? y0 : INT_MIN, xmin = on ? x0 : INT_MAX, xmax = on ? x0 : INT_MIN;
+#pragma unroll
+      for (int o = 4; o < 64; o <<= 1) {
+        ymin = min(ymin, __shfl_xor(ymin, o));
+        ymax = max(ymax, __shfl_xor(ymax, o));
+        xmin = min(xmin, __shfl_xor(xmin, o));
+        xmax = max(xmax, __shfl_xor(xmax, o));
+      }
+      const int yq = __shfl(y0, n16 * 4), xq = __shfl(x0, n16 * 4);  // window of query n16
+      float* const sq = stab + n16 * kBoxQuery<CT>;
+      // the box of the first taps ya .. yb, xa .. xb, clipped to the frame, in groups of four tokens that share a block
+      auto walk = [&](int ya_, int yb_, int xa_, int xb_, bool test) {
+        const int ry0 = __builtin_amdgcn_readfirstlane(min(max(ya_, 0), c.H - 1));
+        const int ry1 = __builtin_amdgcn_readfirstlane(min(max(yb_ + ws, 0), c.H - 1));
+        const int rx0 = __builtin_amdgcn_readfirstlane(min(max(xa_, 0), c.W - 1)) & ~3;
+        const int rx1 = __builtin_amdgcn_readfirstlane(min(max(xb_ + ws, 0), c.W - 1));
+        const int gw = (rx1 - rx0) / 4 + 1;
+        const long long ng = (long long)(ry1 - ry0 + 1) * gw;
+        if (test && ng > 16 * (ws + 1) * ((ws + 7) / 4)) return false;
+        const int pairs = ((int)ng + 7) / 8;  // of tiles
+        const int dq = 4 / gw, dr = 4 % gw;   // groups of a tile: rows and columns on
+        const int ga = n16 >> 2;
+        int ya = ry0 + ga / gw, xa = ga % gw, yd = ry0 + g4 / gw, xd = g4 % gw;  // group of the operand, of the result
+        auto step = [&](int& y, int& x) {
+          y += dq;
+          x += dr;
+          if (x >= gw) {
+            x -= gw;
+            ++y;
+          }
+        };
+        // two tiles at a time; the next two are read while these are multiplied
+        struct Pair {
+          uint4 tok[2][J];
+          float back[2];
+          int dy[2], dx[2];
+        } pr[2];
+        auto fetch = [&](Pair& f) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const unsigned at = (unsigned)(min(ya, c.H - 1) * rowbytes) +
+                                __umul24((unsigned)min(rx0 + 4 * xa + (n16 & 3), c.W - 1), (unsigned)c.Cp);
+#pragma unroll
+            for (int jj = 0; jj < J; ++jj)
+              f.tok[u][jj] = *reinterpret_cast<const uint4*>(
+                  kp + (at + (unsigned)(min(kPack ? (g4 & 1) : 4 * jj + g4, c.nv - 1) * 16)));
+            f.back[u] = ksp[(unsigned)((min(yd, c.H - 1) >> c.sh) * c.nbx + ((rx0 + 4 * xd) >> c.sh))];
+            f.dy[u] = yd - yq;
+            f.dx[u] = rx0 + 4 * xd - xq + 3;
+            step(ya, xa);
+            step(yd, xd);
+          }
+        };
+        fetch(pr[0]);
+        for (int t = 0; t < pairs; t += 2)
+#pragma unroll
+          for (int turn = 0; turn < 2; ++turn) {
+            if (t + turn >= pairs) break;
+            const Pair& f = pr[turn];
+            if (t + turn + 1 < pairs) fetch(pr[1 - turn]);
+            f32x4 d[2], e[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              d[u] = e[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int jj = 0; jj < J; ++jj) {
+                const uint4 w = f.tok[u][jj];
+                const half8_t k0 = codes_f16(w.x, w.y), k1 = codes_f16(w.z, w.w);
+                if constexpr (kPack) {
+                  d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[jj][0], d[u], 0, 0, 0);
+                  e[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[jj][1], e[u], 0, 0, 0);
+                } else {
+                  e[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, ql[jj][0], e[u], 0, 0, 0);
+                  d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[jj][0], d[u], 0, 0, 0);
+                  e[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, ql[jj][1], e[u], 0, 0, 0);
+                  d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[jj][1], d[u], 0, 0, 0);
+                }
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if ((unsigned)f.dy[u] <= (unsigned)ws && (unsigned)f.dx[u] < (unsigned)(ws + 4)) {
+                float* to = sq + f.dy[u] * kBoxPitch<CT> + f.dx[u];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[i] = (d[u][i] + e[u][i]) * f.back[u] * qback;
+              }
+          }
+        return true;
+      };
+      if (!walk(ymin, ymax, xmin, xmax, true))
+        for (int n = 0; n < 16; ++n) {
+          const int y1 = __shfl(y0, 4 * n), x1 = __shfl(x0, 4 * n);
+          walk(y1, y1, x1, x1, false);
+        }
+    }
     // byte offsets of the tap columns this lane reads; its own columns' scales
     // (a window meets at most three rows of blocks), validity and buckets
     int xoff[K][R];
@@ -557,14 +736,21 @@ __global__ void __launch_bounds__(256, V >= 3 ? 2 : 1) attend_quad_kernel(Attend
       const bool yin = (unsigned)y < (unsigned)c.H;
       const int yo = min(max(y, 0), c.H - 1) * rowbytes;
       const int dyb = (y >> c.sh) - yb0;
-      uint4 kb[kBuf], vb[kBuf];
-      if (kRow && row <= ws) load_row(kp, yo, kb);
-      if constexpr (K * R * V <= kAhead) load_row(vp, yov, vb);
+      uint4 kb[MX ? 1 : kBuf], vb[kBuf];
+      if constexpr (!MX && kRow)
+        if (row <= ws) load_row(kp, yo, kb);
+      if constexpr (kRow && K * R * V <= kAhead) load_row(vp, yov, vb);
       float sc[K + 1];
 #pragma unroll
       for (int k = 0; k <= K; ++k) sc[k] = 0.f;
       const int rb = rowb[min(row, 4 * K - 1)];
-      if (row <= ws) {
+      if constexpr (MX) {
+        if (row <= ws) {
+          const float* from = stab + sub * kBoxQuery<CT> + row * kBoxPitch<CT> + 3 + l;
+#pragma unroll
+          for (int k = 0; k < K; ++k) sc[k] = yin && tin[k] ? from[4 * k] : 0.f;
+        }
+      } else if (row <= ws) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
           uint4* kk = kRow ? kb + k * R * V : kb;
@@ -728,22 +914,38 @@ static void run_attend_quad(const AttendArgs& a, int split, hipStream_t s) {
   const long long blocks = POINTS ? (a.n + groups * 16 - 1) / (groups * 16) : (long long)c.B * tx * ty;
   const dim3 grid((unsigned)(POINTS ? blocks * c.HD : (blocks * c.HD + 7) / 8 * 8)), block(256);
   size_t lds = (64 * 16 + (a.table ? a.bias.buckets : 1)) * sizeof(float);
-  auto room = [&](int V) {
+  // Scores from the matrix cores, where LDS for them fits the 64 KB that a launch may ask for (ws <= 9 whatever the
+  // table).  3 slots, vector units / matrix cores: 32 channels ws = 7 69 / 78 us, ws = 9 120 / 104, ws = 11 135 / 148;
+  // 64 channels ws = 3 50 / 59, ws = 5 90 / 76, ws = 9 164 / 132, ws = 11 211 / 205; 128 channels ws = 5 154 / 153, ws
+  // = 9 305 / 259, ws = 11 394 / 318 (200 x 240); 16 channels: the tiles' other work is what the products were
+  const size_t boxes = 4 * 16 * kBoxQuery<CT> * sizeof(float);
+  const bool mx = lds + boxes <= 65536;
+  auto room = [&](int V, bool with_boxes) {
     const size_t join = split > 1 ? (size_t)groups * 64 * (2 + 16 * V) * sizeof(float) : 0;
-    return join > lds ? join : lds;
+    const size_t own = lds + (with_boxes ? boxes : 0);
+    return join > own ? join : own;
   };
 #define SNLS_QUAD(R, V) \
-  hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, POINTS>), grid, block, room(V), s, a, tx, ty, split)
+  hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, POINTS, false>), grid, block, room(V, false), s, a, tx, ty, split)
+#define SNLS_QUAD_MX(R, V)                                                                                            \
+  if constexpr (!POINTS && (R * V == 2 ? CT == 10 : CT >= 6 && CT <= 12))                                           \
+    if (mx) {                                                                                                       \
+      hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, false, true>), grid, block, room(V, true), s, a, tx, ty,     \
+                         split);                                                                                    \
+      break;                                                                                                        \
+    }                                                                                                               \
+  SNLS_QUAD(R, V)
   switch (c.nv) {
     case 1: SNLS_QUAD(1, 1); break;
-    case 2: SNLS_QUAD(2, 1); break;
-    case 3: SNLS_QUAD(1, 3); break;
-    case 4: SNLS_QUAD(4, 1); break;
-    case 6: SNLS_QUAD(2, 3); break;
-    case 5: case 7: case 8: SNLS_QUAD(4, 2); break;
+    case 2: SNLS_QUAD_MX(2, 1); break;
+    case 3: SNLS_QUAD_MX(1, 3); break;
+    case 4: SNLS_QUAD_MX(4, 1); break;
+    case 6: SNLS_QUAD_MX(2, 3); break;
+    case 5: case 7: case 8: SNLS_QUAD_MX(4, 2); break;
     case 9: case 10: case 11: case 12: SNLS_QUAD(4, 3); break;
     default: SNLS_QUAD(4, 4); break;
   }
+#undef SNLS_QUAD_MX
 #undef SNLS_QUAD
 }
 

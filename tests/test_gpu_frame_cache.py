@@ -425,3 +425,83 @@ def test_long_lists_of_points(dev, C, HD, ws, slots):
     keep = torch.ones(len(bad), dtype=torch.bool)
     keep[5::7] = keep[6::7] = False
     assert bool((got[~keep] == 0).all()) and torch.equal(got[keep], b[keep])
+
+
+def _sampled(dev, cp, ws, q, fl, ages, cache, kv, vv, scale, n, g, table=None, bias=None):
+    """The dense form and n of its pixels in 64 bits."""
+    to = lambda x: None if x is None else x.to(dev)  # noqa: E731
+    got = B.snls_cache_attend(to(q), to(fl), to(ages), cache, cp, ws, scale, table=to(table), bias=bias)
+    pts = _points(cp, n, g)
+    pts[0], pts[1] = torch.tensor([0, 0, 0]), torch.tensor([cp["B"] - 1, cp["H"] - 1, cp["W"] - 1])
+    b, h, w = (pts[:, j].long() for j in range(3))
+    qp = q[b, :, h, w].contiguous()
+    ref, big = R.attend(qp, pts, fl[b, :, :, h, w].contiguous(), ages, kv, vv, cp, ws, scale, table, bias)
+    return got.cpu().double()[b, :, h, w], ref, big, qp, got
+
+
+@pytest.mark.parametrize("C,ws,slots,block", [(32, 9, 2, 8), (48, 5, 3, 16), (64, 9, 1, 8), (64, 7, 2, 16),
+                                              (96, 11, 2, 8), (120, 9, 2, 8)], ids=str)
+@pytest.mark.parametrize("spread", [3.0, 40.0])
+def test_boxes(dev, C, ws, slots, block, spread):
+    """Offsets of neighbouring pixels that share a box of tokens (3 pixels apart) and that do not (40 pixels)."""
+    cp = _cp(B=2, C=C, HD=1, H=101, W=94, slots=slots, block=block)
+    g = torch.Generator().manual_seed(31)
+    cache, kv, vv = _filled(cp, dev)
+    bias = dict(radius=1, edges=[1.0, 4.0])
+    table = torch.randn(B.bias_table_shape(bias, 1), generator=g)
+    q = 2 * torch.randn(2, C, 101, 94, generator=g)
+    fl = spread * torch.randn(2, slots, 2, 101, 94, generator=g)
+    fl[:, :, :, 40:60] = 0.25  # narrow boxes, and wide ones beside them
+    ages = torch.zeros(2, slots, dtype=torch.int32)
+    scale = 1.0 / C ** 0.5
+    print("boxes", cp, ws, spread, flush=True)
+    got, ref, big, qp, whole = _sampled(dev, cp, ws, q, fl, ages, cache, kv, vv, scale, 40, g, table, bias)
+    assert float((got - ref).abs().max()) <= _tol(qp, kv, vv, cp, ws, scale, big, table)
+    # all pixels, against the vector units' form of the same operator
+    _, pts, qa, _, _ = _both(dev, cp, ws, q, fl, ages, cache, scale, table, bias)
+    pts = pts.view(2, 101, 94, C).permute(0, 3, 1, 2)
+    assert float((pts - whole.cpu()).abs().max()) <= 2 * _tol(qa, kv, vv, cp, ws, scale, big, table)
+
+
+def test_channels_of_very_different_size(dev):
+    """Keys whose channels are up to 2^14 apart and queries the other way round, so that all count alike.  The two fp16
+    parts of a query's channel are off by at most 2^-22 of it: with S = sum |q_c| max |k_c| per query, a logit is off by
+    at most scale * ((C + 16) u + 2^-22) S."""
+    C = 64
+    cp = _cp(C=C, HD=1, H=40, W=41, slots=2)
+    g = torch.Generator().manual_seed(41)
+    amp = torch.exp2(-14.0 * torch.arange(C) / (C - 1)).view(1, C, 1, 1)
+    cache = B.cache_alloc(cp, dev)
+    for s in range(2):
+        k, v = (torch.randn(1, C, 40, 41, generator=g) for _ in range(2))
+        B.snls_cache_store((k * amp).to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
+    kv, vv = R.decoded(cache[0], cache[1].cpu(), cp), R.decoded(cache[2], cache[3].cpu(), cp)
+    q = torch.randn(1, C, 40, 41, generator=g) / amp
+    fl = torch.randn(1, 2, 2, 40, 41, generator=g)
+    ages = torch.zeros(1, 2, dtype=torch.int32)
+    got, ref, big, qp, _ = _sampled(dev, cp, 9, q, fl, ages, cache, kv, vv, 0.125, 60, g)
+    S = float((qp.double().abs() * kv.abs().amax((0, 1, 2, 3, 4))).sum(1).max())
+    delta = 0.125 * ((C + 16) * U + 2.0 ** -22) * S
+    tol = float(vv.abs().max()) * (2 * delta + 4 * big * U + 2 * 162 * U + 32 * U)
+    print("err %.2e tol %.2e" % (float((got - ref).abs().max()), tol))
+    assert float((got - ref).abs().max()) <= tol
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-6, 1e4, 1e30])
+def test_query_sizes(dev, size):
+    """Queries far from 1 against keys far the other way; a NaN or infinite channel of one query stays with it."""
+    cp = _cp(C=64, HD=1, H=30, W=31, slots=2)
+    g = torch.Generator().manual_seed(51)
+    cache, kv, vv = _filled(cp, dev, amp=1.0 / size)
+    q = size * torch.randn(1, 64, 30, 31, generator=g)
+    fl = torch.randn(1, 2, 2, 30, 31, generator=g)
+    ages = torch.zeros(1, 2, dtype=torch.int32)
+    got, ref, big, qp, whole = _sampled(dev, cp, 9, q, fl, ages, cache, kv, vv, 0.125, 40, g)
+    assert float((got - ref).abs().max()) <= _tol(qp, kv, vv, cp, 9, 0.125, big, None)
+    bad = q.clone()
+    bad[0, 7, 10, 11], bad[0, 9, 20, 3], bad[0, :, 5, 5] = float("nan"), float("inf"), 0.0
+    out = B.snls_cache_attend(bad.to(dev), fl.to(dev), ages.to(dev), cache, cp, 9, 0.125)
+    keep = torch.ones(30, 31, dtype=torch.bool, device=dev)
+    keep[10, 11] = keep[20, 3] = keep[5, 5] = False
+    assert bool((out[0, :, 10, 11] == 0).all()) and bool((out[0, :, 20, 3] == 0).all())
+    assert torch.equal(out[:, :, keep], whole[:, :, keep]) and bool((out[0, :, 5, 5] != 0).any())
