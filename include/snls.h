@@ -344,7 +344,8 @@ typedef struct {
  *   table   device, (HD, 2*radius+1, 2E+1, 2E+1)
  *   out     device out, as dists; may be dists itself
  * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for more buckets per head
- * than SNLS_BIAS_MAX_BUCKETS or more than 2^40 scores; SNLS_ERR_HIP. */
+ * than SNLS_BIAS_MAX_BUCKETS, 2^38 scores or more, or 2^24 images (B*HD*T) or
+ * more; SNLS_ERR_HIP. */
 snls_status snls_bias(const float* dists, const float* inds, const float* table, const snls_params* p,
                       const snls_bias_params* bias, float* out, void* stream);
 
@@ -360,7 +361,8 @@ snls_status snls_bias(const float* dists, const float* inds, const float* table,
  *                snls_workspace_size(SNLS_OP_BIAS_BACKWARD, p) bytes, 256-byte
  *                aligned
  * The result does not depend on scheduling: it is bit-identical between runs.
- * Errors: as snls_bias; SNLS_ERR_WORKSPACE. */
+ * Errors: as snls_bias; SNLS_ERR_UNSUPPORTED for 2^16 heads or more;
+ * SNLS_ERR_WORKSPACE. */
 snls_status snls_bias_backward(const float* grad_scores, const float* dists, const float* inds, const snls_params* p,
                                const snls_bias_params* bias, float* grad_table, void* workspace,
                                size_t workspace_bytes, void* stream);
@@ -388,7 +390,8 @@ snls_status snls_backward_scores(const float* q, const float* k, const float* v,
  *   scales  (B, slots, HD, ceil(H/block), ceil(W/block)) fp32, powers of two
  * and stands for code * scale.  struct_size must be sizeof(snls_cache_params).
  * Limits (SNLS_ERR_UNSUPPORTED): block 8 or 16, C/HD <= 256, H and W below
- * 1,000,000, H*W*Cp below 2^31. */
+ * 1,000,000, H*W*Cp below 2^31, B*slots below 2^31, and B*HD*H*W, with H and W
+ * rounded up to multiples of 16 and 32, below 2^30. */
 typedef struct {
   uint32_t struct_size;
   int32_t B, slots, C, H, W, HD;
@@ -397,8 +400,8 @@ typedef struct {
 
 /* snls_cache_store -- one frame of keys and values into the cache.  The scale
  * of a block is the smallest power of two (2^-126 or more) with which its
- * largest finite magnitude fits e4m3 (448); a value is its quotient by the scale, rounded to the
- * nearest code, ties to even.  Infinities are held as +-448 * scale, NaN as NaN;
+ * largest finite magnitude fits e4m3 (448); a value is its quotient by the
+ * scale, rounded to the nearest code, ties to even.  Infinities are held as +-448 * scale, NaN as NaN;
  * a block of zeros has scale 1.
  *   k, v     device, (B, C, H, W)
  *   slots    device, int32 (B): the slot video b's frame goes to; a value
@@ -427,9 +430,11 @@ snls_status snls_cache_store(const float* k, const float* v, const int32_t* slot
  *   ws       window side, 1 .. 15 (SNLS_ERR_UNSUPPORTED above)
  *   scale    finite
  *   out      device out, (B, C, H, W), fully overwritten
+ * Logits may be held in base 2, so a sum of q.k~ and the table entry whose
+ * logit's magnitude passes 2.3e38 may count as not finite; a table entry alone
+ * does not (a mask of the type's lowest value is a finite logit).
  * The result does not depend on scheduling.  Errors: SNLS_ERR_INVALID_ARG,
- * SNLS_ERR_UNSUPPORTED (limits of the cache and of the bias, 2^31 pixels and
- * heads in all), SNLS_ERR_HIP. */
+ * SNLS_ERR_UNSUPPORTED (limits of the cache and of the bias), SNLS_ERR_HIP. */
 snls_status snls_cache_attend(const float* q, const float* flows, const int32_t* ages, const void* k_codes,
                               const float* k_scales, const void* v_codes, const float* v_scales,
                               const float* table, const snls_cache_params* cp, const snls_bias_params* bias,
@@ -443,7 +448,8 @@ snls_status snls_cache_attend(const float* q, const float* flows, const int32_t*
  *   flows    device, (n, slots, 2), or NULL for offsets of 0
  *   out      device out, (n, C), fully overwritten; nothing is touched when
  *            n == 0
- * Everything else as in snls_cache_attend; n < 0 is SNLS_ERR_INVALID_ARG. */
+ * Everything else as in snls_cache_attend; n < 0 is SNLS_ERR_INVALID_ARG,
+ * (n + 64) * HD of 2^30 or more SNLS_ERR_UNSUPPORTED. */
 snls_status snls_cache_attend_points(const float* q, const int32_t* points, int64_t n, const float* flows,
                                      const int32_t* ages, const void* k_codes, const float* k_scales,
                                      const void* v_codes, const float* v_scales, const float* table,

@@ -54,7 +54,8 @@ snls_status check_bias_call(const snls_params* p, const snls_bias_params* bias, 
   snls_status st = check_params(p, false, g);
   if (st != SNLS_OK) return st;
   if ((st = check_bias(bias, b)) != SNLS_OK) return st;
-  if ((double)g->rows * (g->k > 0 ? g->k : g->ncand) > 1099511627776.0) return SNLS_ERR_UNSUPPORTED;
+  if ((double)g->rows * (g->k > 0 ? g->k : g->ncand) >= 274877906944.0) return SNLS_ERR_UNSUPPORTED;  // 2^38
+  if ((double)g->B * g->HD * g->T >= 16777216.0) return SNLS_ERR_UNSUPPORTED;
   return SNLS_OK;
 }
 
@@ -245,6 +246,7 @@ snls_status snls_bias_backward(const float* grad_scores, const float* dists, con
   snls_status st = check_bias_call(p, bias, &g, &b);
   if (st != SNLS_OK) return st;
   if (!grad_scores || !dists || !inds || !grad_table) return SNLS_ERR_INVALID_ARG;
+  if (g.HD >= 1 << 16) return SNLS_ERR_UNSUPPORTED;  // a launch holds less than 2^32 threads
   if (!workspace || workspace_bytes < bias_backward_ws_bytes(g) || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return SNLS_ERR_WORKSPACE;
   if ((st = device_ready()) != SNLS_OK) return st;
@@ -288,7 +290,7 @@ snls_status snls_cache_attend_points(const float* q, const int32_t* points, int6
   snls_status st = check_attend(q, ages, k_codes, k_scales, v_codes, v_scales, table, cp, bias, ws, scale, out, &c, &b);
   if (st != SNLS_OK) return st;
   if (!points || n < 0) return SNLS_ERR_INVALID_ARG;
-  if ((double)n * c.HD >= 2147483648.0) return SNLS_ERR_UNSUPPORTED;
+  if ((double)n * c.HD >= 1073741824.0 - 64.0 * c.HD) return SNLS_ERR_UNSUPPORTED;  // 4 threads each
   if (n == 0) return SNLS_OK;
   if ((st = device_ready()) != SNLS_OK) return st;
   return launch_cache_attend(q, points, n, flows, ages, static_cast<const uint8_t*>(k_codes), k_scales,

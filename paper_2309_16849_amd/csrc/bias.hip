@@ -142,13 +142,13 @@ __global__ void __launch_bounds__(64) bias_grad_kernel(const float* __restrict__
   }
 }
 
-// grad_table[hd][i] = sum of the head's slices, in 64 bits: 64 entries a
-// workgroup, its 16 waves take every 16th slice.
+// grad_table[hd][i] = sum of the head's slices, in 64 bits: 64 entries of a
+// head a workgroup, its 16 waves take every 16th slice.
 __global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const float* __restrict__ part, int buckets, int slices,
                                                              float* __restrict__ grad_table) {
   __shared__ double sums[16][64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int hd = blockIdx.y, i = blockIdx.x * 64 + lane;
+  const int per = (buckets + 63) / 64, hd = blockIdx.x / per, i = (int)(blockIdx.x % per) * 64 + lane;
   double s = 0.0;
   if (i < buckets) {
     const float* p = part + (long long)hd * slices * buckets + i;
@@ -194,7 +194,7 @@ snls_status launch_bias(const float* dists, const float* inds, const float* tabl
   long long run = images * r.chunks / (4 * 8192);
   run = run < 1 ? 1 : run > 16 ? 16 : run;
   const long long groups = (r.chunks + 4 * run - 1) / (4 * run);
-  if (images * groups > 0x7fffffffLL) return SNLS_ERR_UNSUPPORTED;
+  if (images * groups >= 1LL << 24) return SNLS_ERR_UNSUPPORTED;  // a launch holds less than 2^32 threads
   hipLaunchKernelGGL(bias_kernel, dim3((unsigned)(images * groups)), dim3(256), bias.buckets * sizeof(float), s, dists,
                      inds, table, r, bias, g.dist == SNLS_DIST_PROD ? 1.f : -1.f, (int)run, (unsigned)groups, out);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
@@ -203,13 +203,14 @@ snls_status launch_bias(const float* dists, const float* inds, const float* tabl
 snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
                                  const Bias& bias, float* grad_table, float* ws, hipStream_t s) {
   const int slices = (int)bias_slices(g, bias.buckets);
+  const int sums = (bias.buckets + 63) / 64 * g.HD;  // at most 64 a head
   int cols = 8;  // as many copies as leave room for all the waves
   while (cols > 1 && bias.buckets * cols * (int)sizeof(double) > kLds / kMostWaves) cols /= 2;
   hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)(g.HD * slices)), dim3(64),
                      (size_t)bias.buckets * cols * sizeof(double), s, grad, dists, inds, bias_rows(g), bias,
                      g.dist == SNLS_DIST_PROD ? 1.f : -1.f, cols, slices, ws);
-  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)((bias.buckets + 63) / 64), (unsigned)g.HD), dim3(1024), 0,
-                     s, ws, bias.buckets, slices, grad_table);
+  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)sums), dim3(1024), 0, s, ws, bias.buckets, slices,
+                     grad_table);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 

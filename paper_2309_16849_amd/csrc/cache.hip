@@ -119,7 +119,7 @@ snls_status launch_cache_store(const float* k, const float* v, const int32_t* sl
                                uint8_t* k_codes, float* k_scales, uint8_t* v_codes, float* v_scales, hipStream_t s) {
   const int tw = c.sh == 3 ? 32 : 16, th = 256 / tw;
   const int tx = (c.W + tw - 1) / tw, ty = (c.H + th - 1) / th;
-  // (fewer workgroups than pixels and heads, which fit 31 bits)
+  // (one thread per pixel and head of the padded frame, which fit 30 bits)
   const dim3 grid((unsigned)(c.B * c.HD * tx * ty), 2);
 #define SNLS_STORE(NV)                                                                                        \
   hipLaunchKernelGGL(cache_store_kernel<NV>, grid, dim3(256), 0, s, k, v, slots, c, k_codes, k_scales, v_codes, \

@@ -80,8 +80,9 @@ snls_status check_cache(const snls_cache_params* c, CacheGeo* out) {
   const int Cp = (Ch + 15) / 16 * 16;
   // a token's byte offset inside its plane is 32-bit; planes are found with 64 bits
   if ((long long)c->H * c->W * Cp >= 1LL << 31) return SNLS_ERR_UNSUPPORTED;
-  // workgroups: one per head and some pixels at most
-  if ((double)c->B * c->HD * c->H * c->W >= 2147483648.0 || (double)c->B * c->slots >= 2147483648.0)
+  // a launch holds less than 2^32 threads, 4 per pixel and head of the padded frame
+  const double pixels = (double)((c->H + 15) / 16 * 16) * ((c->W + 31) / 32 * 32);
+  if ((double)c->B * c->HD * pixels >= 1073741824.0 || (double)c->B * c->slots >= 2147483648.0)
     return SNLS_ERR_UNSUPPORTED;
   out->B = c->B; out->S = c->slots; out->C = c->C; out->HD = c->HD; out->H = c->H; out->W = c->W;
   out->Ch = Ch;

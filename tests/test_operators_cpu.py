@@ -98,6 +98,9 @@ BAD_CACHE = [
     (dict(C=514), B.SNLS_ERR_UNSUPPORTED), (dict(H=1000000, W=1), B.SNLS_ERR_UNSUPPORTED),
     (dict(H=40000, W=40000), B.SNLS_ERR_UNSUPPORTED),  # a plane of 2^31 bytes or more
     (dict(B=1 << 20, H=1 << 10, W=1 << 10), B.SNLS_ERR_UNSUPPORTED),
+    (dict(B=1 << 10, H=1 << 9, W=1 << 10), B.SNLS_ERR_UNSUPPORTED),  # 2^30 pixels and heads
+    (dict(B=1 << 20, H=3, W=3), B.SNLS_ERR_UNSUPPORTED),  # ... of padded frames
+    (dict(B=1 << 16, slots=1 << 15, H=3, W=3), B.SNLS_ERR_UNSUPPORTED),
 ]
 
 
@@ -145,7 +148,20 @@ def test_cache_refuses_bad_arguments(lib):
                                         None) == B.SNLS_ERR_INVALID_ARG
     assert lib.snls_cache_attend_points(FAKE, FAKE, 1 << 30, *ok[1:], None, cp, None, 3, 1.0, FAKE,
                                         None) == B.SNLS_ERR_UNSUPPORTED
+    assert lib.snls_cache_attend_points(FAKE, FAKE, (1 << 29) - 64, *ok[1:], None, cp, None, 3, 1.0, FAKE,
+                                        None) == B.SNLS_ERR_UNSUPPORTED  # a launch of 2^32 threads
     assert lib.snls_cache_attend_points(FAKE, FAKE, 0, *ok[1:], None, cp, None, 3, 1.0, FAKE, None) == B.SNLS_OK
+
+
+def test_bias_refuses_too_many(lib):
+    bp = ctypes.byref(_bias())
+    many = ctypes.byref(_params(B=1 << 13, T=1 << 10, H=16, W=16))  # 2^24 images
+    long = ctypes.byref(_params(B=1 << 10, T=1 << 10, H=1 << 10, W=1 << 10, k=1))  # 2^41 scores
+    heads = ctypes.byref(_params(B=1, T=1, C=1 << 17, HD=1 << 16, H=16, W=16))
+    for pp in (many, long):
+        assert lib.snls_bias(FAKE, FAKE, FAKE, pp, bp, FAKE, None) == B.SNLS_ERR_UNSUPPORTED
+        assert lib.snls_bias_backward(FAKE, FAKE, FAKE, pp, bp, FAKE, FAKE, BIG, None) == B.SNLS_ERR_UNSUPPORTED
+    assert lib.snls_bias_backward(FAKE, FAKE, FAKE, heads, bp, FAKE, FAKE, BIG, None) == B.SNLS_ERR_UNSUPPORTED
 
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="checks the no-device error path")
