@@ -505,3 +505,56 @@ def test_query_sizes(dev, size):
     keep[10, 11] = keep[20, 3] = keep[5, 5] = False
     assert bool((out[0, :, 10, 11] == 0).all()) and bool((out[0, :, 20, 3] == 0).all())
     assert torch.equal(out[:, :, keep], whole[:, :, keep]) and bool((out[0, :, 5, 5] != 0).any())
+
+
+@pytest.mark.parametrize("C,HD,ws", [(64, 2, 9), (64, 1, 9), (96, 1, 5), (256, 2, 7)])
+def test_wide_heads_in_a_graph_and_beside_another_call(dev, C, HD, ws):
+    """Heads whose scores come from the matrix cores: replays with new inputs, offsets that are not finite, tokens
+    that are NaN and slots that hold nothing; the same call on another stream meanwhile."""
+    cp = _cp(B=2, C=C, HD=HD, H=37, W=45, slots=3)
+    gen = torch.Generator(device=dev).manual_seed(61)
+    cache, _, _ = _filled(cp, dev)
+    q = torch.randn(2, C, 37, 45, device=dev, generator=gen)
+    fl = torch.empty(2, 3, 2, 37, 45, device=dev)
+    ages = torch.tensor([[2, 1, 0], [0, -1, 5]], dtype=torch.int32, device=dev)
+    scale = 1.0 / (C // HD) ** 0.5
+    keys = cache[0].view(torch.uint8)
+    keys[0, 0, :, 10, 10, 3] = 0x7F  # NaN
+    keys[1, 1] = 0x7F  # a slot that holds no frame
+    cache[2].view(torch.uint8)[1, 1] = 0x7F
+    out, other = torch.empty_like(q), torch.empty_like(q)
+
+    def step(to):
+        return B.snls_cache_attend(q, fl, ages, cache, cp, ws, scale, out=to)
+
+    def fresh():
+        fl.normal_(generator=gen).mul_(3)
+        fl[0, 1, 0, 5:9, 3], fl[0, 2, 1, 20, 7:30], fl[1, 0, 0, 30] = float("nan"), float("inf"), 1e6
+        fl[1, 2, :, :8, :8] = -1e5  # windows outside the frame
+        q.normal_(generator=gen)
+
+    fresh()
+    step(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        fresh()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(other)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, other) and torch.equal(out, step(torch.empty_like(q)))
+        assert bool(out.isfinite().all())
+        # the points' form of the same pixels, by the vector units
+        b, h, w = torch.meshgrid(torch.arange(2), torch.arange(37), torch.arange(45), indexing="ij")
+        pts = torch.stack([b, h, w], -1).view(-1, 3).to(torch.int32).to(dev)
+        qp = q.permute(0, 2, 3, 1).reshape(-1, C).contiguous()
+        fp = fl.permute(0, 3, 4, 1, 2).reshape(-1, 3, 2).contiguous()
+        got = B.snls_cache_attend_points(qp, pts, fp, ages, cache, cp, ws, scale).view(2, 37, 45, C)
+        kv, vv = (torch.full((1,), x, dtype=R.F64) for x in (6.0, 6.0))  # |N(0,1)| of these sizes stays below 6
+        tol = 2 * _tol(qp.cpu(), kv, vv, cp, ws, scale, 60.0, None)
+        assert float((got.permute(0, 3, 1, 2) - out).abs().max()) <= tol

@@ -215,3 +215,53 @@ def test_streams_and_graph(dev):
         torch.cuda.synchronize()
         assert torch.equal(out.view(torch.int32), B.snls_bias(dg, ig, table, p, bias).view(torch.int32))
         assert torch.equal(gt, B.snls_bias_backward(grad, dg, ig, p, bias))
+
+
+@pytest.mark.parametrize("HD", [4095, 4097, 9000])
+def test_many_heads(dev, HD):
+    """More heads than waves on the chip: one slice a head."""
+    p, bias = small_params(T=2, C=HD, H=3, W=3, HD=HD, k=3), dict(radius=0, edges=[1.0])
+    d, inds = _neighbours(p, 3)
+    g = torch.Generator().manual_seed(4)
+    table = torch.randn(B.bias_table_shape(bias, HD), generator=g)
+    grad = torch.randn(d.shape, generator=g)
+    out = B.snls_bias(d.to(dev), inds.to(dev), table.to(dev), p, bias)
+    assert torch.equal(out.cpu().view(torch.int32), R.biased(d, inds, table, p, bias).view(torch.int32))
+    got = B.snls_bias_backward(grad.to(dev), d.to(dev), inds.to(dev), p, bias).cpu()
+    ref, cnt, mag = R.table_grad(grad, d, inds, p, bias, HD)
+    assert bool(((got.double() - ref).abs() <= cnt * EPS * mag + 1e-300).all())
+
+
+def test_training_step_in_a_graph(dev):
+    """Search to table gradient in one graph on one workspace each, replayed with new inputs against the eager step."""
+    p = small_params(T=3, C=16, H=12, W=13, HD=2, ws=5, wt=1, ps=3, k=6)
+    bias = dict(radius=1, edges=[0.5, 2.0])
+    gen = torch.Generator(device=dev).manual_seed(12)
+    q, k, v, go = (torch.randn(B.video_shape(p), device=dev, generator=gen) for _ in range(4))
+    fl = torch.randn(B.flow_shape(p), device=dev, generator=gen)
+    table = torch.randn(B.bias_table_shape(bias, 2), device=dev, generator=gen)
+
+    def step():
+        d, i = B.snls_search(q, k, fl, p)
+        d = B.snls_bias(d, i, table, p, bias, out=d)
+        out = B.snls_aggregate(v, d, i, p, 0.2)
+        grads = B.snls_backward_scores(q, k, v, fl, d, i, go, p, 0.2)
+        return (out,) + grads + (B.snls_bias_backward(grads[4], d, i, p, bias),)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(3):
+        for t in (q, k, v, go, fl, table):
+            t.normal_(generator=gen)
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        for a, b, name in zip(held, want, ("out", "grad_q", "grad_k", "grad_v", "grad_flows", "grad_scores",
+                                           "grad_table")):
+            assert_close(a.cpu().numpy(), b.cpu().numpy(), name, rel=1e-5)
