@@ -142,26 +142,27 @@ __global__ void __launch_bounds__(64) bias_grad_kernel(const float* __restrict__
   }
 }
 
-// grad_table[hd][i] = sum of the head's slices, in 64 bits: 64 entries of a
-// head a workgroup, its 16 waves take every 16th slice.
+// grad_table[hd][i] = sum of the head's slices, in 64 bits: `ent` entries (a
+// power of two up to 64) of a head a workgroup, its 1024 / ent groups of lanes
+// take the slices in turn.
 __global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const float* __restrict__ part, int buckets, int slices,
-                                                             float* __restrict__ grad_table) {
-  __shared__ double sums[16][64];
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int per = (buckets + 63) / 64, hd = blockIdx.x / per, i = (int)(blockIdx.x % per) * 64 + lane;
+                                                             int ent, float* __restrict__ grad_table) {
+  __shared__ double sums[1024];
+  const int lane = threadIdx.x & (ent - 1), group = threadIdx.x / ent, groups = 1024 / ent;
+  const int per = (buckets + ent - 1) / ent, hd = blockIdx.x / per, i = (int)(blockIdx.x % per) * ent + lane;
   double s = 0.0;
   if (i < buckets) {
     const float* p = part + (long long)hd * slices * buckets + i;
 #pragma unroll 8
-    for (int k = wv; k < slices; k += 16) s += p[(long long)k * buckets];
+    for (int k = group; k < slices; k += groups) s += p[(long long)k * buckets];
   }
-  sums[wv][lane] = s;
+  sums[threadIdx.x] = s;
   __syncthreads();
-  if (wv == 0 && i < buckets) {
-#pragma unroll
-    for (int k = 1; k < 16; ++k) s += sums[k][lane];
-    grad_table[(long long)hd * buckets + i] = (float)s;
+  for (int half = groups / 2; half > 0; half /= 2) {
+    if (group < half) sums[threadIdx.x] += sums[threadIdx.x + half * ent];
+    __syncthreads();
   }
+  if (group == 0 && i < buckets) grad_table[(long long)hd * buckets + i] = (float)sums[lane];
 }
 
 // Slices of a head: as many waves as lie on the chip at once with their tables
@@ -203,13 +204,16 @@ snls_status launch_bias(const float* dists, const float* inds, const float* tabl
 snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
                                  const Bias& bias, float* grad_table, float* ws, hipStream_t s) {
   const int slices = (int)bias_slices(g, bias.buckets);
-  const int sums = (bias.buckets + 63) / 64 * g.HD;  // at most 64 a head
+  // entries a workgroup of the second kernel: few while the table is small and
+  // workgroups short (a whole call with 16 / 64: 2 tables of 75 21.0 / 22.4 us,
+  // 4 of 1,183 141 / 138)
+  const int ent = bias.buckets <= 256 ? 16 : 64, sums = (bias.buckets + ent - 1) / ent * g.HD;  // at most 64 a head
   int cols = 8;  // as many copies as leave room for all the waves
   while (cols > 1 && bias.buckets * cols * (int)sizeof(double) > kLds / kMostWaves) cols /= 2;
   hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)(g.HD * slices)), dim3(64),
                      (size_t)bias.buckets * cols * sizeof(double), s, grad, dists, inds, bias_rows(g), bias,
                      g.dist == SNLS_DIST_PROD ? 1.f : -1.f, cols, slices, ws);
-  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)sums), dim3(1024), 0, s, ws, bias.buckets, slices,
+  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)sums), dim3(1024), 0, s, ws, bias.buckets, slices, ent,
                      grad_table);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }

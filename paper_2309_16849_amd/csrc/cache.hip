@@ -409,7 +409,7 @@ SNLS_DEV float table_base2(float t, float scale) {
   return fabsf(x) < INFINITY ? fminf(fmaxf(x * kLog2e, -3.402823466e38f), 3.402823466e38f) : x;
 }
 
-// MX: scores from the matrix cores (heads of 17 channels and more; 64 channels
+// MX: scores from the matrix cores (heads of 17 to 128 channels; 64 channels
 // at 480 x 854 1.45 -> 1.08 ms, two heads of 32 at 256 x 256 0.32 -> 0.27).  The
 // windows of a wave's 16 queries overlap, so the box around them in a slot's
 // frame is walked in tiles of 16 tokens, v_mfma_f32_16x16x32_f16 with tokens as
@@ -420,7 +420,10 @@ SNLS_DEV float table_base2(float t, float scale) {
 // (offsets carry an error of pixels), the matrix cores 30 times as fast as the
 // vector units on such a product.  Where the box would be larger than the 16
 // windows are together (offsets that differ by tens of pixels between
-// neighbours), every window is a box of its own.
+// neighbours), every window is a box of its own.  64 channels at 200 x 240, 3
+// slots: equal offsets 119 us, neighbours' offsets 1 / 3 / 10 / 40 pixels apart
+// 131 / 149 / 270 / 275, the vector units 165 whatever they are; the vector
+// units' form as a second branch 204 at 40 pixels, but 127 at 0, for its registers.
 template <int CT>
 constexpr int kBoxPitch = CT + 6;  // a row of taps with the three beside it that a group of four tokens may bring
 template <int CT>
