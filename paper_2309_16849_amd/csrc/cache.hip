@@ -44,9 +44,11 @@ SNLS_DEV unsigned encode4(float a, float b, float c, float d, float inv) {
 }
 
 // One workgroup = 256 pixels of one (video, head): a 16 x 16 block, or four
-// 8 x 8 blocks side by side; one thread per pixel.  Up to NV * 16 channels stay
-// in registers between the largest magnitude and the codes; NV = 0: heads of
-// more channels are read twice (the second time from L2).  blockIdx.y = 0
+// 8 x 8 blocks side by side; one thread per pixel.  The channels (up to NV * 16)
+// stay in registers between the largest magnitude and the codes; read a second
+// time instead, 128 channels at 480 x 854 take 286 us, not 144, 256 take 579,
+// not 333 (at one wave a SIMD), 64 take 150, not 67.  Bound by memory: 64
+// channels at 84% of a copy's rate, 128 at 77%, 256 at 67%.  blockIdx.y = 0
 // stores keys, 1 values.
 template <int NV>
 __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restrict__ k, const float* __restrict__ v,
@@ -72,20 +74,14 @@ __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restric
   if (threadIdx.x < 4) top[threadIdx.x] = 0u;
   __syncthreads();
   const float* px = src + (in ? (long long)y * c.W + x : 0);
-  float val[NV ? NV * 16 : 1];
+  float val[NV * 16];
   float amax = 0.f;
-  auto grow = [&](float t) {
-    const float m = fabsf(t);
+#pragma unroll
+  for (int ch = 0; ch < NV * 16; ++ch) val[ch] = in && ch < c.Ch ? px[ch * HW] : 0.f;
+#pragma unroll
+  for (int ch = 0; ch < NV * 16; ++ch) {
+    const float m = fabsf(val[ch]);
     amax = m < INFINITY ? fmaxf(amax, m) : amax;
-  };
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int ch = 0; ch < NV * 16; ++ch) val[ch] = in && ch < c.Ch ? px[ch * HW] : 0.f;
-#pragma unroll
-    for (int ch = 0; ch < NV * 16; ++ch) grow(val[ch]);
-  } else if (in) {
-#pragma unroll 16
-    for (int ch = 0; ch < c.Ch; ++ch) grow(px[ch * HW]);
   }
   // over the block's row in this wave, then over the workgroup (magnitudes order like their bits)
 #pragma unroll
@@ -98,20 +94,12 @@ __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restric
   const int mask = (1 << c.sh) - 1;
   if ((ly & mask) == 0 && (lx & mask) == 0) scales[(y >> c.sh) * c.nbx + (x >> c.sh)] = scale;
   uint4* dst = reinterpret_cast<uint4*>(codes + ((long long)y * c.W + x) * c.Cp);
-  auto put = [&](int j, const float* f) {
-    dst[j] = make_uint4(encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv),
-                        encode4(f[8], f[9], f[10], f[11], inv), encode4(f[12], f[13], f[14], f[15], inv));
-  };
-  if constexpr (NV > 0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) put(j, val + 16 * j);
-  } else {
-    for (int j = 0; j < c.nv; ++j) {
-      float f[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) f[i] = j * 16 + i < c.Ch ? px[(j * 16 + i) * HW] : 0.f;
-      put(j, f);
-    }
+  for (int j = 0; j < NV; ++j) {
+    const float* f = val + 16 * j;
+    if (j < c.nv)
+      dst[j] = make_uint4(encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv),
+                          encode4(f[8], f[9], f[10], f[11], inv), encode4(f[12], f[13], f[14], f[15], inv));
   }
 }
 
@@ -129,7 +117,10 @@ snls_status launch_cache_store(const float* k, const float* v, const int32_t* sl
     case 2: SNLS_STORE(2); break;
     case 3: SNLS_STORE(3); break;
     case 4: SNLS_STORE(4); break;
-    default: SNLS_STORE(0); break;
+    case 5: case 6: SNLS_STORE(6); break;
+    case 7: case 8: SNLS_STORE(8); break;
+    case 9: case 10: case 11: case 12: SNLS_STORE(12); break;
+    default: SNLS_STORE(16); break;
   }
 #undef SNLS_STORE
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;

@@ -107,6 +107,24 @@ def test_store_is_exact(dev, kw):
                 assert bool((codes[b, s][..., Ch:].view(torch.uint8) == 0).all())
 
 
+@pytest.mark.parametrize("C", [80, 96, 100, 112, 127, 129, 160, 191, 192, 200, 240, 255])
+def test_store_wide_heads(dev, C):
+    """Every number of 16-channel vectors a token can have, and numbers of channels that do not fill the last."""
+    cp = _cp(C=C, HD=1, H=21, W=35, slots=2)
+    g = torch.Generator().manual_seed(71)
+    k, v = (torch.randn(1, C, 21, 35, generator=g) * torch.exp2(torch.randint(-9, 9, (1, C, 21, 35), generator=g).float())
+            for _ in range(2))
+    cache = B.cache_alloc(cp, dev)
+    cache[0].view(torch.uint8).fill_(0x55)
+    B.snls_cache_store(k.to(dev), v.to(dev), torch.ones(1, dtype=torch.int32, device=dev), cp, cache)
+    for src, codes, scales in ((k, cache[0], cache[1]), (v, cache[2], cache[3])):
+        rc, rs = R.e4m3(src.view(1, 1, C, 21, 35), 8)
+        assert torch.equal(scales[0, 1].cpu().double(), rs[0])
+        assert torch.equal(codes[0, 1].cpu()[..., :C].float().double(), rc[0].permute(0, 2, 3, 1))
+        assert bool((codes[0, 1].cpu()[..., C:].view(torch.uint8) == 0).all())
+    assert bool((cache[0][0, 0].view(torch.uint8) == 0x55).all())
+
+
 def test_store_not_finite(dev):
     """Infinities are held as +-448 times the scale of the finite values, NaN as NaN; they do not touch the scale."""
     cp = _cp(C=16, HD=1, H=9, W=10, slots=1)
