@@ -369,8 +369,11 @@ snls_status snls_bias_backward(const float* grad_scores, const float* dists, con
 
 /* snls_backward_scores -- snls_backward that also returns grad_scores
  * (B,HD,T,nH,nW,k), dL/d dists of the loss through the aggregation plus
- * grad_dists: what the gradient of anything added to the scores starts from
- * (0 for neighbours that contribute nothing).  With biased scores as dists the
+ * grad_dists: what the gradient of anything added to the scores starts from.
+ * It is 0 for a score that is not finite.  A finite score whose position
+ * contributes nothing stays in snls_aggregate's softmax, where it scales the
+ * other weights, and has the gradient of that; grad_dists is added only where
+ * the position contributes.  With biased scores as dists the
  * gradients of q, k, v and the flows are those of the biased layer.  Every
  * other argument, the workspace (SNLS_OP_BACKWARD) and the errors are those of
  * snls_backward; grad_scores must not be NULL. */

@@ -359,12 +359,11 @@ __global__ void __launch_bounds__(256) backward_search_kernel(const float* __res
   for (int l = 0; l < g.k; ++l) {
     int t2, ny, nx;
     float ay, ax;
-    const bool ok = isfinite(drow[l]) && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
+    const bool fin = isfinite(drow[l]), ok = fin && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
+    // (a finite score at a bad position still scales the other weights: G_l = 0, but dd_l is not)
     float dd = 0.f;
-    if (ok) {
-      if (z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
-      if (grad_dists) dd += grad_dists[row * g.k + l];
-    }
+    if (fin && z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
+    if (ok && grad_dists) dd += grad_dists[row * g.k + l];
     if (dd_out && lane == 0) dd_out[row * g.k + l] = dd;
     if (!ok || dd == 0.f) continue;
     const long long fbase = ((long long)rp.b * g.T + t2) * g.HW;
@@ -607,14 +606,13 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
     const int l = NG == 1 ? l0 : l0 + lane / LW;
     int t2 = 0, ny = 0, nx = 0;
     float ay = 0.f, ax = 0.f;
-    const bool ok = l < g.k && isfinite(drow[l]) && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
+    const bool fin = l < g.k && isfinite(drow[l]), ok = fin && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
     float dd = 0.f;
-    if (ok) {
-      if (z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
-      if (grad_dists) dd += grad_dists[row * g.k + l];
-    }
+    if (fin && z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
+    if (ok && grad_dists) dd += grad_dists[row * g.k + l];
     if (last && l < g.k) dd_out[row * g.k + l] = dd;
-    if (NG == 1 ? dd == 0.f : !__any(dd != 0.f)) continue;  // (dd is 0 where not ok)
+    if (!ok) dd = 0.f;  // nothing is read at a bad position (its score still scales the other weights)
+    if (NG == 1 ? dd == 0.f : !__any(dd != 0.f)) continue;
     const int Y0 = rp.h + lo + ny, X0 = rp.w + lo + nx;
     float kb[PB * PB];
     {
