@@ -424,7 +424,9 @@ snls_status snls_cache_store(const float* k, const float* v, const int32_t* slot
  * [0,H-1] x [0,W-1]; its logit is scale * (q.k~ + table entry), its bucket that
  * of the frame step -age and of the fp32 displacement; a logit that is not
  * finite does not count.  out = sum of softmax(logits) * v~ over the candidates
- * of all slots, 0 where none counts; v~'s taps of weight 0 are not read.
+ * of all slots, 0 where none counts; v~'s taps of weight 0 in fp32 are not
+ * read (a NaN there does not show; one whose weight only rounding makes 0 or
+ * not, about 2^-149 of the largest and below, may).
  *   q        device, (B, C, H, W)
  *   flows    device, (B, slots, 2, H, W), or NULL for offsets of 0
  *   ages     device, int32 (B, slots): frames since the slot's, negative for

@@ -171,6 +171,11 @@ SNLS_DEV void spread16(uint4 t, float wgt, float* acc) {
   }
 }
 
+// A sum of weighted values when the softmax's maximum rises and its weights
+// fall by f.  A factor of 0 takes the values out, NaN among them: a value of
+// weight 0 is not read either where the maximum was known before.
+SNLS_DEV float faded(float x, float f) { return f == 0.f ? 0.f : x * f; }
+
 // A cell at whole-pixel position y, plus a fraction or not, has its centre in
 // [0, n-1].
 SNLS_DEV bool cell_ok(int y, bool frac, int n) { return y >= 0 && (frac ? y < n - 1 : y < n); }
@@ -281,7 +286,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
       m = m2;
       z *= f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[i] *= f;
+      for (int i = 0; i < 16; ++i) acc[i] = faded(acc[i], f);
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
         const int j = k * 64 + lane;
@@ -334,7 +339,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
         if (join_mz[i][0] != -INFINITY) {
           const float f = expf(join_mz[i][0] - M);
           Z += f * join_mz[i][1];
-          o += f * join_acc[i][ch];
+          o += faded(join_acc[i][ch], f);
         }
     a.out[qi * c.C + hd * c.Ch + ch] = Z > 0.f ? o / Z : 0.f;
   }
@@ -796,7 +801,7 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[v][i] *= f;
+          for (int i = 0; i < 16; ++i) acc[v][i] = faded(acc[v][i], f);
       }
       const float mm = fmaxf(m, -3.402823466e38f);  // nothing counted yet: weights 2^-inf
 #pragma unroll
@@ -870,7 +875,8 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
         m = top;
         z = z * f + buf[64] * fj;
 #pragma unroll
-        for (int i = 0; i < 16 * V; ++i) acc[i / 16][i % 16] = acc[i / 16][i % 16] * f + buf[(2 + i) * 64] * fj;
+        for (int i = 0; i < 16 * V; ++i)
+          acc[i / 16][i % 16] = faded(acc[i / 16][i % 16], f) + faded(buf[(2 + i) * 64], fj);
       }
     }
     if (part_of != 0) return;
