@@ -169,7 +169,8 @@ snls_status snls_topk(const float* dists_all, const float* inds_all, int64_t row
 /* snls_aggregate -- weighted patch aggregation (Sec. 3.2 "Aggregation").
  * For each query (b,t,h,w) and head, weights w_l = softmax_l(sign*scale*d_l)
  * over its k neighbours (sign +1 inner product, -1 L2; non-finite d_l get
- * weight 0); every in-frame patch pixel (h+p_h, w+p_w) receives
+ * weight 0; scale*d_l itself may pass fp32's range, as a mask of the type's
+ * lowest value does, only the scores' differences count); every in-frame patch pixel (h+p_h, w+p_w) receives
  * sum_l w_l * v~(frame_l, c, h+p_h+disp_h,l, w+p_w+disp_w,l) for the head's
  * channels; each output pixel is divided by the number of query patches
  * covering it, and pixels no patch covers are 0.  Neighbours whose frame

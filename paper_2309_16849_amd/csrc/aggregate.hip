@@ -51,13 +51,14 @@ __global__ void __launch_bounds__(256) softmax_weights_kernel(const float* __res
   float m = -INFINITY;
   if (live)
     for (int l = sub; l < g.k; l += G)
-      if (isfinite(d[l])) m = fmaxf(m, sscale * d[l]);
+      if (isfinite(d[l])) m = fmaxf(m, softmax_key(sscale, d[l]));
 #pragma unroll
   for (int off = G / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  const RowSoftmax term(sscale, m);
   float z = 0.f;
   if (live)
     for (int l = sub; l < g.k; l += G)
-      if (isfinite(d[l])) z += expf(sscale * d[l] - m);
+      if (isfinite(d[l])) z += term(d[l]);
 #pragma unroll
   for (int off = G / 2; off > 0; off >>= 1) z += __shfl_xor(z, off);
   if (!live) return;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(256) softmax_weights_kernel(const float* __res
     const float tf = ind[3 * l], dh = ind[3 * l + 1], dw = ind[3 * l + 2];
     const bool ok = isfinite(d[l]) && tf >= 0.f && tf < (float)g.T && tf == floorf(tf) && fabsf(dh) < kFarDisp &&
                     fabsf(dw) < kFarDisp;
-    wts[row * g.k + l] = ok ? expf(sscale * d[l] - m) * inv : 0.f;
+    wts[row * g.k + l] = ok ? term(d[l]) * inv : 0.f;
   }
 }
 
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(aggt::NT) aggregate_tile_kernel(const float* _
   using namespace aggt;
   __shared__ int4 rtap[REC];        // fixed-point tap weights (0,0) (0,1) (1,0) (1,1)
   __shared__ int rcode[REC];        // bin of tap (0,0); -1 nothing; -2 direct path
-  __shared__ float qm[MAXQ], qinv[MAXQ];  // softmax max and 1/sum per covering query
+  __shared__ float qm[MAXQ], qinv[MAXQ];  // softmax's top key and 1/sum per covering query
   __shared__ int sstat[3 * NSLOT];  // per slot: sum of row offsets, of column offsets, count
   __shared__ int sbase[2 * NSLOT];  // per slot: box origin (row, column offset)
   __shared__ int ndirect;           // records of the tile outside the bin boxes
@@ -444,9 +445,10 @@ __global__ void __launch_bounds__(aggt::NT) aggregate_tile_kernel(const float* _
     const float* d = dq + j * K;
     float m = -INFINITY, z = 0.f;
     for (int l = 0; l < K; ++l)
-      if (isfinite(d[l])) m = fmaxf(m, sscale * d[l]);
+      if (isfinite(d[l])) m = fmaxf(m, softmax_key(sscale, d[l]));
+    const RowSoftmax term(sscale, m);
     for (int l = 0; l < K; ++l)
-      if (isfinite(d[l])) z += expf(sscale * d[l] - m);
+      if (isfinite(d[l])) z += term(d[l]);
     qm[j] = m;
     qinv[j] = z > 0.f ? 1.f / z : 0.f;
   }
@@ -467,7 +469,7 @@ __global__ void __launch_bounds__(aggt::NT) aggregate_tile_kernel(const float* _
     const bool ok = isfinite(d) && tf >= 0.f && tf < (float)g.T && tf == floorf(tf) && fabsf(dh) < kFarDisp &&
                     fabsf(dw) < kFarDisp;
     if (!ok) return;
-    wl = expf(sscale * d - qm[j]) * qinv[j];
+    wl = RowSoftmax(sscale, qm[j])(d) * qinv[j];
     t2 = (int)tf;
     const float fh = floorf(dh), fw = floorf(dw);
     nh = (int)fh;
@@ -827,11 +829,10 @@ __global__ void __launch_bounds__(256) aggregate_p1_kernel(const float* __restri
       dw = inds[(row * k + lane) * 3 + 2];
     }
     const bool fin = on && isfinite(d);
-    const float x = sscale * d;
-    float m = fin ? x : -INFINITY;
+    float m = fin ? softmax_key(sscale, d) : -INFINITY;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float e = fin ? expf(x - m) : 0.f;
+    const float e = fin ? RowSoftmax(sscale, m)(d) : 0.f;
     float z = e;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);

@@ -99,18 +99,18 @@ SNLS_DEV float load_or_zero(const float* __restrict__ p, long long off, bool ok)
   return ok ? v : 0.f;
 }
 
-// Softmax statistics of a row (lanes over the k entries): max and sum of
-// exp(sscale*d - max) over the finite entries.
-SNLS_DEV void softmax_stats(const float* __restrict__ d, int k, float sscale, int lane, float* m, float* z) {
-  float mx = -INFINITY;
+// Softmax of a row (lanes over the k entries) and its sum over the finite
+// entries.
+SNLS_DEV RowSoftmax row_softmax(const float* __restrict__ d, int k, float sscale, int lane, float* z) {
+  float top = -INFINITY;
   for (int l = lane; l < k; l += 64)
-    if (isfinite(d[l])) mx = fmaxf(mx, sscale * d[l]);
-  mx = wave_max(mx);
+    if (isfinite(d[l])) top = fmaxf(top, softmax_key(sscale, d[l]));
+  const RowSoftmax term(sscale, wave_max(top));
   float s = 0.f;
   for (int l = lane; l < k; l += 64)
-    if (isfinite(d[l])) s += expf(sscale * d[l] - mx);
-  *m = mx;
+    if (isfinite(d[l])) s += term(d[l]);
   *z = wave_sum(s);
+  return term;
 }
 
 // Neighbour l of a row: frame and decomposed displacement; false if it
@@ -285,8 +285,8 @@ __global__ void __launch_bounds__(256) backward_agg_kernel(const float* __restri
   const float* drow = dists + row * g.k;
   const float* irow = inds + row * g.k * 3;
   const float sscale = (g.dist == SNLS_DIST_PROD ? 1.f : -1.f) * scale;
-  float m, z;
-  softmax_stats(drow, g.k, sscale, lane, &m, &z);
+  float z;
+  const RowSoftmax term = row_softmax(drow, g.k, sscale, lane, &z);
   const long long qbase = ((long long)rp.b * g.T + rp.t) * g.HW;  // pixel index base of the query frame
   for (int l = 0; l < g.k; ++l) {
     int t2, ny, nx;
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(256) backward_agg_kernel(const float* __restri
       if (lane == 0) Gws[row * g.k + l] = 0.f;
       continue;
     }
-    const float wl = expf(sscale * drow[l] - m) / z;
+    const float wl = term(drow[l]) / z;
     const long long fbase = ((long long)rp.b * g.T + t2) * g.HW;
     float Gl = 0.f, fh = 0.f, fw = 0.f;
     for (int c0 = 0; c0 < g.Ch; c0 += 64) {
@@ -348,12 +348,12 @@ __global__ void __launch_bounds__(256) backward_search_kernel(const float* __res
   const float* Grow = Gws + row * g.k;
   const float sign = g.dist == SNLS_DIST_PROD ? 1.f : -1.f;
   const float sscale = sign * scale;
-  float m, z;
-  softmax_stats(drow, g.k, sscale, lane, &m, &z);
+  float z;
+  const RowSoftmax term = row_softmax(drow, g.k, sscale, lane, &z);
   float wg = 0.f;
   if (z > 0.f)
     for (int l = lane; l < g.k; l += 64)
-      if (isfinite(drow[l])) wg += expf(sscale * drow[l] - m) / z * Grow[l];
+      if (isfinite(drow[l])) wg += term(drow[l]) / z * Grow[l];
   wg = wave_sum(wg);
   const long long qbase = ((long long)rp.b * g.T + rp.t) * g.HW;
   for (int l = 0; l < g.k; ++l) {
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(256) backward_search_kernel(const float* __res
     const bool fin = isfinite(drow[l]), ok = fin && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
     // (a finite score at a bad position still scales the other weights: G_l = 0, but dd_l is not)
     float dd = 0.f;
-    if (fin && z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
+    if (fin && z > 0.f) dd = sscale * (term(drow[l]) / z) * (Grow[l] - wg);
     if (ok && grad_dists) dd += grad_dists[row * g.k + l];
     if (dd_out && lane == 0) dd_out[row * g.k + l] = dd;
     if (!ok || dd == 0.f) continue;
@@ -467,8 +467,8 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
   const float* drow = dists + row * g.k;
   const float* irow = inds + row * g.k * 3;
   const float sscale = (g.dist == SNLS_DIST_PROD ? 1.f : -1.f) * scale;
-  float m, z;
-  softmax_stats(drow, g.k, sscale, lane, &m, &z);
+  float z;
+  const RowSoftmax term = row_softmax(drow, g.k, sscale, lane, &z);
   const bool act = cl < g.Ch;
   const unsigned ch4 = act ? (unsigned)(rp.hd * g.Ch + cl) * 4u : kOOB2;
   const int lo = -(P / 2);
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(256) backward_agg_block_kernel(const float* __
       wl_out[row * g.k + l] = 0.f;
     }
     if (NG == 1 ? !ok : !__any(ok)) continue;
-    const float wl = ok ? expf(sscale * drow[l] - m) / z : 0.f;
+    const float wl = ok ? term(drow[l]) / z : 0.f;
     const int Y0 = rp.h + lo + ny, X0 = rp.w + lo + nx;  // block origin
     // the block of V values (0 outside the frame)
     float vb[PB * PB];
@@ -571,12 +571,12 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
   const float* Grow = Gws + row * g.k;
   constexpr bool ip = IP;
   const float sscale = (ip ? 1.f : -1.f) * scale;
-  float m, z;
-  softmax_stats(drow, g.k, sscale, lane, &m, &z);
+  float z;
+  const RowSoftmax term = row_softmax(drow, g.k, sscale, lane, &z);
   float wg = 0.f;
   if (z > 0.f)
     for (int l = lane; l < g.k; l += 64)
-      if (isfinite(drow[l])) wg += expf(sscale * drow[l] - m) / z * Grow[l];
+      if (isfinite(drow[l])) wg += term(drow[l]) / z * Grow[l];
   wg = wave_sum(wg);
   const long long qbase = ((long long)rp.b * g.T + rp.t) * g.HW;
   const bool act = cl < g.Ch;
@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(256) backward_search_block_kernel(const float*
     float ay = 0.f, ax = 0.f;
     const bool fin = l < g.k && isfinite(drow[l]), ok = fin && neighbour(irow, l, g, &t2, &ny, &nx, &ay, &ax);
     float dd = 0.f;
-    if (fin && z > 0.f) dd = sscale * (expf(sscale * drow[l] - m) / z) * (Grow[l] - wg);
+    if (fin && z > 0.f) dd = sscale * (term(drow[l]) / z) * (Grow[l] - wg);
     if (ok && grad_dists) dd += grad_dists[row * g.k + l];
     if (last && l < g.k) dd_out[row * g.k + l] = dd;
     if (!ok) dd = 0.f;  // nothing is read at a bad position (its score still scales the other weights)

@@ -187,6 +187,20 @@ SNLS_DEV int flow_slot(int dt, int wt) { return dt < 0 ? dt + wt : dt + wt - 1; 
 SNLS_DEV float to_score(float d, int dist) { return dist == SNLS_DIST_PROD ? d : -d; }
 SNLS_DEV float from_score(float s, int dist) { return dist == SNLS_DIST_PROD ? s : -s; }
 
+// Softmax of a row of finite scores d at the signed scale s: a weight is
+// exp(s * d - m) over the row's sum, m = s * best, best the score of the largest
+// key.  Where s * best leaves fp32 (scores masked with the type's lowest
+// value, a scale above 1) the scores' difference is taken first: it is all
+// that counts.
+SNLS_DEV float softmax_key(float s, float d) { return s < 0.f ? -d : d; }
+struct RowSoftmax {
+  float s, best, m;
+  SNLS_DEV RowSoftmax(float s_, float top_key) : s(s_), best(softmax_key(s_, top_key)), m(s_ * best) {}
+  SNLS_DEV float operator()(float d) const {
+    return expf(fabsf(m) < INFINITY ? fmaf(s, d, -m) : s * (d - best));
+  }
+};
+
 // (s1, id1) ranks before (s2, id2): larger score, ties to the smaller id.
 SNLS_DEV bool ranks_before(float s1, int id1, float s2, int id2) { return s1 > s2 || (s1 == s2 && id1 < id2); }
 
