@@ -436,9 +436,14 @@ snls_status snls_cache_store(const float* k, const float* v, const int32_t* slot
  *   ws       window side, 1 .. 15 (SNLS_ERR_UNSUPPORTED above)
  *   scale    finite
  *   out      device out, (B, C, H, W), fully overwritten
- * Logits may be held in base 2, so a sum of q.k~ and the table entry whose
- * logit's magnitude passes 2.3e38 may count as not finite; a table entry alone
- * does not (a mask of the type's lowest value is a finite logit).
+ * Queries, keys and scale may lie anywhere in fp32 as long as the logits do
+ * not leave it: where scale * (q.k~ of a whole-pixel tap), or its sum with the
+ * table's, passes 1.1e38 in magnitude, a logit may count as not finite; scale *
+ * table entry alone does not (a mask of the type's lowest value is a finite
+ * logit), but is held as 2.3e38 at most.  Sums of weights times values are fp32
+ * before the division: a value times the number of candidates stays below
+ * 8e34.  Whole frames of heads of 17 to 128 channels may take their scores from
+ * queries held in 22 bits, and down to 2^-38 of a query's largest channel.
  * The result does not depend on scheduling.  Errors: SNLS_ERR_INVALID_ARG,
  * SNLS_ERR_UNSUPPORTED (limits of the cache and of the bias), SNLS_ERR_HIP. */
 snls_status snls_cache_attend(const float* q, const float* flows, const int32_t* ages, const void* k_codes,

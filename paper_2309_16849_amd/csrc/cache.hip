@@ -142,9 +142,25 @@ struct AttendArgs {
   CacheGeo c;
   Bias bias;
   int ws;
-  float scale;
+  float scale;  // of the table
+  float sm;     // scale = sm * 2^se, |sm| in [0.5, 1) or 0
+  int se;
   float* out;
 };
+
+// The range of scores.  A query's channels are brought to 2^kQTop by a power of
+// two of the query's own, and that, the scale's and the block scale's meet in
+// one factor per tap: neither scale * q nor q * code, nor a sum of these, leaves
+// fp32 where the logit does not (channels below 2^-91 of a query's largest
+// against keys of 2^100 aside).  Queries as they are, times the scale, lost
+// logits of ordinary size for queries from 1e33 on.
+constexpr int kQTop = 100;  // 256 products with codes of up to 448 stay below 2^118
+SNLS_DEV int exponent(float most) { return __builtin_amdgcn_frexp_expf(most) - 1; }  // most in [2^e, 2^(e+1)), or 0
+SNLS_DEV float key_factor(float scale, int e) { return fminf(ldexpf(scale, e), 3.402823466e38f); }
+SNLS_DEV float finite_top(float most, float x) {
+  const float t = fabsf(x);
+  return t < INFINITY ? fmaxf(most, t) : most;
+}
 
 // s plus the dot product of 16 codes with q; spread16: acc[i] += wgt * code i.
 SNLS_DEV float dot16(uint4 t, const float* q, float s) {
@@ -205,14 +221,20 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
   const bool inb = b >= 0 && b < c.B && h >= 0 && h < c.H && w >= 0 && w < c.W;
   const int vec = lane & (G - 1), tok = lane / G;
   const bool vlive = vec < c.nv;
-  float q[16], acc[16];
+  float q[16], acc[16], most = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int ch = vec * 16 + i;
     q[i] = 0.f;
     acc[i] = 0.f;
     if (inb && ch < c.Ch) q[i] = a.q[qi * c.C + hd * c.Ch + ch];
+    most = finite_top(most, q[i]);
   }
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+  const int up = kQTop - exponent(most);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) q[i] = ldexpf(q[i], up) * a.sm;
   for (int i = lane; i < (ws + 2) * (ws + 2); i += 64) cells[i] = 0.f;
   float m = -INFINITY, z = 0.f;  // running maximum (of the wave) and this lane's sum
   if (inb)
@@ -243,7 +265,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
         float d = 0.f;
         if (in && vlive) {
           d = dot16(*reinterpret_cast<const uint4*>(kp + (unsigned)((y * c.W + x) * c.Cp + vec * 16)), q, 0.f);
-          d *= ksp[(y >> c.sh) * c.nbx + (x >> c.sh)];
+          d *= key_factor(ksp[(y >> c.sh) * c.nbx + (x >> c.sh)], a.se - up);
         }
 #pragma unroll
         for (int o = 1; o < G; o <<= 1) d += __shfl_xor(d, o);
@@ -267,9 +289,8 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
             if (a.table) {
               const int at = (bt * a.bias.nb + bias_bucket(Fh + (float)(dh - r), a.bias)) * a.bias.nb +
                              bias_bucket(Fw + (float)(dw - r), a.bias);
-              sc += a.table[(long long)hd * a.bias.buckets + at];
+              sc += a.scale * a.table[(long long)hd * a.bias.buckets + at];
             }
-            sc *= a.scale;
             if (isfinite(sc)) lg[k] = sc;
           }
         }
@@ -372,7 +393,8 @@ static void run_attend_wave(const AttendArgs& a, hipStream_t s) {
 // but two rows is kept.
 //
 // Logits are held in base 2 (q and the table are multiplied by scale * log2 e
-// as they are read).  The maximum follows the logits only in steps of more
+// as they are read: one rounding more per channel and entry, in place of one
+// per cell, and the hardware's base-2 exponential, 1 ulp, in place of expf).  The maximum follows the logits only in steps of more
 // than kSlack, so that the outputs are rescaled once or twice per frame, not
 // per row: weights are then at most 2^kSlack, far from fp32's limits.
 constexpr float kLog2e = 1.44269504088896341f;
@@ -512,9 +534,25 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
       acc[v][i] = 0.f;
       if constexpr (!MX) q[v][i] = 0.f;
       if (!MX && live && ch < c.Ch)
-        q[MX ? 0 : v][i] = (a.scale * kLog2e) * (POINTS ? a.q[qi * c.C + hd * c.Ch + ch]
-                                               : a.q[((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w]);
+        q[MX ? 0 : v][i] = POINTS ? a.q[qi * c.C + hd * c.Ch + ch]
+                                  : a.q[((long long)b * c.C + hd * c.Ch + ch) * HW + (long long)h * c.W + w];
     }
+  }
+  int qexp = 0;  // undoes the query's power of two, and holds the scale's
+  if constexpr (!MX) {
+    float most = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = finite_top(most, q[v][i]);
+    most = fmaxf(most, quad<1, 0, 3, 2>(most));
+    most = fmaxf(most, quad<2, 3, 0, 1>(most));
+    const int up = kQTop - exponent(most);
+    qexp = a.se - up;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) q[v][i] = ldexpf(q[v][i], up) * (a.sm * kLog2e);
   }
   const int lane0 = min(lr, c.nv - 1) * 16, rowbytes = c.W * c.Cp;
   // Matrix-core operand of query lane % 16: lanes of group lane / 16 hold the
@@ -523,7 +561,6 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
   constexpr bool kPack = R * V == 2;
   constexpr int J = (R * V + 3) / 4;
   half8_t qh[MX ? J : 1][2], ql[MX && !kPack ? J : 1][2];
-  float qback = 0.f;  // undoes the query's power of two
   const int n16 = lane & 15, g4 = lane >> 4;
   float* const stab = tab + max(a.bias.buckets, 1) + wv * 16 * kBoxQuery<CT>;
   if constexpr (MX) {
@@ -536,21 +573,22 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int ch = (kPack ? (g4 & 1) : 4 * jj + g4) * 16 + i;
-        x[jj][i] = inq && ch < c.Ch ? (a.scale * kLog2e) * qp[ch * HW] : 0.f;
-        const float t = fabsf(x[jj][i]);
-        most = t < INFINITY ? fmaxf(most, t) : most;
+        x[jj][i] = inq && ch < c.Ch ? qp[ch * HW] : 0.f;
+        most = finite_top(most, x[jj][i]);
       }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    // the largest channel to 2^14 .. 2^15, just below fp16's end: channels 2^-15 of it still have all of both parts
-    const int e = max((int)(__float_as_uint(most) >> 23) - 127, -110) - 14;
-    const float up = __uint_as_float((unsigned)(127 - e) << 23);
-    qback = __uint_as_float((unsigned)(127 + e) << 23);
+    // the largest channel to 2^14 .. 2^15, times 0.72 .. 1.45 just below fp16's end: channels 2^-14 of it still have all
+    // of both parts
+    const int up = 14 - exponent(most);
+    qexp = a.se - up;
 #pragma unroll
     for (int jj = 0; jj < J; ++jj)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float t = x[jj][i] * up;
+        float t = ldexpf(x[jj][i], up) * (a.sm * kLog2e);
+        // one number for both parts: folded into the conversion the product may round to another hi than lo is the rest of
+        asm volatile("" : "+v"(t));
         const _Float16 hi = (_Float16)t, lo = (_Float16)(t - (float)hi);
         if constexpr (kPack) {
           qh[jj][i / 8][i % 8] = g4 < 2 ? hi : lo;
@@ -667,8 +705,11 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
             for (int u = 0; u < 2; ++u)
               if ((unsigned)f.dy[u] <= (unsigned)ws && (unsigned)f.dx[u] < (unsigned)(ws + 4)) {
                 float* to = sq + f.dy[u] * kBoxPitch<CT> + f.dx[u];
+                // (the powers of two in one step: the product with either alone may leave fp32)
+                const float bm = __builtin_amdgcn_frexp_mantf(f.back[u]);
+                const int be = __builtin_amdgcn_frexp_expf(f.back[u]) + qexp;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) to[i] = (d[u][i] + e[u][i]) * f.back[u] * qback;
+                for (int i = 0; i < 4; ++i) to[i] = ldexpf((d[u][i] + e[u][i]) * bm, be);
               }
           }
         return true;
@@ -704,7 +745,7 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
         const unsigned at = (unsigned)(min(max(yb0 + i, 0), c.nby - 1) * c.nbx + xb);
-        ksc[i][k] = ksp[at];
+        ksc[i][k] = key_factor(ksp[at], qexp);
         vsc[i][k] = vsp[at];
       }
       cb[k] = bt + bias_bucket(Fw + (float)(col - r), a.bias);
@@ -976,7 +1017,9 @@ snls_status launch_cache_attend(const float* q, const int32_t* points, long long
                                 const int32_t* ages, const uint8_t* k_codes, const float* k_scales,
                                 const uint8_t* v_codes, const float* v_scales, const float* table,
                                 const CacheGeo& c, const Bias& bias, int ws, float scale, float* out, hipStream_t s) {
-  const AttendArgs a{q, points, n, flows, ages, k_codes, k_scales, v_codes, v_scales, table, c, bias, ws, scale, out};
+  int se = 0;
+  const float sm = frexpf(scale, &se);
+  const AttendArgs a{q, points, n, flows, ages, k_codes, k_scales, v_codes, v_scales, table, c, bias, ws, scale, sm, se, out};
   // few points: 4, 8 or 16 waves each, which share its slots, for the shortest way through one query.  4 waves / quads
   // (6 slots, ws = 9): one head of 64 channels 30 / 51 us for 1,024 points, 56 / 52 us for 2,048; 4 heads of 16
   // channels 29 / 32 us for 512, 51 / 33 us for 1,024.  4 / 16 waves (16 slots): 12 heads 20.0 / 17.3 us for 16

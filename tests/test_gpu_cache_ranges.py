@@ -1,0 +1,154 @@
+"""Attention over cached frames with queries, keys and scales near the ends
+of fp32's range whose logits are ordinary: none of them is lost on the way.
+Every form of the operator: lists of few points, long lists, whole frames on
+the vector units (16, 160 and 256 channels) and on the matrix cores (32 to 128).
+"""
+import pytest
+import torch
+
+from paper_2309_16849_amd import snls as B
+from tests import attention64 as R
+from tests.test_gpu_frame_cache import _both, _cp
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load_library()
+    return torch.device("cuda:0")
+
+
+def _bound(vv, biggest):
+    """Several deviations of what roundings do (test_gpu_query_bits.py): a logit L is off by about 2^-22 L."""
+    return 1e-5 * float(vv.abs().max()) * max(biggest / 16, 1)
+
+
+def _run(dev, cp, ws, q, fl, cache, scale, g, table=None, bias=None, kv=None, vv=None):
+    """All three forms against 64 bits; returns the reference."""
+    kv = R.decoded(cache[0], cache[1].cpu(), cp) if kv is None else kv
+    vv = R.decoded(cache[2], cache[3].cpu(), cp) if vv is None else vv
+    ages = torch.zeros(1, cp["slots"], dtype=torch.int32)
+    a, b, qa, allp, fa = _both(dev, cp, ws, q, fl, ages, cache, scale, table, bias)
+    pick = torch.randint(0, qa.shape[0], (24,), generator=g)
+    to = lambda x: None if x is None else x.to(dev)  # noqa: E731
+    few = B.snls_cache_attend_points(to(qa[pick]), to(allp[pick]), to(fa[pick]), to(ages), cache, cp, ws, scale,
+                                     table=to(table), bias=bias).cpu()
+    ref, big = R.attend(qa[pick], allp[pick], fa[pick], ages, kv, vv, cp, ws, scale, table, bias)
+    assert bool((ref != 0).any(1).all())
+    tol = _bound(vv, big)
+    for o, what in ((a[pick], "frame"), (b[pick], "list"), (few, "few")):
+        err = float((o.double() - ref).abs().max())
+        print(what, "err %.2e tol %.2e" % (err, tol), flush=True)
+        assert err <= tol, what
+    return ref
+
+
+CHANNELS = [16, 32, 64, 128, 160, 256]
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+@pytest.mark.parametrize("size", [1e-37, 1e-34, 1e-32, 1e-30, 1e33, 1e35, 1e37])
+def test_query_against_key_sizes(dev, C, size):
+    """Queries of one end of the range against keys of the other."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=2)
+    g = torch.Generator().manual_seed(51)
+    cache = B.cache_alloc(cp, dev)
+    for s in range(2):
+        k, v = (torch.randn(1, C, 48, 47, generator=g) for _ in range(2))
+        B.snls_cache_store((k / size).to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
+    q = size * torch.randn(1, C, 48, 47, generator=g)
+    fl = torch.randn(1, 2, 2, 48, 47, generator=g)
+    _run(dev, cp, 5, q, fl, cache, C ** -0.5, g)
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+@pytest.mark.parametrize("qs,ks,scale", [(1e20, 1e10, 1e-30), (1e-20, 1e-12, 1e32), (1e38, 1.0, 1e-38), (1.0, 1e-37, 3e36),
+                                         (1e30, 1e30, 1e-38), (1e-25, 1e-10, 3e34)], ids=str)
+def test_scale_takes_part(dev, C, qs, ks, scale):
+    """The scale far from 1: neither scale * q nor q . k need be in fp32's range where the logit is (1e30 * 1e30 * 1e-38
+    gives logits of 1e22: one candidate takes all)."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=2)
+    g = torch.Generator().manual_seed(52)
+    cache = B.cache_alloc(cp, dev)
+    for s in range(2):
+        k, v = (torch.randn(1, C, 48, 47, generator=g) for _ in range(2))
+        B.snls_cache_store((ks * k).to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
+    q = qs * torch.randn(1, C, 48, 47, generator=g).clamp(-3, 3)
+    # whole pixels: candidates of logits that large are told apart by the products alone
+    fl = torch.randn(1, 2, 2, 48, 47, generator=g).round()
+    big = qs * ks * scale
+    _run(dev, cp, 5, q, fl, cache, scale, g) if big < 1e10 else _one_takes_all(dev, cp, 5, q, fl, cache, scale, g)
+
+
+def _one_takes_all(dev, cp, ws, q, fl, cache, scale, g):
+    kv, vv = R.decoded(cache[0], cache[1].cpu(), cp), R.decoded(cache[2], cache[3].cpu(), cp)
+    ages = torch.zeros(1, 2, dtype=torch.int32)
+    a, b, qa, allp, fa = _both(dev, cp, ws, q, fl, ages, cache, scale)
+    pick = torch.randint(0, qa.shape[0], (24,), generator=g)
+    ref, _ = R.attend(qa[pick], allp[pick], fa[pick], ages, kv, vv, cp, ws, scale)
+    for o in (a[pick], b[pick]):
+        # the winner's value exactly (weight 1), but where two products agree to fp32's rounding
+        same = ((o.double() - ref).abs() <= 4 * 2.0 ** -24 * ref.abs()).all(1)
+        assert int(same.sum()) >= 23, int(same.sum())
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+def test_largest_keys(dev, C):
+    """Keys of +-448 * 2^100 against queries of 2^-100: logits of 448 C, and -448 C in every second column."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=1)
+    g = torch.Generator().manual_seed(53)
+    cache = B.cache_alloc(cp, dev)
+    k = 448.0 * 2.0 ** 100 * torch.ones(1, C, 48, 47)
+    k[..., 1::2] *= -1  # columns of either sign
+    v = torch.randn(1, C, 48, 47, generator=g)
+    B.snls_cache_store(k.to(dev), v.to(dev), torch.zeros(1, dtype=torch.int32, device=dev), cp, cache)
+    q = 2.0 ** -100 * torch.ones(1, C, 48, 47)
+    # the largest logit is exact (but for the roundings of one common factor, log2 e): weights of 1 / 10 to 1 / 15 each
+    a, b, qa, allp, _ = _both(dev, cp, 5, q, None, torch.zeros(1, 1, dtype=torch.int32), cache, 1.0)
+    vv = R.decoded(cache[2], cache[3].cpu(), cp)[0, 0, 0]
+    for o in (a.view(48, 47, C), b.view(48, 47, C)):
+        for h, w in ((0, 0), (0, 1), (20, 21), (20, 22), (47, 46), (30, 0)):
+            win = vv[max(h - 2, 0):h + 3, max(w - 2, 0):w + 3]
+            cols = torch.arange(max(w - 2, 0), min(w + 3, 47)) % 2 == 0
+            want = win[:, cols].reshape(-1, C).mean(0)
+            assert float((o[h, w].double() - want).abs().max()) <= 1e-5 * float(vv.abs().max())
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+def test_large_channel_against_zero(dev, C):
+    """Queries with up to 1e38 in a channel where the keys hold 0, and ordinary ones elsewhere, which make the logits.  The
+    vector units' forms hold them all; the matrix cores' hold a query's channels down to 2^-38 of its largest."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=1)
+    g = torch.Generator().manual_seed(54)
+    cache = B.cache_alloc(cp, dev)
+    k, v, q = (torch.randn(1, C, 48, 47, generator=g) for _ in range(3))
+    k[:, 0], q[:, 0] = 0.0, 1e37 * q[:, 0]
+    B.snls_cache_store(k.to(dev), v.to(dev), torch.zeros(1, dtype=torch.int32, device=dev), cp, cache)
+    kv, vv = R.decoded(cache[0], cache[1].cpu(), cp), R.decoded(cache[2], cache[3].cpu(), cp)
+    ages = torch.zeros(1, 1, dtype=torch.int32)
+    a, b, qa, allp, fa = _both(dev, cp, 5, q, None, ages, cache, 0.25)
+    pick = torch.randint(0, qa.shape[0], (24,), generator=g)
+    few = B.snls_cache_attend_points(qa[pick].to(dev), allp[pick].to(dev), None, ages.to(dev), cache, cp, 5, 0.25).cpu()
+    ref, big = R.attend(qa[pick], allp[pick], None, ages, kv, vv, cp, 5, 0.25)
+    tol = _bound(vv, big)
+    assert bool(a.isfinite().all()) and bool((a != 0).any(1).all())
+    for o in (b[pick], few) + ((a[pick],) if C in (16, 160, 256) else ()):
+        assert float((o.double() - ref).abs().max()) <= tol
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+def test_table_beside_extreme_sizes(dev, C):
+    """The table's entries are logits of their own beside products of extreme factors."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=2)
+    g = torch.Generator().manual_seed(55)
+    bias = dict(radius=0, edges=[1.0, 2.0])
+    table = torch.randn(B.bias_table_shape(bias, 1), generator=g)
+    cache = B.cache_alloc(cp, dev)
+    for s in range(2):
+        k, v = (torch.randn(1, C, 48, 47, generator=g) for _ in range(2))
+        B.snls_cache_store((1e-34 * k).to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
+    q = 1e34 * torch.randn(1, C, 48, 47, generator=g)
+    _run(dev, cp, 5, q, torch.randn(1, 2, 2, 48, 47, generator=g), cache, 2.0 * C ** -0.5, g, table, bias)
