@@ -361,7 +361,8 @@ snls_status snls_bias(const float* dists, const float* inds, const float* table,
  *   workspace    device scratch of at least
  *                snls_workspace_size(SNLS_OP_BIAS_BACKWARD, p) bytes, 256-byte
  *                aligned
- * The result does not depend on scheduling: it is bit-identical between runs.
+ * Sums are held in 64 bits and rounded once.  The result does not depend on
+ * scheduling: it is bit-identical between runs.
  * Errors: as snls_bias; SNLS_ERR_UNSUPPORTED for 2^16 heads or more;
  * SNLS_ERR_WORKSPACE. */
 snls_status snls_bias_backward(const float* grad_scores, const float* dists, const float* inds, const snls_params* p,

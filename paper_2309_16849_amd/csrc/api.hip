@@ -250,7 +250,7 @@ snls_status snls_bias_backward(const float* grad_scores, const float* dists, con
   if (!workspace || workspace_bytes < bias_backward_ws_bytes(g) || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return SNLS_ERR_WORKSPACE;
   if ((st = device_ready()) != SNLS_OK) return st;
-  return launch_bias_backward(grad_scores, dists, inds, g, b, grad_table, static_cast<float*>(workspace),
+  return launch_bias_backward(grad_scores, dists, inds, g, b, grad_table, static_cast<double*>(workspace),
                               as_stream(stream));
 }
 

@@ -106,12 +106,21 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* dists, const flo
 // take 180 cycles an instruction on this chip, fp64 10 to 13, a read and a
 // write 25), `cols` copies of every entry so that fewer lanes meet.  No other
 // wave touches the table, so every entry's additions happen in one order.
-__global__ void __launch_bounds__(64) bias_grad_kernel(const float* __restrict__ grad, const float* __restrict__ dists,
-                                                       const float* __restrict__ inds, BiasRows r, Bias b, float sign,
-                                                       int cols, int slices, float* __restrict__ part) {
-  extern __shared__ double acc[];
-  const int lane = threadIdx.x;
-  const int hd = blockIdx.x / slices, slice = blockIdx.x % slices;
+// NW waves a workgroup join their tables in LDS, in order, and write one: its
+// sums stay in 64 bits to the end, twice the bytes of fp32 ones, which lost
+// the last places where the slices cancel and all of a sum whose slices pass
+// fp32's range (31 million gradients into 4 tables of 1,183: 149 us a call,
+// 157 with a 64-bit table per wave, 150 with an fp32 one).
+template <int NW>
+__global__ void __launch_bounds__(64 * NW) bias_grad_kernel(const float* __restrict__ grad,
+                                                            const float* __restrict__ dists,
+                                                            const float* __restrict__ inds, BiasRows r, Bias b,
+                                                            float sign, int cols, int groups,
+                                                            double* __restrict__ part) {
+  extern __shared__ double tables[];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int hd = blockIdx.x / groups, slices = groups * NW, slice = (int)(blockIdx.x % groups) * NW + wv;
+  double* const acc = tables + wv * b.buckets * cols;
   for (int i = lane; i < b.buckets * cols; i += 64) acc[i] = 0.0;
   wave_lds_sync();
   const long long total = (long long)r.B * r.T * r.chunks;  // of this head
@@ -134,25 +143,27 @@ __global__ void __launch_bounds__(64) bias_grad_kernel(const float* __restrict__
       }
     }
   }
-  wave_lds_sync();
-  for (int i = lane; i < b.buckets; i += 64) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < b.buckets; i += 64 * NW) {
     double s = 0.0;
-    for (int k = 0; k < cols; ++k) s += acc[i * cols + k];
-    part[(long long)blockIdx.x * b.buckets + i] = (float)s;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+      for (int k = 0; k < cols; ++k) s += tables[(w * b.buckets + i) * cols + k];
+    part[(long long)blockIdx.x * b.buckets + i] = s;
   }
 }
 
-// grad_table[hd][i] = sum of the head's slices, in 64 bits: `ent` entries (a
-// power of two up to 64) of a head a workgroup, its 1024 / ent groups of lanes
-// take the slices in turn.
-__global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const float* __restrict__ part, int buckets, int slices,
+// grad_table[hd][i] = sum of the head's `slices` tables, in 64 bits: `ent`
+// entries (a power of two up to 64) of a head a workgroup, its 1024 / ent
+// groups of lanes take the tables in turn.
+__global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const double* __restrict__ part, int buckets, int slices,
                                                              int ent, float* __restrict__ grad_table) {
   __shared__ double sums[1024];
   const int lane = threadIdx.x & (ent - 1), group = threadIdx.x / ent, groups = 1024 / ent;
   const int per = (buckets + ent - 1) / ent, hd = blockIdx.x / per, i = (int)(blockIdx.x % per) * ent + lane;
   double s = 0.0;
   if (i < buckets) {
-    const float* p = part + (long long)hd * slices * buckets + i;
+    const double* p = part + (long long)hd * slices * buckets + i;
 #pragma unroll 8
     for (int k = group; k < slices; k += groups) s += p[(long long)k * buckets];
   }
@@ -168,7 +179,8 @@ __global__ void __launch_bounds__(1024) bias_grad_sum_kernel(const float* __rest
 // Slices of a head: as many waves as lie on the chip at once with their tables
 // (16 a CU up to 1,280 entries: 31 million gradients into 4 tables of 1,183
 // took 215 us with 8 a CU, 142 with 16, 178 with 24, which do not fit), and
-// four chunks a slice at least.
+// four chunks a slice at least.  Where 16 tables fit, four waves share a
+// workgroup; larger ones keep a workgroup each, whose launches fill LDS.
 constexpr int kCUs = 256, kLds = 160 * 1024, kMostWaves = 16;
 
 static long long bias_slices(const Geo& g, int buckets) {
@@ -184,7 +196,7 @@ size_t bias_backward_ws_bytes(const Geo& g) {
   const size_t heads = (size_t)g.HD * SNLS_BIAS_MAX_BUCKETS, full = (size_t)kCUs * (kLds / sizeof(double));
   const size_t few = heads * bias_slices(g, 1);
   const size_t most = heads > full ? heads : full;
-  return (few < most ? few : most) * sizeof(float);
+  return (few < most ? few : most) * sizeof(double);
 }
 
 snls_status launch_bias(const float* dists, const float* inds, const float* table, const Geo& g, const Bias& bias,
@@ -202,18 +214,25 @@ snls_status launch_bias(const float* dists, const float* inds, const float* tabl
 }
 
 snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
-                                 const Bias& bias, float* grad_table, float* ws, hipStream_t s) {
-  const int slices = (int)bias_slices(g, bias.buckets);
+                                 const Bias& bias, float* grad_table, double* ws, hipStream_t s) {
+  const bool four = bias.buckets * (int)sizeof(double) <= kLds / kMostWaves;
+  const int slices = (int)bias_slices(g, bias.buckets), groups = four ? (slices + 3) / 4 : slices;
   // entries a workgroup of the second kernel: few while the table is small and
-  // workgroups short (a whole call with 16 / 64: 2 tables of 75 21.0 / 22.4 us,
-  // 4 of 1,183 141 / 138)
+  // workgroups short (a whole call with 16 / 64, a table a wave: 2 tables of 75
+  // 21.0 / 22.4 us, 4 of 1,183 141 / 138)
   const int ent = bias.buckets <= 256 ? 16 : 64, sums = (bias.buckets + ent - 1) / ent * g.HD;  // at most 64 a head
   int cols = 8;  // as many copies as leave room for all the waves
   while (cols > 1 && bias.buckets * cols * (int)sizeof(double) > kLds / kMostWaves) cols /= 2;
-  hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)(g.HD * slices)), dim3(64),
-                     (size_t)bias.buckets * cols * sizeof(double), s, grad, dists, inds, bias_rows(g), bias,
-                     g.dist == SNLS_DIST_PROD ? 1.f : -1.f, cols, slices, ws);
-  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)sums), dim3(1024), 0, s, ws, bias.buckets, slices, ent,
+  const size_t lds = (size_t)bias.buckets * cols * sizeof(double);
+  const float sign = g.dist == SNLS_DIST_PROD ? 1.f : -1.f;
+  const dim3 grid((unsigned)(g.HD * groups));
+  if (four)
+    hipLaunchKernelGGL(bias_grad_kernel<4>, grid, dim3(256), 4 * lds, s, grad, dists, inds, bias_rows(g), bias, sign,
+                       cols, groups, ws);
+  else
+    hipLaunchKernelGGL(bias_grad_kernel<1>, grid, dim3(64), lds, s, grad, dists, inds, bias_rows(g), bias, sign, cols,
+                       groups, ws);
+  hipLaunchKernelGGL(bias_grad_sum_kernel, dim3((unsigned)sums), dim3(1024), 0, s, ws, bias.buckets, groups, ent,
                      grad_table);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }

@@ -154,7 +154,7 @@ snls_status launch_backward(const float* q, const float* k, const float* v, cons
 snls_status launch_bias(const float* dists, const float* inds, const float* table, const Geo& g, const Bias& bias,
                         float* out, hipStream_t s);
 snls_status launch_bias_backward(const float* grad, const float* dists, const float* inds, const Geo& g,
-                                 const Bias& bias, float* grad_table, float* ws, hipStream_t s);
+                                 const Bias& bias, float* grad_table, double* ws, hipStream_t s);
 snls_status launch_cache_store(const float* k, const float* v, const int32_t* slots, const CacheGeo& c,
                                uint8_t* k_codes, float* k_scales, uint8_t* v_codes, float* v_scales, hipStream_t s);
 // points == nullptr: every pixel of a frame (q and out (B, C, H, W), flows
