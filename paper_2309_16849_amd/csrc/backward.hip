@@ -54,33 +54,20 @@ SNLS_DEV float wave_sum(float v) {
   return v;
 }
 
-// Sum over the wave through DPP adds (rows of 16, then the row broadcasts of
-// lanes 15 and 31): no LDS crossbar.  The result is wave-uniform.
-SNLS_DEV float wave_sum_dpp(float v) {
-#define SNLS_DPP_ADD(CTRL, MASK) \
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, MASK, 0xf, false))
-  SNLS_DPP_ADD(0x111, 0xf);  // row_shr:1
-  SNLS_DPP_ADD(0x112, 0xf);  // row_shr:2
-  SNLS_DPP_ADD(0x114, 0xf);  // row_shr:4
-  SNLS_DPP_ADD(0x118, 0xf);  // row_shr:8: lane 15 of a row holds its sum
-  SNLS_DPP_ADD(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
-  SNLS_DPP_ADD(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
-#undef SNLS_DPP_ADD
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
-// Sum over groups of LW lanes (16, 32 or 64), in the last lane of each.
+// Sum over groups of LW lanes (16, 32 or 64), in the last lane of each, through
+// DPP adds (rows of 16, then the row broadcasts of lanes 15 and 31): no LDS
+// crossbar.
 template <int LW>
 SNLS_DEV float group_sum_dpp(float v) {
   static_assert(LW == 16 || LW == 32 || LW == 64, "lanes per group");
 #define SNLS_DPP_ADD(CTRL, MASK) \
   v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, MASK, 0xf, false))
-  SNLS_DPP_ADD(0x111, 0xf);
-  SNLS_DPP_ADD(0x112, 0xf);
-  SNLS_DPP_ADD(0x114, 0xf);
-  SNLS_DPP_ADD(0x118, 0xf);
-  if constexpr (LW >= 32) SNLS_DPP_ADD(0x142, 0xa);
-  if constexpr (LW == 64) SNLS_DPP_ADD(0x143, 0xc);
+  SNLS_DPP_ADD(0x111, 0xf);                          // row_shr:1
+  SNLS_DPP_ADD(0x112, 0xf);                          // row_shr:2
+  SNLS_DPP_ADD(0x114, 0xf);                          // row_shr:4
+  SNLS_DPP_ADD(0x118, 0xf);                          // row_shr:8: lane 15 of a row holds its sum
+  if constexpr (LW >= 32) SNLS_DPP_ADD(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+  if constexpr (LW == 64) SNLS_DPP_ADD(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
 #undef SNLS_DPP_ADD
   return v;
 }
@@ -89,14 +76,6 @@ SNLS_DEV float wave_max(float v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
   return v;
-}
-
-// p[off] when ok, else 0, with the load itself unconditional (address 0
-// when !ok, which the caller keeps valid), so that a run of such reads is
-// issued back to back instead of one per branch.
-SNLS_DEV float load_or_zero(const float* __restrict__ p, long long off, bool ok) {
-  const float v = p[ok ? off : 0];
-  return ok ? v : 0.f;
 }
 
 // Softmax of a row (lanes over the k entries) and its sum over the finite

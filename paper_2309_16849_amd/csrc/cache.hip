@@ -394,18 +394,17 @@ static void run_attend_wave(const AttendArgs& a, hipStream_t s) {
 //
 // Logits are held in base 2 (q and the table are multiplied by scale * log2 e
 // as they are read: one rounding more per channel and entry, in place of one
-// per cell, and the hardware's base-2 exponential, 1 ulp, in place of expf).  The maximum follows the logits only in steps of more
-// than kSlack, so that the outputs are rescaled once or twice per frame, not
-// per row: weights are then at most 2^kSlack, far from fp32's limits.
+// per cell, and the hardware's base-2 exponential, 1 ulp, in place of expf).
+// The maximum follows the logits only in steps of more than kSlack, so that the
+// outputs are rescaled once or twice per frame, not per row: weights are then at
+// most 2^kSlack, far from fp32's limits.
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kSlack = 12.f;
-// Loads of a tap row (K * R * V) up to which the values' are issued beside the
-// keys', a row's arithmetic ahead of their use: 4 heads of 16 channels at 256 x
-// 256 0.74 -> 0.70 ms, 64 channels at 480 x 854 1.53 -> 1.41 ms; above it the
-// registers would halve the waves.
-constexpr int kAhead = 12;
-// ... and up to which a row's loads stand together at all; wider heads issue
-// those of one column group (R * V) at a time (96 channels at 160 x 160 with 3
+// Loads of a tap row (K * R * V) up to which they stand together, the values'
+// beside the keys', a row's arithmetic ahead of their use (4 heads of 16
+// channels at 256 x 256 0.74 -> 0.70 ms, 64 channels at 480 x 854 1.53 -> 1.41
+// ms); more would take the registers of half the waves.  Wider heads issue the
+// loads of one column group (R * V) at a time (96 channels at 160 x 160 with 3
 // slots 308 -> 193 us), and above 128 channels two waves a SIMD are worth some
 // spilled registers (192 channels 440 -> 276 us).
 constexpr int kTogether = 12;
@@ -779,7 +778,7 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
       uint4 kb[MX ? 1 : kBuf], vb[kBuf];
       if constexpr (!MX && kRow)
         if (row <= ws) load_row(kp, yo, kb);
-      if constexpr (kRow && K * R * V <= kAhead) load_row(vp, yov, vb);
+      if constexpr (kRow) load_row(vp, yov, vb);
       float sc[K + 1];
 #pragma unroll
       for (int k = 0; k <= K; ++k) sc[k] = 0.f;
@@ -857,7 +856,6 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
             if (4 * k + (R == 1 ? 0 : n / V) < CT) pin(t[n]);
         };
         if constexpr (kRow) {
-          if constexpr (K * R * V > kAhead) load_row(vp, yov, vb);
 #pragma unroll
           for (int k = 0; k < K; ++k) pin_group(k, vb + k * R * V);
         }
