@@ -139,6 +139,13 @@ def _dev(t, name, shape=None):
     return t
 
 
+def _room(workspace):
+    """Address and bytes of a workspace, a contiguous tensor of any type on the GPU."""
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 # the current stream's handle without a Stream object around it (3 us a call)
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -200,7 +207,7 @@ def snls_search(q, k, flows, p: dict, dists=None, inds=None, workspace=None, str
         workspace = workspace_for(SNLS_OP_SEARCH, p, q.device)
     prm = params_from_dict(p)
     _check(lib.snls_search(_ptr(q), _ptr(k), _ptr(flows), ctypes.byref(prm), _ptr(dists), _ptr(inds),
-                           _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_search")
+                           *_room(workspace), _stream(stream)), "snls_search")
     return dists, inds
 
 
@@ -245,7 +252,7 @@ def snls_aggregate(v, dists, inds, p: dict, scale: float = 1.0, out=None, worksp
         workspace = workspace_for(SNLS_OP_AGGREGATE, p, v.device)
     prm = params_from_dict(p)
     _check(lib.snls_aggregate(_ptr(v), _ptr(dists), _ptr(inds), ctypes.byref(prm), float(scale), _ptr(out),
-                              _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_aggregate")
+                              *_room(workspace), _stream(stream)), "snls_aggregate")
     return out
 
 
@@ -286,7 +293,7 @@ def snls_backward(q, k, v, flows, dists, inds, grad_out, p: dict, scale: float =
     prm = params_from_dict(p)
     _check(lib.snls_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(flows), _ptr(dists), _ptr(inds), _ptr(grad_out),
                              _ptr(grad_dists), ctypes.byref(prm), float(scale), _ptr(gq), _ptr(gk), _ptr(gv),
-                             _ptr(gf), _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_backward")
+                             _ptr(gf), *_room(workspace), _stream(stream)), "snls_backward")
     return gq, gk, gv, gf
 
 
@@ -305,7 +312,7 @@ def snls_aggregate_stacked(v, dists, inds, p: dict, scale: float = 1.0, stacked=
         workspace = workspace_for(SNLS_OP_AGGREGATE_STACKED, p, v.device)
     prm = params_from_dict(p)
     _check(lib.snls_aggregate_stacked(_ptr(v), _ptr(dists), _ptr(inds), ctypes.byref(prm), float(scale),
-                                      _ptr(stacked), _ptr(workspace), workspace.numel() * 4, _stream(stream)),
+                                      _ptr(stacked), *_room(workspace), _stream(stream)),
            "snls_aggregate_stacked")
     return stacked
 
@@ -344,7 +351,7 @@ def snls_gather_stacked(v, weights, inds, p: dict, stacked=None, workspace=None,
         workspace = workspace_for(SNLS_OP_GATHER_STACKED, p, v.device)
     prm = params_from_dict(p)
     _check(lib.snls_gather_stacked(_ptr(v), _ptr(weights), _ptr(inds), ctypes.byref(prm), _ptr(stacked),
-                                   _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_gather_stacked")
+                                   *_room(workspace), _stream(stream)), "snls_gather_stacked")
     return stacked
 
 
@@ -383,7 +390,7 @@ def snls_gather_reduce(v, weights, inds, proj, p: dict, out=None, workspace=None
         workspace = workspace_for(SNLS_OP_GATHER_REDUCE, p, v.device)
     prm = params_from_dict(p)
     _check(lib.snls_gather_reduce(_ptr(v), _ptr(weights), _ptr(inds), _ptr(proj), ctypes.byref(prm), cout, _ptr(out),
-                                  _ptr(workspace), workspace.numel() * 4, _stream(stream)), "snls_gather_reduce")
+                                  *_room(workspace), _stream(stream)), "snls_gather_reduce")
     return out
 
 
@@ -442,7 +449,7 @@ def snls_bias_backward(grad_scores, dists, inds, p: dict, bias: dict, grad_table
     _here(grad_scores, dists, inds, grad_table, workspace)
     prm, bprm = params_from_dict(p), bias_from_dict(bias)
     _check(lib.snls_bias_backward(_ptr(grad_scores), _ptr(dists), _ptr(inds), ctypes.byref(prm), ctypes.byref(bprm),
-                                  _ptr(grad_table), _ptr(workspace), workspace.numel() * 4, _stream(stream)),
+                                  _ptr(grad_table), *_room(workspace), _stream(stream)),
            "snls_bias_backward")
     return grad_table
 
@@ -469,7 +476,7 @@ def snls_backward_scores(q, k, v, flows, dists, inds, grad_out, p: dict, scale: 
     prm = params_from_dict(p)
     _check(lib.snls_backward_scores(_ptr(q), _ptr(k), _ptr(v), _ptr(flows), _ptr(dists), _ptr(inds), _ptr(grad_out),
                                     _ptr(grad_dists), ctypes.byref(prm), float(scale), _ptr(gq), _ptr(gk), _ptr(gv),
-                                    _ptr(gf), _ptr(gs), _ptr(workspace), workspace.numel() * 4, _stream(stream)),
+                                    _ptr(gf), _ptr(gs), *_room(workspace), _stream(stream)),
            "snls_backward_scores")
     return gq, gk, gv, gf, gs
 
