@@ -19,6 +19,7 @@ returns.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -146,6 +147,14 @@ def _room(workspace):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+def _new(shape, like, stream):
+    """An output beside tensor like; a call on another stream than the current one keeps its memory until that is done."""
+    t = torch.empty(shape, device=like.device, dtype=torch.float32)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 # the current stream's handle without a Stream object around it (3 us a call)
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -198,13 +207,13 @@ def snls_search(q, k, flows, p: dict, dists=None, inds=None, workspace=None, str
         _dev(flows, "flows", flow_shape(p))
     shp = out_shape(p)
     if dists is None:
-        dists = torch.empty(shp, device=q.device, dtype=torch.float32)
+        dists = _new(shp, q, stream)
     if inds is None:
-        inds = torch.empty(shp + (3,), device=q.device, dtype=torch.float32)
+        inds = _new(shp + (3,), q, stream)
     _dev(dists, "dists", shp)
     _dev(inds, "inds", shp + (3,))
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_SEARCH, p, q.device)
+        workspace = workspace_for(SNLS_OP_SEARCH, p, q.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_search(_ptr(q), _ptr(k), _ptr(flows), ctypes.byref(prm), _ptr(dists), _ptr(inds),
                            *_room(workspace), _stream(stream)), "snls_search")
@@ -220,9 +229,9 @@ def snls_topk(dists_all, inds_all, k: int, dist_type: int, dists=None, inds=None
     _dev(inds_all, "inds_all", lead + (n_c, 3))
     rows = dists_all.numel() // max(n_c, 1)
     if dists is None:
-        dists = torch.empty(lead + (k,), device=dists_all.device, dtype=torch.float32)
+        dists = _new(lead + (k,), dists_all, stream)
     if inds is None:
-        inds = torch.empty(lead + (k, 3), device=dists_all.device, dtype=torch.float32)
+        inds = _new(lead + (k, 3), dists_all, stream)
     _dev(dists, "dists", lead + (k,))
     _dev(inds, "inds", lead + (k, 3))
     _check(lib.snls_topk(_ptr(dists_all), _ptr(inds_all), rows, n_c, k, dist_type, _ptr(dists), _ptr(inds),
@@ -230,12 +239,14 @@ def snls_topk(dists_all, inds_all, k: int, dist_type: int, dists=None, inds=None
     return dists, inds
 
 
-def workspace_for(op: int, p: dict, device):
-    """A device buffer of snls_workspace_size(op, p) bytes (torch allocations are 256-byte aligned)."""
+def workspace_for(op: int, p: dict, device, stream=None):
+    """A device buffer of snls_workspace_size(op, p) bytes (torch allocations are 256-byte aligned), for calls on
+    stream (default: the current one): its memory goes to other work of that stream only."""
     need = snls_workspace_size(op, p)
     if need == ctypes.c_size_t(-1).value:
         raise SnlsError(SNLS_ERR_INVALID_ARG, "snls_workspace_size")
-    return torch.empty(max((need + 3) // 4, 1), device=device, dtype=torch.float32)
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        return torch.empty(max((need + 3) // 4, 1), device=device, dtype=torch.float32)
 
 
 def snls_aggregate(v, dists, inds, p: dict, scale: float = 1.0, out=None, workspace=None, stream=None):
@@ -246,10 +257,10 @@ def snls_aggregate(v, dists, inds, p: dict, scale: float = 1.0, out=None, worksp
     _dev(dists, "dists", shp)
     _dev(inds, "inds", shp + (3,))
     if out is None:
-        out = torch.empty(video_shape(p), device=v.device, dtype=torch.float32)
+        out = _new(video_shape(p), v, stream)
     _dev(out, "out", video_shape(p))
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_AGGREGATE, p, v.device)
+        workspace = workspace_for(SNLS_OP_AGGREGATE, p, v.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_aggregate(_ptr(v), _ptr(dists), _ptr(inds), ctypes.byref(prm), float(scale), _ptr(out),
                               *_room(workspace), _stream(stream)), "snls_aggregate")
@@ -265,7 +276,7 @@ def snls_aggregate_static(v, dists, inds, p: dict, scale: float = 1.0, out=None,
     _dev(dists, "dists", shp)
     _dev(inds, "inds", shp + (3,))
     if out is None:
-        out = torch.empty(video_shape(p), device=v.device, dtype=torch.float32)
+        out = _new(video_shape(p), v, stream)
     _dev(out, "out", video_shape(p))
     prm = params_from_dict(p)
     _check(lib.snls_aggregate_static(_ptr(v), _ptr(dists), _ptr(inds), ctypes.byref(prm), float(scale), _ptr(out),
@@ -286,10 +297,10 @@ def snls_backward(q, k, v, flows, dists, inds, grad_out, p: dict, scale: float =
         _dev(grad_dists, "grad_dists", shp)
     if p["wt"] > 0 or flows is not None:
         _dev(flows, "flows", flow_shape(p))
-    gq, gk, gv = (torch.empty(vs, device=q.device, dtype=torch.float32) for _ in range(3))
-    gf = torch.empty(flow_shape(p), device=q.device, dtype=torch.float32)
+    gq, gk, gv = (_new(vs, q, stream) for _ in range(3))
+    gf = _new(flow_shape(p), q, stream)
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_BACKWARD, p, q.device)
+        workspace = workspace_for(SNLS_OP_BACKWARD, p, q.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(flows), _ptr(dists), _ptr(inds), _ptr(grad_out),
                              _ptr(grad_dists), ctypes.byref(prm), float(scale), _ptr(gq), _ptr(gk), _ptr(gv),
@@ -306,10 +317,10 @@ def snls_aggregate_stacked(v, dists, inds, p: dict, scale: float = 1.0, stacked=
     _dev(inds, "inds", shp + (3,))
     st_shape = (p["B"], p["HD"], p["k"], p["T"], p["C"] // p["HD"], p["H"], p["W"])
     if stacked is None:
-        stacked = torch.empty(st_shape, device=v.device, dtype=torch.float32)
+        stacked = _new(st_shape, v, stream)
     _dev(stacked, "stacked", st_shape)
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_AGGREGATE_STACKED, p, v.device)
+        workspace = workspace_for(SNLS_OP_AGGREGATE_STACKED, p, v.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_aggregate_stacked(_ptr(v), _ptr(dists), _ptr(inds), ctypes.byref(prm), float(scale),
                                       _ptr(stacked), *_room(workspace), _stream(stream)),
@@ -326,7 +337,7 @@ def snls_chain_flows(fflow, bflow, wt: int, flows=None, stream=None):
         raise ValueError("fflow must be (B, T, 2, H, W)")
     _dev(bflow, "bflow", tuple(fflow.shape))
     if flows is None:
-        flows = torch.empty((B, T, 2 * wt, 2, H, W), device=fflow.device, dtype=torch.float32)
+        flows = _new((B, T, 2 * wt, 2, H, W), fflow, stream)
     _dev(flows, "flows", (B, T, 2 * wt, 2, H, W))
     _check(lib.snls_chain_flows(_ptr(fflow), _ptr(bflow), B, T, H, W, int(wt), _ptr(flows), _stream(stream)),
            "snls_chain_flows")
@@ -345,10 +356,10 @@ def snls_gather_stacked(v, weights, inds, p: dict, stacked=None, workspace=None,
     _dev(weights, "weights", shp)
     _dev(inds, "inds", shp + (3,))
     if stacked is None:
-        stacked = torch.empty(stacked_shape(p), device=v.device, dtype=torch.float32)
+        stacked = _new(stacked_shape(p), v, stream)
     _dev(stacked, "stacked", stacked_shape(p))
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_GATHER_STACKED, p, v.device)
+        workspace = workspace_for(SNLS_OP_GATHER_STACKED, p, v.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_gather_stacked(_ptr(v), _ptr(weights), _ptr(inds), ctypes.byref(prm), _ptr(stacked),
                                    *_room(workspace), _stream(stream)), "snls_gather_stacked")
@@ -364,7 +375,7 @@ def snls_stacked_reduce(stacked, proj, p: dict, out=None, stream=None):
     if tuple(proj.shape) != (cout, p["C"], p["k"]):
         raise ValueError("proj must be (Cout, C, k)")
     if out is None:
-        out = torch.empty((p["B"], p["T"], cout, p["H"], p["W"]), device=stacked.device, dtype=torch.float32)
+        out = _new((p["B"], p["T"], cout, p["H"], p["W"]), stacked, stream)
     _dev(out, "out", (p["B"], p["T"], cout, p["H"], p["W"]))
     prm = params_from_dict(p)
     _check(lib.snls_stacked_reduce(_ptr(stacked), _ptr(proj), ctypes.byref(prm), cout, _ptr(out), _stream(stream)),
@@ -384,10 +395,10 @@ def snls_gather_reduce(v, weights, inds, proj, p: dict, out=None, workspace=None
     if tuple(proj.shape) != (cout, p["C"], p["k"]):
         raise ValueError("proj must be (Cout, C, k)")
     if out is None:
-        out = torch.empty((p["B"], p["T"], cout, p["H"], p["W"]), device=v.device, dtype=torch.float32)
+        out = _new((p["B"], p["T"], cout, p["H"], p["W"]), v, stream)
     _dev(out, "out", (p["B"], p["T"], cout, p["H"], p["W"]))
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_GATHER_REDUCE, p, v.device)
+        workspace = workspace_for(SNLS_OP_GATHER_REDUCE, p, v.device, stream)
     prm = params_from_dict(p)
     _check(lib.snls_gather_reduce(_ptr(v), _ptr(weights), _ptr(inds), _ptr(proj), ctypes.byref(prm), cout, _ptr(out),
                                   *_room(workspace), _stream(stream)), "snls_gather_reduce")
@@ -425,7 +436,7 @@ def snls_bias(dists, inds, table, p: dict, bias: dict, out=None, stream=None):
     _dev(inds, "inds", shp + (3,))
     _dev(table, "table", bias_table_shape(bias, p["HD"]))
     if out is None:
-        out = torch.empty(shp, device=dists.device, dtype=torch.float32)
+        out = _new(shp, dists, stream)
     _dev(out, "out", shp)
     _here(dists, inds, table, out)
     prm, bprm = params_from_dict(p), bias_from_dict(bias)
@@ -442,10 +453,10 @@ def snls_bias_backward(grad_scores, dists, inds, p: dict, bias: dict, grad_table
     _dev(dists, "dists", shp)
     _dev(inds, "inds", shp + (3,))
     if grad_table is None:
-        grad_table = torch.empty(bias_table_shape(bias, p["HD"]), device=dists.device, dtype=torch.float32)
+        grad_table = _new(bias_table_shape(bias, p["HD"]), dists, stream)
     _dev(grad_table, "grad_table", bias_table_shape(bias, p["HD"]))
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_BIAS_BACKWARD, p, dists.device)
+        workspace = workspace_for(SNLS_OP_BIAS_BACKWARD, p, dists.device, stream)
     _here(grad_scores, dists, inds, grad_table, workspace)
     prm, bprm = params_from_dict(p), bias_from_dict(bias)
     _check(lib.snls_bias_backward(_ptr(grad_scores), _ptr(dists), _ptr(inds), ctypes.byref(prm), ctypes.byref(bprm),
@@ -467,11 +478,11 @@ def snls_backward_scores(q, k, v, flows, dists, inds, grad_out, p: dict, scale: 
         _dev(grad_dists, "grad_dists", shp)
     if p["wt"] > 0 or flows is not None:
         _dev(flows, "flows", flow_shape(p))
-    gq, gk, gv = (torch.empty(vs, device=q.device, dtype=torch.float32) for _ in range(3))
-    gf = torch.empty(flow_shape(p), device=q.device, dtype=torch.float32)
-    gs = torch.empty(shp, device=q.device, dtype=torch.float32)
+    gq, gk, gv = (_new(vs, q, stream) for _ in range(3))
+    gf = _new(flow_shape(p), q, stream)
+    gs = _new(shp, q, stream)
     if workspace is None:
-        workspace = workspace_for(SNLS_OP_BACKWARD, p, q.device)
+        workspace = workspace_for(SNLS_OP_BACKWARD, p, q.device, stream)
     _here(q, k, v, dists, inds, grad_out, grad_dists, flows, workspace)
     prm = params_from_dict(p)
     _check(lib.snls_backward_scores(_ptr(q), _ptr(k), _ptr(v), _ptr(flows), _ptr(dists), _ptr(inds), _ptr(grad_out),
@@ -563,7 +574,7 @@ def snls_cache_attend(q, flows, ages, cache, cp: dict, ws: int, scale: float = 1
         _dev(flows, "flows", (cp["B"], cp["slots"], 2, cp["H"], cp["W"]))
     ptrs, bp = _attend_common(cp, ages, cache, table, bias)
     if out is None:
-        out = torch.empty(shp, device=q.device, dtype=torch.float32)
+        out = _new(shp, q, stream)
     _dev(out, "out", shp)
     _here(q, flows, ages, table, out, *cache)
     prm = cache_from_dict(cp)
@@ -585,7 +596,7 @@ def snls_cache_attend_points(q, points, flows, ages, cache, cp: dict, ws: int, s
         _dev(flows, "flows", (n, cp["slots"], 2))
     ptrs, bp = _attend_common(cp, ages, cache, table, bias)
     if out is None:
-        out = torch.empty((n, cp["C"]), device=q.device, dtype=torch.float32)
+        out = _new((n, cp["C"]), q, stream)
     _dev(out, "out", (n, cp["C"]))
     if n == 0:
         return out
