@@ -443,8 +443,9 @@ snls_status snls_cache_store(const float* k, const float* v, const int32_t* slot
  * table entry alone does not (a mask of the type's lowest value is a finite
  * logit), but is held as 2.3e38 at most.  Sums of weights times values are fp32
  * before the division: a value times the number of candidates stays below
- * 8e34.  Whole frames of heads of 17 to 128 channels may take their scores from
- * queries held in 22 bits, and down to 2^-38 of a query's largest channel.
+ * 8e34, and values below 1e-33 lose places.  Whole frames of heads of 17 to
+ * 128 channels may take their scores from queries held in 22 bits, and down to
+ * 2^-38 of a query's largest channel.
  * The result does not depend on scheduling.  Errors: SNLS_ERR_INVALID_ARG,
  * SNLS_ERR_UNSUPPORTED (limits of the cache and of the bias), SNLS_ERR_HIP. */
 snls_status snls_cache_attend(const float* q, const float* flows, const int32_t* ages, const void* k_codes,

@@ -32,9 +32,7 @@ FORMS = [  # channels, heads, window, slots, frame: few waves (slots split over 
 @pytest.mark.parametrize("masked", [(0,), (-1,), (0, 1), (1,)], ids=str)
 @pytest.mark.parametrize("C,HD,ws,slots,frame", FORMS, ids=str)
 def test_nan_behind_a_mask(dev, C, HD, ws, slots, frame, masked, low):
-    masked = [s % slots for s in masked]
-    if len(set(masked)) == slots:
-        pytest.skip("nothing is left")
+    masked = [s % slots for s in masked][:slots - 1]  # one slot at least is left
     cp = _cp(C=C, HD=HD, H=frame[0], W=frame[1], slots=slots)
     g = torch.Generator().manual_seed(7)
     cache, _, _ = _filled(cp, dev)
