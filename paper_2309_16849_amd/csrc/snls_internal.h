@@ -190,15 +190,18 @@ SNLS_DEV float from_score(float s, int dist) { return dist == SNLS_DIST_PROD ? s
 // Softmax of a row of finite scores d at the signed scale s: a weight is
 // exp(s * d - m) over the row's sum, m = s * best, best the score of the largest
 // key.  Where s * best leaves fp32 (scores masked with the type's lowest
-// value, a scale above 1) the scores' difference is taken first: it is all
-// that counts.
+// value, a scale above 1) the scores' difference, which is all that counts, is
+// taken first.
 SNLS_DEV float softmax_key(float s, float d) { return s < 0.f ? -d : d; }
 struct RowSoftmax {
-  float s, best, m;
-  SNLS_DEV RowSoftmax(float s_, float top_key) : s(s_), best(softmax_key(s_, top_key)), m(s_ * best) {}
-  SNLS_DEV float operator()(float d) const {
-    return expf(fabsf(m) < INFINITY ? fmaf(s, d, -m) : s * (d - best));
+  float s, from, m;
+  SNLS_DEV RowSoftmax(float s_, float top_key) : s(s_) {
+    const float best = softmax_key(s, top_key), sb = s * best;
+    const bool fits = fabsf(sb) < INFINITY;
+    from = fits ? 0.f : best;
+    m = fits ? sb : 0.f;
   }
+  SNLS_DEV float operator()(float d) const { return expf(fmaf(s, d - from, -m)); }
 };
 
 // (s1, id1) ranks before (s2, id2): larger score, ties to the smaller id.
