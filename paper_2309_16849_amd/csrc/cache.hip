@@ -465,10 +465,12 @@ SNLS_DEV half8_t codes_f16(unsigned a, unsigned b) {
 // Waves a SIMD that the registers are held to (160 x 160 to 480 x 854, ws = 9):
 // with the matrix cores 3 for heads up to 64 channels (64 channels 1.32 -> 1.08
 // ms at 480 x 854, 48 channels 151 -> 132 us at 200 x 240; 4 spill), without
-// them what the compiler takes (3 at 16 channels; 4 cost 1 to 7%).
+// them what the compiler takes (3 at 16 channels; 4 cost 1 to 7%), but 2 from
+// two vectors a lane on: a register or two more leave one wave (6,000 points of
+// 128 channels 120 us, not 94).
 constexpr int attend_waves(int CT, int R, int V, bool MX) {
   if (MX && (V == 1 || (R == 1 && CT <= 10))) return 3;
-  return V >= 3 || (MX && V >= 2) ? 2 : 1;
+  return V >= 2 ? 2 : 1;
 }
 template <int CT, int R, int V, bool POINTS, bool MX>
 __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_kernel(AttendArgs a, int tiles_x, int tiles_y, int split) {
@@ -958,6 +960,7 @@ static void run_attend_quad(const AttendArgs& a, int split, hipStream_t s) {
   // 64 channels ws = 3 50 / 59, ws = 5 90 / 76, ws = 9 164 / 132, ws = 11 211 / 205; 128 channels ws = 5 154 / 153, ws
   // = 9 305 / 259, ws = 11 394 / 318 (200 x 240); 16 channels: the tiles' other work is what the products were
   const size_t boxes = 4 * 16 * kBoxQuery<CT> * sizeof(float);
+  static_assert((64 * 16 + SNLS_BIAS_MAX_BUCKETS + 4 * 16 * kBoxQuery<10>) * sizeof(float) <= 65536, "ws <= 9 always fits");
   const bool mx = lds + boxes <= 65536;
   auto room = [&](int V, bool with_boxes) {
     const size_t join = split > 1 ? (size_t)groups * 64 * (2 + 16 * V) * sizeof(float) : 0;
@@ -967,13 +970,14 @@ static void run_attend_quad(const AttendArgs& a, int split, hipStream_t s) {
 #define SNLS_QUAD(R, V) \
   hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, POINTS, false>), grid, block, room(V, false), s, a, tx, ty, split)
 #define SNLS_QUAD_MX(R, V)                                                                                            \
-  if constexpr (!POINTS && (R * V == 2 ? CT == 10 : CT >= 6 && CT <= 12))                                           \
-    if (mx) {                                                                                                       \
+  if constexpr (!POINTS && (R * V == 2 ? CT == 10 : CT >= 6 && CT <= 12)) {                                         \
+    if (CT <= 10 || mx) {                                                                                           \
       hipLaunchKernelGGL((attend_quad_kernel<CT, R, V, false, true>), grid, block, room(V, true), s, a, tx, ty,     \
                          split);                                                                                    \
       break;                                                                                                        \
     }                                                                                                               \
-  SNLS_QUAD(R, V)
+  }                                                                                                                 \
+  if constexpr (POINTS || !(R * V == 2 ? CT == 10 : CT >= 6 && CT <= 10)) SNLS_QUAD(R, V)
   switch (c.nv) {
     case 1: SNLS_QUAD(1, 1); break;
     case 2: SNLS_QUAD_MX(2, 1); break;
