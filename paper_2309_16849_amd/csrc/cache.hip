@@ -155,12 +155,9 @@ struct AttendArgs {
 // against keys of 2^100 aside).  Queries as they are, times the scale, lost
 // logits of ordinary size for queries from 1e33 on.
 constexpr int kQTop = 100;  // 256 products with codes of up to 448 stay below 2^118
-SNLS_DEV int exponent(float most) { return __builtin_amdgcn_frexp_expf(most) - 1; }  // most in [2^e, 2^(e+1)), or 0
+// e of the largest magnitude, in [2^e, 2^(e+1)), or 0.  (Infinities need no care: no logit of such a query is finite.)
+SNLS_DEV int exponent(float most) { return __builtin_amdgcn_frexp_expf(most) - 1; }
 SNLS_DEV float key_factor(float scale, int e) { return fminf(ldexpf(scale, e), 3.402823466e38f); }
-SNLS_DEV float finite_top(float most, float x) {
-  const float t = fabsf(x);
-  return t < INFINITY ? fmaxf(most, t) : most;
-}
 
 // s plus the dot product of 16 codes with q; spread16: acc[i] += wgt * code i.
 SNLS_DEV float dot16(uint4 t, const float* q, float s) {
@@ -221,20 +218,25 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
   const bool inb = b >= 0 && b < c.B && h >= 0 && h < c.H && w >= 0 && w < c.W;
   const int vec = lane & (G - 1), tok = lane / G;
   const bool vlive = vec < c.nv;
-  float q[16], acc[16], most = 0.f;
+  float q[16], acc[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int ch = vec * 16 + i;
     q[i] = 0.f;
     acc[i] = 0.f;
-    if (inb && ch < c.Ch) q[i] = a.q[qi * c.C + hd * c.Ch + ch];
-    most = finite_top(most, q[i]);
+    if (ch < c.Ch) q[i] = a.q[qi * c.C + hd * c.Ch + ch];  // (under way beside the point itself, inside or not)
   }
+  // As much of the powers of two of query and scale as fits goes to q: all of it but at fp32's ends, where the cells get
+  // the rest; what leaves fp32 before that leaves it with the rest too.
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(q[i]));
 #pragma unroll
   for (int o = 1; o < G; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
-  const int up = kQTop - exponent(most);
+  const int eq = exponent(most), top = min(max(eq + a.se, -60), kQTop);
+  const int rest = __builtin_amdgcn_readfirstlane(eq + a.se - top);  // one query and head a wave
 #pragma unroll
-  for (int i = 0; i < 16; ++i) q[i] = ldexpf(q[i], up) * a.sm;
+  for (int i = 0; i < 16; ++i) q[i] = ldexpf(q[i], top - eq) * a.sm;
   for (int i = lane; i < (ws + 2) * (ws + 2); i += 64) cells[i] = 0.f;
   float m = -INFINITY, z = 0.f;  // running maximum (of the wave) and this lane's sum
   if (inb)
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
         float d = 0.f;
         if (in && vlive) {
           d = dot16(*reinterpret_cast<const uint4*>(kp + (unsigned)((y * c.W + x) * c.Cp + vec * 16)), q, 0.f);
-          d *= key_factor(ksp[(y >> c.sh) * c.nbx + (x >> c.sh)], a.se - up);
+          d *= ksp[(y >> c.sh) * c.nbx + (x >> c.sh)];
         }
 #pragma unroll
         for (int o = 1; o < G; o <<= 1) d += __shfl_xor(d, o);
@@ -285,7 +287,7 @@ __global__ void __launch_bounds__(64 * SPLIT) attend_wave_kernel(AttendArgs a) {
           if (cell_ok(y0 + dh, ay != 0.f, c.H) && cell_ok(x0 + dw, ax != 0.f, c.W)) {
             const float* tp = taps + dh * nt + dw;
             const float up = (1.f - ax) * tp[0] + ax * tp[1], dn = (1.f - ax) * tp[nt] + ax * tp[nt + 1];
-            float sc = (1.f - ay) * up + ay * dn;
+            float sc = ldexpf((1.f - ay) * up + ay * dn, rest);
             if (a.table) {
               const int at = (bt * a.bias.nb + bias_bucket(Fh + (float)(dh - r), a.bias)) * a.bias.nb +
                              bias_bucket(Fw + (float)(dw - r), a.bias);
@@ -545,7 +547,7 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) most = finite_top(most, q[v][i]);
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(q[v][i]));
     most = fmaxf(most, quad<1, 0, 3, 2>(most));
     most = fmaxf(most, quad<2, 3, 0, 1>(most));
     const int up = kQTop - exponent(most);
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(256, attend_waves(CT, R, V, MX)) attend_quad_k
       for (int i = 0; i < 16; ++i) {
         const int ch = (kPack ? (g4 & 1) : 4 * jj + g4) * 16 + i;
         x[jj][i] = inq && ch < c.Ch ? qp[ch * HW] : 0.f;
-        most = finite_top(most, x[jj][i]);
+        most = fmaxf(most, fabsf(x[jj][i]));
       }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
