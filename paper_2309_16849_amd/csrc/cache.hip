@@ -47,8 +47,9 @@ SNLS_DEV unsigned encode4(float a, float b, float c, float d, float inv) {
 // 8 x 8 blocks side by side; one thread per pixel.  The channels (up to NV * 16)
 // stay in registers between the largest magnitude and the codes; read a second
 // time instead, 128 channels at 480 x 854 take 286 us, not 144, 256 take 579,
-// not 333 (at one wave a SIMD), 64 take 150, not 67.  Bound by memory: 64
-// channels at 84% of a copy's rate, 128 at 77%, 256 at 67%.  blockIdx.y = 0
+// not 334 (at one wave a SIMD), 64 take 150, not 68.  Bound by memory: 3.9 TB/s
+// at 64 channels, 3.6 at 128, 3.1 at 256, four fifths of it reads, where a large
+// copy has 5.0 and the position bias, of the same mix, 5.3.  blockIdx.y = 0
 // stores keys, 1 values.
 template <int NV>
 __global__ void __launch_bounds__(256) cache_store_kernel(const float* __restrict__ k, const float* __restrict__ v,
@@ -428,21 +429,24 @@ SNLS_DEV float table_base2(float t, float scale) {
   return fabsf(x) < INFINITY ? fminf(fmaxf(x * kLog2e, -3.402823466e38f), 3.402823466e38f) : x;
 }
 
-// MX: scores from the matrix cores (heads of 17 to 128 channels; 64 channels
-// at 480 x 854 1.45 -> 1.08 ms, two heads of 32 at 256 x 256 0.32 -> 0.27).  The
-// windows of a wave's 16 queries overlap, so the box around them in a slot's
-// frame is walked in tiles of 16 tokens, v_mfma_f32_16x16x32_f16 with tokens as
-// rows and queries as columns, and each query's own taps of the product go to
-// LDS, from where the rows of taps are read.  Codes are exact in fp16; q is
-// split in two fp16 parts that hold 22 bits of a query's largest channel
-// (scaled by a power of two per query).  A box is some four times a window
+// MX: scores from the matrix cores (heads of 17 to 128 channels; 64 channels at
+// 480 x 854, 3 slots, 1.03 -> 0.78 ms, two heads of 32 at 256 x 256 0.23 -> 0.20).
+// The windows of a wave's 16 queries overlap, so the box around them in a
+// slot's frame is walked in tiles of 16 tokens, v_mfma_f32_16x16x32_f16 with
+// tokens as rows and queries as columns, and each query's own taps of the
+// product go to LDS, from where the rows of taps are read.  Codes are exact in
+// fp16; q is split in two fp16 parts that hold 22 bits of a query's largest
+// channel (scaled by a power of two per query): outputs are 3.9e-7 of the values
+// off 64 bits on the 480 x 854 frame, where fp32 queries, three parts and half as
+// many products again, would leave 1.7e-7.  A box is some four times a window
 // (offsets carry an error of pixels), the matrix cores 30 times as fast as the
 // vector units on such a product.  Where the box would be larger than the 16
 // windows are together (offsets that differ by tens of pixels between
 // neighbours), every window is a box of its own.  64 channels at 200 x 240, 3
-// slots: equal offsets 119 us, neighbours' offsets 1 / 3 / 10 / 40 pixels apart
-// 131 / 149 / 270 / 275, the vector units 165 whatever they are; the vector
-// units' form as a second branch 204 at 40 pixels, but 127 at 0, for its registers.
+// slots: equal offsets 104 us, neighbours' offsets 1 / 3 / 10 / 40 pixels apart
+// 118 / 139 / 263 / 276, the vector units 144 to 157; the vector units' form as a
+// second branch was faster at 40 pixels (204, not 275), but took 7% at 0, for its
+// registers.
 template <int CT>
 constexpr int kBoxPitch = CT + 6;  // a row of taps with the three beside it that a group of four tokens may bring
 template <int CT>
@@ -958,9 +962,10 @@ static void run_attend_quad(const AttendArgs& a, int split, hipStream_t s) {
   const dim3 grid((unsigned)(POINTS ? blocks * c.HD : (blocks * c.HD + 7) / 8 * 8)), block(256);
   size_t lds = (64 * 16 + (a.table ? a.bias.buckets : 1)) * sizeof(float);
   // Scores from the matrix cores, where LDS for them fits the 64 KB that a launch may ask for (ws <= 9 whatever the
-  // table).  3 slots, vector units / matrix cores: 32 channels ws = 7 69 / 78 us, ws = 9 120 / 104, ws = 11 135 / 148;
-  // 64 channels ws = 3 50 / 59, ws = 5 90 / 76, ws = 9 164 / 132, ws = 11 211 / 205; 128 channels ws = 5 154 / 153, ws
-  // = 9 305 / 259, ws = 11 394 / 318 (200 x 240); 16 channels: the tiles' other work is what the products were
+  // table).  3 slots, 200 x 240, offsets 1.5 pixels apart, vector units / matrix cores: 32 channels ws = 7 60 / 70 us,
+  // ws = 9 107 / 96, ws = 11 124 / 137; 48 channels ws = 3 43 / 55, ws = 5 76 / 74; 64 channels ws = 3 40 / 49, ws = 5
+  // 73 / 67, ws = 9 149 / 121, ws = 11 195 / 187; 128 channels ws = 3 71 / 88, ws = 5 124 / 129, ws = 7 182 / 171, ws = 9
+  // 295 / 235, ws = 11 369 / 292; 16 channels: the tiles' other work is what the products were
   const size_t boxes = 4 * 16 * kBoxQuery<CT> * sizeof(float);
   static_assert((64 * 16 + SNLS_BIAS_MAX_BUCKETS + 4 * 16 * kBoxQuery<10>) * sizeof(float) <= 65536, "ws <= 9 always fits");
   const bool mx = lds + boxes <= 65536;
