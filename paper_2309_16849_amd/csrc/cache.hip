@@ -437,8 +437,8 @@ SNLS_DEV float table_base2(float t, float scale) {
 // product go to LDS, from where the rows of taps are read.  Codes are exact in
 // fp16; q is split in two fp16 parts that hold 22 bits of a query's largest
 // channel (scaled by a power of two per query): outputs are 3.9e-7 of the values
-// off 64 bits on the 480 x 854 frame, where fp32 queries, three parts and half as
-// many products again, would leave 1.7e-7.  A box is some four times a window
+// off 64 bits on the 480 x 854 frame, plain fp32 1.7e-7; all 24 bits would be
+// three parts and half as many products again.  A box is some four times a window
 // (offsets carry an error of pixels), the matrix cores 30 times as fast as the
 // vector units on such a product.  Where the box would be larger than the 16
 // windows are together (offsets that differ by tens of pixels between
