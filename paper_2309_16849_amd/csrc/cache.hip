@@ -158,7 +158,10 @@ struct AttendArgs {
 constexpr int kQTop = 100;  // 256 products with codes of up to 448 stay below 2^118
 // e of the largest magnitude, in [2^e, 2^(e+1)), or 0.  (Infinities need no care: no logit of such a query is finite.)
 SNLS_DEV int exponent(float most) { return __builtin_amdgcn_frexp_expf(most) - 1; }
-SNLS_DEV float key_factor(float scale, int e) { return fminf(ldexpf(scale, e), 3.402823466e38f); }
+SNLS_DEV float key_factor(float scale, int e) {
+  const float f = ldexpf(scale, e);
+  return f > 3.402823466e38f ? 3.402823466e38f : f;  // (0 times it stays 0; NaN stays NaN)
+}
 
 // s plus the dot product of 16 codes with q; spread16: acc[i] += wgt * code i.
 SNLS_DEV float dot16(uint4 t, const float* q, float s) {

@@ -152,3 +152,18 @@ def test_table_beside_extreme_sizes(dev, C):
         B.snls_cache_store((1e-34 * k).to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
     q = 1e34 * torch.randn(1, C, 48, 47, generator=g)
     _run(dev, cp, 5, q, torch.randn(1, 2, 2, 48, 47, generator=g), cache, 2.0 * C ** -0.5, g, table, bias)
+
+
+@pytest.mark.parametrize("C", CHANNELS)
+def test_scales_not_finite(dev, C):
+    """A block of keys whose scale is NaN or infinite takes out the candidates that read it, in every form."""
+    cp = _cp(C=C, HD=1, H=48, W=47, slots=2)
+    g = torch.Generator().manual_seed(56)
+    cache = B.cache_alloc(cp, dev)
+    for s in range(2):
+        k, v = (torch.randn(1, C, 48, 47, generator=g) for _ in range(2))
+        B.snls_cache_store(k.to(dev), v.to(dev), torch.full((1,), s, dtype=torch.int32, device=dev), cp, cache)
+    cache[1][0, 0, 0, 2, 3] = float("nan")
+    cache[1][0, 1, 0, 0, 0] = float("inf")
+    q = torch.randn(1, C, 48, 47, generator=g)
+    _run(dev, cp, 5, q, torch.randn(1, 2, 2, 48, 47, generator=g), cache, C ** -0.5, g)
