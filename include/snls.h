@@ -24,7 +24,12 @@
  *                   neighbours' relative position and its training;
  *   snls_cache_store, snls_cache_attend, snls_cache_attend_points  past frames
  *                   held in 8 bits and attention over their whole windows, for
- *                   programs that see a video frame by frame.
+ *                   programs that see a video frame by frame;
+ *   snls_norm, snls_norm_backward, snls_dropout, snls_rotate,
+ *   snls_rotate_points, snls_project_pack, snls_project  what a layer has
+ *                   around its attention: the norm (of a residual sum) and its
+ *                   gradients, dropout, rotary positions over time, rows and
+ *                   columns, and projections with 8-bit weights.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -468,6 +473,172 @@ snls_status snls_cache_attend_points(const float* q, const int32_t* points, int6
                                      const void* v_codes, const float* v_scales, const float* table,
                                      const snls_cache_params* cp, const snls_bias_params* bias, int32_t ws,
                                      float scale, float* out, void* stream);
+
+/* ---- norm, dropout --------------------------------------------------------
+ * Features are (frames, C, pixels): the frames of every video one after the
+ * other, as (B, T, C, H, W) holds them, or, with pixels == 1, a list of
+ * `frames` tokens of C channels.  struct_size must be
+ * sizeof(snls_norm_params).
+ *
+ * Dropout's mask is a function of an element's flat index i, of `site` (which
+ * dropout of the network it is) and of two numbers on the device, rng[0] the
+ * seed and rng[1] the step: word i % 4 of the Philox 4x32 generator with 10
+ * rounds at counter (i/4 mod 2^32, i/4 div 2^32, step mod 2^32, site) and key
+ * (seed mod 2^32, seed div 2^32); the element stays if the word is at least
+ * floor(drop * 2^32) and is divided by 1 - drop, otherwise it is 0, whatever it
+ * was.  No mask is stored: the backward pass forms it again from the same rng.
+ * A captured graph reads rng anew in every replay. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t C;       /* >= 1 */
+  int64_t frames;  /* >= 0 */
+  int64_t pixels;  /* >= 1 */
+  float eps;       /* >= 0, finite */
+  float drop;      /* 0 <= drop < 1, finite */
+  uint32_t site;
+} snls_norm_params;
+
+/* snls_norm -- layer norm over the channels of every pixel, of x or of a
+ * residual sum: total = x + dropout(branch), mean and rstd = 1 / sqrt(variance
+ * + eps) over the C channels of a pixel of total (of x without branch), y =
+ * (total - mean) * rstd * gamma + beta.  The variance is the mean of the squared
+ * differences from the mean.  Sums of C values and of their squares stay in
+ * fp32: |x| * C and (x - mean)^2 * C have to stay in its range.
+ *   x       device, (frames, C, pixels)
+ *   branch  device, as x, or NULL (then total is not written; drop must be 0)
+ *   rng     device, 2 x uint64 (seed, step); may be NULL when drop == 0
+ *   gamma, beta  device, (C), or NULL for 1 and for 0
+ *   total   device out, as x, or NULL without branch; may be x or branch itself
+ *   y       device out, as x, fully overwritten; overlaps no other buffer but,
+ *           without branch, may be x itself
+ *   stats   device out, (2, frames, pixels): the means, then the rstds; NULL if
+ *           no backward pass follows
+ * Nothing is touched when frames == 0.  The result does not depend on
+ * scheduling.
+ * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for pixels of 2^30 or more
+ * or 2^38 elements or more; SNLS_ERR_HIP. */
+snls_status snls_norm(const float* x, const float* branch, const uint64_t* rng, const float* gamma, const float* beta,
+                      const snls_norm_params* np, float* total, float* y, float* stats, void* stream);
+
+/* snls_norm_backward -- gradients of snls_norm: with xh = (total - mean) * rstd
+ * and g = grad_y * gamma, grad_x = rstd * (g - mean over C of g - xh * mean over
+ * C of g * xh) + grad_total, grad_branch = grad_x through the same dropout,
+ * grad_gamma = sum over frames and pixels of grad_y * xh, grad_beta = that of
+ * grad_y.
+ *   grad_y      device, (frames, C, pixels)
+ *   grad_total  device, the gradient that reaches total by other ways, or NULL
+ *   total       device, snls_norm's (x without branch)
+ *   stats       device, snls_norm's
+ *   gamma, rng, np  as in snls_norm
+ *   grad_x      device out; may be grad_y or grad_total itself
+ *   grad_branch device out; NULL allowed when drop == 0, where it is grad_x
+ *   grad_gamma, grad_beta  device out, (C), fully overwritten (0 when frames ==
+ *               0), or both NULL
+ *   workspace   device scratch of at least snls_norm_workspace_size(np) bytes,
+ *               256-byte aligned; not needed without grad_gamma
+ * The sums over pixels are held in 64 bits behind the first few hundred terms
+ * of each and the result does not depend on scheduling.
+ * Errors: as snls_norm; SNLS_ERR_WORKSPACE. */
+snls_status snls_norm_backward(const float* grad_y, const float* grad_total, const float* total, const float* stats,
+                               const float* gamma, const uint64_t* rng, const snls_norm_params* np, float* grad_x,
+                               float* grad_branch, float* grad_gamma, float* grad_beta, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Device workspace of snls_norm_backward ((size_t)-1 for invalid arguments). */
+size_t snls_norm_workspace_size(const snls_norm_params* np);
+
+/* snls_dropout -- out = dropout(x), or residual + dropout(x), of n values (the
+ * mask above, i counted from x).  Applied to a gradient it is its own backward
+ * pass.
+ *   x, residual  device, n values; residual may be NULL
+ *   rng          device, 2 x uint64; may be NULL when drop == 0
+ *   out          device out; may be x or residual itself; nothing is touched
+ *                when n == 0
+ * Errors: SNLS_ERR_INVALID_ARG (n < 0, drop outside [0, 1), NULL buffers),
+ * SNLS_ERR_UNSUPPORTED (n of 2^38 or more), SNLS_ERR_HIP. */
+snls_status snls_dropout(const float* x, const float* residual, const uint64_t* rng, int64_t n, float drop,
+                         uint32_t site, float* out, void* stream);
+
+/* ---- rotary positions -----------------------------------------------------
+ * A head's first 2 * pairs[0] channels carry the time, the next 2 * pairs[1]
+ * the row, the next 2 * pairs[2] the column; channels behind them stay as they
+ * are.  Pair i of an axis with n pairs is its channels 2i and 2i+1
+ * (interleaved) or i and n+i (not), and is turned by the angle position *
+ * theta^(-i/n): (a, b) -> (a cos - b sin, a sin + b cos).  Inner products of
+ * turned queries and keys depend on the difference of their positions.
+ * Positions are the frame's time, row0 + row and col0 + column.  Angles are
+ * formed and reduced in 64 bits: off by at most |angle| * 2^-51 radians and
+ * 2^-24 more.  struct_size must be sizeof(snls_rotate_params). */
+#define SNLS_ROTATE_MAX_PAIRS 128 /* largest sum of pairs */
+typedef struct {
+  uint32_t struct_size;
+  int32_t B, T, C, H, W, HD;
+  int32_t pairs[3];    /* >= 0, 2 * their sum at most C/HD */
+  float theta[3];      /* > 0, finite */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t row0, col0;
+} snls_rotate_params;
+
+/* snls_rotate -- rotary positions of videos q and k.
+ *   q, k          device, (B, T, C, H, W); k may be NULL, and then k_out too
+ *   times         device, int64 (B, T): the time of each frame, or NULL for 0 .. T-1
+ *   inverse       0, or 1 for the angles' negatives: the gradients of q and k
+ *                 from those of q_out and k_out
+ *   q_out, k_out  device out, fully overwritten; may be q and k themselves
+ * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED beyond
+ * SNLS_ROTATE_MAX_PAIRS, H*W of 2^30 or more, 2^38 elements or more;
+ * SNLS_ERR_HIP. */
+snls_status snls_rotate(const float* q, const float* k, const int64_t* times, const snls_rotate_params* rp,
+                        int32_t inverse, float* q_out, float* k_out, void* stream);
+
+/* snls_rotate_points -- the same for a list of n single tokens.
+ *   q       device, (n, C)
+ *   points  device, int32 (n, 3): video of the batch, row, column; a point
+ *           outside the batch or the frame gets a row of zeros
+ *   times   device, int64 (B): the time of each video, or NULL for 0 (rp->T is
+ *           not used)
+ *   out     device out, (n, C); may be q itself; nothing is touched when n == 0
+ * Errors: as snls_rotate; n < 0 is SNLS_ERR_INVALID_ARG. */
+snls_status snls_rotate_points(const float* q, const int32_t* points, int64_t n, const int64_t* times,
+                               const snls_rotate_params* rp, int32_t inverse, float* out, void* stream);
+
+/* ---- projections in 8 bits ------------------------------------------------
+ * out[o] = token scale * scales[o] * sum over c of code[c] * codes[o, c] + bias[o]
+ * for every pixel of (frames, cin, pixels), or every token of (frames, cin)
+ * with pixels == 1.  A token's scale is max(largest magnitude, 2^-100) / 127
+ * rounded to fp32, its codes the quotients by that scale, rounded to the
+ * nearest whole number, ties to even (of the exact quotient); the sum is exact.
+ * A token with an infinity or a NaN has NaN in all its outputs.  The output is
+ * split into `parts` of equal size (q, k and v), each a tensor of its own.
+ * struct_size must be sizeof(snls_project_params). */
+#define SNLS_PROJECT_MAX_CIN 1024
+typedef struct {
+  uint32_t struct_size;
+  int32_t cin, cout; /* >= 1; codes are (cout, cin) */
+  int32_t parts;     /* >= 1, cout % parts == 0 */
+  int64_t frames;    /* >= 0 */
+  int64_t pixels;    /* >= 1 */
+} snls_project_params;
+
+/* snls_project_pack -- weights w (cout, cin) as codes and a scale per output
+ * channel, by the rounding above (a row with an infinity or a NaN gets the scale
+ * NaN and codes 0).  Once per model.
+ *   codes   device out, int8 (cout, cin);  scales  device out, (cout)
+ * Of pp only cin and cout count.  Errors: as snls_project. */
+snls_status snls_project_pack(const float* w, const snls_project_params* pp, void* codes, float* scales, void* stream);
+
+/* snls_project -- the product.
+ *   x       device, (frames, cin, pixels)
+ *   codes   device, int8 (cout, cin), values -127 .. 127;  scales  device, (cout)
+ *   bias    device, (cout), or NULL for 0
+ *   out     device out, (parts, frames, cout/parts, pixels), fully overwritten;
+ *           overlaps no input; nothing is touched when frames == 0
+ * |x| * 127 * cin has to stay in fp32's range.  The result does not depend on
+ * scheduling.  Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for cin above
+ * SNLS_PROJECT_MAX_CIN, cout of 2^16 or more, pixels of 2^30 or more, 2^38
+ * elements of x or out or more; SNLS_ERR_HIP. */
+snls_status snls_project(const float* x, const void* codes, const float* scales, const float* bias,
+                         const snls_project_params* pp, float* out, void* stream);
 
 #define SNLS_OP_SEARCH 0
 #define SNLS_OP_AGGREGATE 1

@@ -298,4 +298,99 @@ snls_status snls_cache_attend_points(const float* q, const int32_t* points, int6
                              as_stream(stream));
 }
 
+snls_status snls_norm(const float* x, const float* branch, const uint64_t* rng, const float* gamma, const float* beta,
+                      const snls_norm_params* np, float* total, float* y, float* stats, void* stream) {
+  Drop d;
+  snls_status st = check_norm(np);
+  if (st != SNLS_OK) return st;
+  if ((st = check_drop(np->drop, np->site, rng, &d)) != SNLS_OK) return st;
+  if (!branch && np->drop > 0.f) return SNLS_ERR_INVALID_ARG;
+  if (np->frames == 0) return SNLS_OK;
+  if (!x || !y || (branch && !total)) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_norm(x, branch, d, gamma, beta, *np, total, y, stats, as_stream(stream));
+}
+
+snls_status snls_norm_backward(const float* grad_y, const float* grad_total, const float* total, const float* stats,
+                               const float* gamma, const uint64_t* rng, const snls_norm_params* np, float* grad_x,
+                               float* grad_branch, float* grad_gamma, float* grad_beta, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  Drop d;
+  snls_status st = check_norm(np);
+  if (st != SNLS_OK) return st;
+  if ((st = check_drop(np->drop, np->site, rng, &d)) != SNLS_OK) return st;
+  if (!grad_gamma != !grad_beta) return SNLS_ERR_INVALID_ARG;
+  if (np->frames > 0 && (!grad_y || !total || !stats || !grad_x || (np->drop > 0.f && !grad_branch)))
+    return SNLS_ERR_INVALID_ARG;
+  if (np->frames == 0 && !grad_gamma) return SNLS_OK;
+  if (grad_gamma && (!workspace || workspace_bytes < norm_backward_ws_bytes(*np) ||
+                     (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return SNLS_ERR_WORKSPACE;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_norm_backward(grad_y, grad_total, total, stats, gamma, d, *np, grad_x, grad_branch, grad_gamma,
+                              grad_beta, static_cast<double*>(workspace), as_stream(stream));
+}
+
+size_t snls_norm_workspace_size(const snls_norm_params* np) {
+  return check_norm(np) == SNLS_OK ? norm_backward_ws_bytes(*np) : (size_t)-1;
+}
+
+snls_status snls_dropout(const float* x, const float* residual, const uint64_t* rng, int64_t n, float drop,
+                         uint32_t site, float* out, void* stream) {
+  Drop d;
+  snls_status st = check_drop(drop, site, rng, &d);
+  if (st != SNLS_OK) return st;
+  if (n < 0) return SNLS_ERR_INVALID_ARG;
+  if (n >= 1LL << 38) return SNLS_ERR_UNSUPPORTED;
+  if (n == 0) return SNLS_OK;
+  if (!x || !out) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_dropout(x, residual, d, n, out, as_stream(stream));
+}
+
+snls_status snls_rotate(const float* q, const float* k, const int64_t* times, const snls_rotate_params* rp,
+                        int32_t inverse, float* q_out, float* k_out, void* stream) {
+  Rotary r;
+  if (inverse != 0 && inverse != 1) return SNLS_ERR_INVALID_ARG;
+  snls_status st = check_rotate(rp, inverse != 0, &r);
+  if (st != SNLS_OK) return st;
+  if (!q || !q_out || !k != !k_out) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_rotate(q, k, times, r, q_out, k_out, as_stream(stream));
+}
+
+snls_status snls_rotate_points(const float* q, const int32_t* points, int64_t n, const int64_t* times,
+                               const snls_rotate_params* rp, int32_t inverse, float* out, void* stream) {
+  Rotary r;
+  if (inverse != 0 && inverse != 1) return SNLS_ERR_INVALID_ARG;
+  snls_status st = check_rotate(rp, inverse != 0, &r);
+  if (st != SNLS_OK) return st;
+  if (n < 0) return SNLS_ERR_INVALID_ARG;
+  if ((double)n * r.C >= 274877906944.0) return SNLS_ERR_UNSUPPORTED;
+  if (n == 0) return SNLS_OK;
+  if (!q || !points || !out) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_rotate_points(q, points, n, times, r, out, as_stream(stream));
+}
+
+snls_status snls_project_pack(const float* w, const snls_project_params* pp, void* codes, float* scales,
+                              void* stream) {
+  snls_status st = check_project(pp);
+  if (st != SNLS_OK) return st;
+  if (!w || !codes || !scales) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_project_pack(w, pp->cin, pp->cout, static_cast<int8_t*>(codes), scales, as_stream(stream));
+}
+
+snls_status snls_project(const float* x, const void* codes, const float* scales, const float* bias,
+                         const snls_project_params* pp, float* out, void* stream) {
+  snls_status st = check_project(pp);
+  if (st != SNLS_OK) return st;
+  if (!codes || !scales) return SNLS_ERR_INVALID_ARG;
+  if (pp->frames == 0) return SNLS_OK;
+  if (!x || !out) return SNLS_ERR_INVALID_ARG;
+  if ((st = device_ready()) != SNLS_OK) return st;
+  return launch_project(x, static_cast<const int8_t*>(codes), scales, bias, *pp, out, as_stream(stream));
+}
+
 }  // extern "C"

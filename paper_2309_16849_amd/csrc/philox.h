@@ -1,0 +1,52 @@
+// philox.h -- dropout's mask (device side; the same for the norm of a residual
+// sum, its gradients and the dropout on its own).
+//
+// Philox 4x32 with 10 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3", 2011): four words of 32 bits from a counter of
+// 128 bits and a key of 64.  Elements 4b .. 4b+3 take the words of block b, so
+// a lane with four consecutive elements forms one block for them, or two where
+// they straddle a border.
+#pragma once
+
+#include "snls_internal.h"
+
+#ifdef __HIPCC__
+
+namespace snls {
+
+struct Words {
+  unsigned w[4];
+};
+
+// The generator of a call: key and the counter's upper half.
+struct Philox {
+  unsigned k0, k1, step, site;
+  SNLS_DEV explicit Philox(const Drop& d) {
+    const unsigned long long seed = d.rng ? d.rng[0] : 0;
+    k0 = (unsigned)seed, k1 = (unsigned)(seed >> 32);
+    step = d.rng ? (unsigned)d.rng[1] : 0, site = d.site;
+  }
+  SNLS_DEV Words block(long long b) const {
+    unsigned c0 = (unsigned)b, c1 = (unsigned)(b >> 32), c2 = step, c3 = site, a = k0, e = k1;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      const unsigned h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0;
+      const unsigned h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
+      c0 = h1 ^ c1 ^ a, c1 = l1, c2 = h0 ^ c3 ^ e, c3 = l0;
+      a += 0x9E3779B9u, e += 0xBB67AE85u;
+    }
+    return {{c0, c1, c2, c3}};
+  }
+  // Word of element i.
+  SNLS_DEV unsigned word(long long i) const {
+    const Words b = block(i >> 2);
+    const int j = (int)(i & 3);
+    return j == 0 ? b.w[0] : j == 1 ? b.w[1] : j == 2 ? b.w[2] : b.w[3];
+  }
+};
+
+SNLS_DEV float dropped(float x, unsigned word, const Drop& d) { return word >= d.thr ? x * d.keep : 0.f; }
+
+}  // namespace snls
+
+#endif  // __HIPCC__

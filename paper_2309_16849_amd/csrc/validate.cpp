@@ -94,4 +94,69 @@ snls_status check_cache(const snls_cache_params* c, CacheGeo* out) {
   return SNLS_OK;
 }
 
+// Elements of (frames, C, pixels): offsets are 64-bit, grids strided.
+static bool too_many(long long frames, long long channels, long long pixels) {
+  return (double)frames * (double)channels * (double)pixels >= 274877906944.0;  // 2^38
+}
+
+snls_status check_norm(const snls_norm_params* np) {
+  if (!np || np->struct_size != sizeof(snls_norm_params)) return SNLS_ERR_INVALID_ARG;
+  if (np->C < 1 || np->frames < 0 || np->pixels < 1) return SNLS_ERR_INVALID_ARG;
+  if (!isfinite(np->eps) || np->eps < 0.f) return SNLS_ERR_INVALID_ARG;
+  if (!(np->drop >= 0.f && np->drop < 1.f)) return SNLS_ERR_INVALID_ARG;
+  if (np->pixels >= kMaxPlane || too_many(np->frames, np->C, np->pixels)) return SNLS_ERR_UNSUPPORTED;
+  return SNLS_OK;
+}
+
+snls_status check_drop(float drop, uint32_t site, const uint64_t* rng, Drop* out) {
+  if (!(drop >= 0.f && drop < 1.f)) return SNLS_ERR_INVALID_ARG;
+  if (drop > 0.f && !rng) return SNLS_ERR_INVALID_ARG;
+  out->rng = drop > 0.f ? reinterpret_cast<const unsigned long long*>(rng) : nullptr;
+  out->thr = (unsigned)((double)drop * 4294967296.0);
+  out->site = site;
+  out->keep = (float)(1.0 / (1.0 - (double)drop));
+  return SNLS_OK;
+}
+
+snls_status check_rotate(const snls_rotate_params* rp, bool inverse, Rotary* out) {
+  if (!rp || rp->struct_size != sizeof(snls_rotate_params)) return SNLS_ERR_INVALID_ARG;
+  if (rp->B < 1 || rp->T < 1 || rp->C < 1 || rp->H < 1 || rp->W < 1 || rp->HD < 1 || rp->C % rp->HD != 0)
+    return SNLS_ERR_INVALID_ARG;
+  if (rp->interleaved != 0 && rp->interleaved != 1) return SNLS_ERR_INVALID_ARG;
+  long long total = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (rp->pairs[a] < 0 || !isfinite(rp->theta[a]) || !(rp->theta[a] > 0.f)) return SNLS_ERR_INVALID_ARG;
+    total += rp->pairs[a];
+  }
+  const int Ch = rp->C / rp->HD;
+  if (2 * total > Ch) return SNLS_ERR_INVALID_ARG;
+  if (total > SNLS_ROTATE_MAX_PAIRS) return SNLS_ERR_UNSUPPORTED;
+  if ((long long)rp->H * rp->W >= kMaxPlane || too_many((long long)rp->B * rp->T, rp->C, (long long)rp->H * rp->W))
+    return SNLS_ERR_UNSUPPORTED;
+  out->B = rp->B; out->T = rp->T; out->C = rp->C; out->H = rp->H; out->W = rp->W; out->HD = rp->HD;
+  out->Ch = Ch;
+  out->total = (int)total;
+  out->interleaved = rp->interleaved;
+  out->row0 = rp->row0; out->col0 = rp->col0;
+  int at = 0;
+  for (int a = 0; a < 3; ++a) {
+    out->pairs[a] = rp->pairs[a];
+    for (int i = 0; i < rp->pairs[a]; ++i) {
+      const double f = pow((double)rp->theta[a], -(double)i / rp->pairs[a]) / 6.283185307179586476925;
+      out->turns[at++] = inverse ? -f : f;
+    }
+  }
+  return SNLS_OK;
+}
+
+snls_status check_project(const snls_project_params* pp) {
+  if (!pp || pp->struct_size != sizeof(snls_project_params)) return SNLS_ERR_INVALID_ARG;
+  if (pp->cin < 1 || pp->cout < 1 || pp->parts < 1 || pp->frames < 0 || pp->pixels < 1) return SNLS_ERR_INVALID_ARG;
+  if (pp->cout % pp->parts != 0) return SNLS_ERR_INVALID_ARG;
+  if (pp->cin > SNLS_PROJECT_MAX_CIN || pp->cout >= 1 << 16 || pp->pixels >= kMaxPlane) return SNLS_ERR_UNSUPPORTED;
+  if (too_many(pp->frames, pp->cin, pp->pixels) || too_many(pp->frames, pp->cout, pp->pixels))
+    return SNLS_ERR_UNSUPPORTED;
+  return SNLS_OK;
+}
+
 }  // namespace snls

@@ -9,11 +9,15 @@ Functions carry the C names: snls_search, snls_topk, snls_aggregate,
 snls_backward, snls_aggregate_stacked, snls_chain_flows, snls_aggregate_static,
 snls_gather_stacked, snls_stacked_reduce, snls_gather_reduce, snls_bias,
 snls_bias_backward, snls_backward_scores, snls_cache_store, snls_cache_attend,
-snls_cache_attend_points, snls_workspace_size, snls_status_string,
+snls_cache_attend_points, snls_norm, snls_norm_backward, snls_dropout,
+snls_rotate, snls_rotate_points, snls_project_pack, snls_project,
+snls_workspace_size, snls_norm_workspace_size, snls_status_string,
 snls_abi_version.
 Parameters are plain dicts with keys B, T, C, H, W, HD, ws, wt, ps, stride0,
 stride1, k, dist_type (see ``params_from_dict``); the position bias's with keys
-radius and edges (a list), a cache's with keys B, slots, C, H, W, HD, block.
+radius and edges (a list), a cache's with keys B, slots, C, H, W, HD, block, the
+rotary positions' with keys B, T, C, H, W, HD, pairs and theta (three numbers
+each) and, where they are not 0, interleaved, row0, col0.
 A cache is the tuple (k_codes, k_scales, v_codes, v_scales) that ``cache_alloc``
 returns.
 """
@@ -36,11 +40,13 @@ SNLS_OP_BIAS_BACKWARD = 6
 SNLS_MAX_K = 128
 SNLS_BIAS_MAX_EDGES, SNLS_BIAS_MAX_BUCKETS = 16, 4096
 SNLS_STATIC_SCRATCH_BYTES = 64 << 20
+SNLS_ROTATE_MAX_PAIRS, SNLS_PROJECT_MAX_CIN = 128, 1024
 SYMBOLS = ("snls_search", "snls_topk", "snls_aggregate", "snls_backward", "snls_workspace_size",
            "snls_status_string", "snls_abi_version", "snls_aggregate_stacked", "snls_chain_flows",
            "snls_aggregate_static", "snls_gather_stacked", "snls_stacked_reduce", "snls_gather_reduce",
            "snls_bias", "snls_bias_backward", "snls_backward_scores", "snls_cache_store", "snls_cache_attend",
-           "snls_cache_attend_points")
+           "snls_cache_attend_points", "snls_norm", "snls_norm_backward", "snls_norm_workspace_size", "snls_dropout",
+           "snls_rotate", "snls_rotate_points", "snls_project_pack", "snls_project")
 
 
 class SnlsParams(ctypes.Structure):
@@ -60,6 +66,27 @@ class SnlsCacheParams(ctypes.Structure):
     """Mirror of the C struct snls_cache_params."""
     _fields_ = [("struct_size", ctypes.c_uint32)] + [
         (n, ctypes.c_int32) for n in ("B", "slots", "C", "H", "W", "HD", "block")]
+
+
+class SnlsNormParams(ctypes.Structure):
+    """Mirror of the C struct snls_norm_params."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("C", ctypes.c_int32), ("frames", ctypes.c_int64),
+                ("pixels", ctypes.c_int64), ("eps", ctypes.c_float), ("drop", ctypes.c_float),
+                ("site", ctypes.c_uint32)]
+
+
+class SnlsRotateParams(ctypes.Structure):
+    """Mirror of the C struct snls_rotate_params."""
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("B", "T", "C", "H", "W", "HD")
+    ] + [("pairs", ctypes.c_int32 * 3), ("theta", ctypes.c_float * 3)] + [
+        (n, ctypes.c_int32) for n in ("interleaved", "row0", "col0")]
+
+
+class SnlsProjectParams(ctypes.Structure):
+    """Mirror of the C struct snls_project_params."""
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("cin", "cout", "parts")] + [
+        ("frames", ctypes.c_int64), ("pixels", ctypes.c_int64)]
 
 
 class SnlsError(RuntimeError):
@@ -97,6 +124,16 @@ def load_library():
         lib.snls_cache_store.argtypes = [P, P, P, PC, P, P, P, P, P]
         lib.snls_cache_attend.argtypes = [P] * 8 + [PC, PB, I32, F32, P, P]
         lib.snls_cache_attend_points.argtypes = [P, P, I64] + [P] * 7 + [PC, PB, I32, F32, P, P]
+        PN, PR, PJ = (ctypes.POINTER(c) for c in (SnlsNormParams, SnlsRotateParams, SnlsProjectParams))
+        lib.snls_norm.argtypes = [P] * 5 + [PN, P, P, P, P]
+        lib.snls_norm_backward.argtypes = [P] * 6 + [PN, P, P, P, P, P, SZ, P]
+        lib.snls_norm_workspace_size.argtypes = [PN]
+        lib.snls_norm_workspace_size.restype = SZ
+        lib.snls_dropout.argtypes = [P, P, P, I64, F32, ctypes.c_uint32, P, P]
+        lib.snls_rotate.argtypes = [P, P, P, PR, I32, P, P, P]
+        lib.snls_rotate_points.argtypes = [P, P, I64, P, PR, I32, P, P]
+        lib.snls_project_pack.argtypes = [P, PJ, P, P, P]
+        lib.snls_project.argtypes = [P, P, P, P, PJ, P, P]
         lib.snls_workspace_size.argtypes = [ctypes.c_int, PP]
         lib.snls_workspace_size.restype = SZ
         lib.snls_status_string.argtypes = [ctypes.c_int]
@@ -105,7 +142,9 @@ def load_library():
         for f in ("snls_search", "snls_topk", "snls_aggregate", "snls_backward", "snls_abi_version",
                   "snls_aggregate_stacked", "snls_chain_flows", "snls_aggregate_static", "snls_gather_stacked",
                   "snls_stacked_reduce", "snls_gather_reduce", "snls_bias", "snls_bias_backward",
-                  "snls_backward_scores", "snls_cache_store", "snls_cache_attend", "snls_cache_attend_points"):
+                  "snls_backward_scores", "snls_cache_store", "snls_cache_attend", "snls_cache_attend_points",
+                  "snls_norm", "snls_norm_backward", "snls_dropout", "snls_rotate", "snls_rotate_points",
+                  "snls_project_pack", "snls_project"):
             getattr(lib, f).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -605,4 +644,207 @@ def snls_cache_attend_points(q, points, flows, ages, cache, cp: dict, ws: int, s
     _check(lib.snls_cache_attend_points(_ptr(q), _ptr(points), n, _ptr(flows), _ptr(ages), *ptrs, _ptr(table),
                                         ctypes.byref(prm), bp, int(ws), float(scale), _ptr(out), _stream(stream)),
            "snls_cache_attend_points")
+    return out
+
+
+# ------------------------------------------------- norm, dropout, around a layer --
+
+_NORM_SIZE = ctypes.sizeof(SnlsNormParams)
+
+
+def _features(t, name):
+    """frames, C, pixels of features (..., C, H, W), or of n tokens (n, C), and the shape of a value a pixel."""
+    _dev(t, name)
+    s = t.shape
+    if len(s) == 2:
+        return s[0], s[1], 1, (s[0],)
+    if len(s) < 3:
+        raise ValueError("%s must be (..., C, H, W) or (n, C)" % name)
+    frames = 1
+    for n in s[:-3]:
+        frames *= n
+    return frames, s[-3], s[-2] * s[-1], tuple(s[:-3]) + tuple(s[-2:])
+
+
+def _per_channel(C, **tensors):
+    for n, t in tensors.items():
+        if t is not None:
+            _dev(t, n, (C,))
+
+
+def _rng(rng, drop):
+    """Address of a generator's state, a tensor of two int64: seed and step."""
+    if rng is None:
+        if drop > 0:
+            raise ValueError("dropout needs rng, a tensor of two int64 (seed, step)")
+        return None
+    return _dev_as(rng, "rng", (2,), (torch.int64, torch.uint64)).data_ptr()
+
+
+def snls_norm(x, gamma=None, beta=None, eps: float = 1e-5, branch=None, drop: float = 0.0, rng=None, site: int = 0,
+              y=None, total=None, stats=None, stream=None):
+    """Layer norm over the channels of features (..., C, H, W) or tokens (n, C), of x or of the residual sum
+    x + dropout(branch); returns (y, total, stats), total being x without branch.  rng: two int64 on the GPU, seed
+    and step."""
+    lib = load_library()
+    frames, C, pixels, px = _features(x, "x")
+    _per_channel(C, gamma=gamma, beta=beta)
+    if branch is not None:
+        _dev(branch, "branch", x.shape)
+        total = _dev(total, "total", x.shape) if total is not None else _new(x.shape, x, stream)
+    elif total is not None:
+        raise ValueError("total goes with branch")
+    y = _dev(y, "y", x.shape) if y is not None else _new(x.shape, x, stream)
+    stats = _dev(stats, "stats", (2,) + px) if stats is not None else _new((2,) + px, x, stream)
+    _here(x, gamma, beta, branch, rng, y, total, stats)
+    prm = SnlsNormParams(_NORM_SIZE, C, frames, pixels or 1, float(eps), float(drop), int(site))
+    if pixels:
+        _check(lib.snls_norm(_ptr(x), _ptr(branch), _rng(rng, drop), _ptr(gamma), _ptr(beta), ctypes.byref(prm),
+                             _ptr(total), _ptr(y), _ptr(stats), _stream(stream)), "snls_norm")
+    return y, x if branch is None else total, stats
+
+
+def snls_norm_backward(grad_y, total, stats, gamma=None, grad_total=None, drop: float = 0.0, rng=None, site: int = 0,
+                       weights: bool = True, grad_x=None, grad_branch=None, workspace=None, stream=None):
+    """Gradients of snls_norm: (grad_x, grad_branch, grad_gamma, grad_beta); grad_branch is grad_x when nothing is
+    dropped, the last two are None for weights=False."""
+    lib = load_library()
+    frames, C, pixels, px = _features(total, "total")
+    _dev(grad_y, "grad_y", total.shape)
+    _dev(stats, "stats", (2,) + px)
+    _per_channel(C, gamma=gamma)
+    if grad_total is not None:
+        _dev(grad_total, "grad_total", total.shape)
+    grad_x = _dev(grad_x, "grad_x", total.shape) if grad_x is not None else _new(total.shape, total, stream)
+    if grad_branch is not None:
+        _dev(grad_branch, "grad_branch", total.shape)
+    elif drop > 0:
+        grad_branch = _new(total.shape, total, stream)
+    prm = SnlsNormParams(_NORM_SIZE, C, frames if pixels else 0, pixels or 1, 0.0, float(drop), int(site))
+    gg, gb, room = None, None, (None, 0)
+    if weights:
+        gg, gb = _new((C,), total, stream), _new((C,), total, stream)
+        if workspace is None:
+            need = lib.snls_norm_workspace_size(ctypes.byref(prm))
+            if need == ctypes.c_size_t(-1).value:
+                raise SnlsError(SNLS_ERR_INVALID_ARG, "snls_norm_workspace_size")
+            workspace = _new(((need + 3) // 4,), total, stream)
+        room = _room(workspace)
+    _here(grad_y, total, stats, gamma, grad_total, rng, grad_x, grad_branch, workspace)
+    _check(lib.snls_norm_backward(_ptr(grad_y), _ptr(grad_total), _ptr(total), _ptr(stats), _ptr(gamma),
+                                  _rng(rng, drop), ctypes.byref(prm), _ptr(grad_x), _ptr(grad_branch), _ptr(gg),
+                                  _ptr(gb), *room, _stream(stream)), "snls_norm_backward")
+    return grad_x, grad_x if grad_branch is None else grad_branch, gg, gb
+
+
+def snls_dropout(x, rng, drop: float, site: int = 0, residual=None, out=None, stream=None):
+    """dropout(x), or residual + dropout(x); applied to a gradient it is its own backward pass.  out may be x or
+    residual."""
+    lib = load_library()
+    _dev(x, "x")
+    if residual is not None:
+        _dev(residual, "residual", x.shape)
+    out = _dev(out, "out", x.shape) if out is not None else _new(x.shape, x, stream)
+    _here(x, residual, rng, out)
+    _check(lib.snls_dropout(_ptr(x), _ptr(residual), _rng(rng, drop), x.numel(), float(drop), int(site), _ptr(out),
+                            _stream(stream)), "snls_dropout")
+    return out
+
+
+# ------------------------------------------------------------- rotary positions --
+
+_ROTATE_SIZE, _Int3, _Float3 = ctypes.sizeof(SnlsRotateParams), ctypes.c_int32 * 3, ctypes.c_float * 3
+
+
+def rotate_from_dict(rp: dict) -> SnlsRotateParams:
+    if len(rp["pairs"]) != 3 or len(rp["theta"]) != 3:
+        raise ValueError("pairs and theta have three entries: time, row, column")
+    return SnlsRotateParams(_ROTATE_SIZE, int(rp["B"]), int(rp["T"]), int(rp["C"]), int(rp["H"]), int(rp["W"]),
+                            int(rp["HD"]), _Int3(*rp["pairs"]), _Float3(*rp["theta"]),
+                            int(rp.get("interleaved", 0)), int(rp.get("row0", 0)), int(rp.get("col0", 0)))
+
+
+def snls_rotate(q, k, rp: dict, times=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotary positions of videos q and k (None for q alone); returns (q_out, k_out).  times: int64 (B, T), or None
+    for 0 .. T-1.  inverse: the gradients of q and k from those of the outputs.  Outputs may be q and k."""
+    lib = load_library()
+    shp = video_shape(rp)
+    _dev(q, "q", shp)
+    q_out = _dev(q_out, "q_out", shp) if q_out is not None else _new(shp, q, stream)
+    if k is not None:
+        _dev(k, "k", shp)
+        k_out = _dev(k_out, "k_out", shp) if k_out is not None else _new(shp, k, stream)
+    elif k_out is not None:
+        raise ValueError("k_out goes with k")
+    if times is not None:
+        _dev_as(times, "times", (rp["B"], rp["T"]), (torch.int64,))
+    _here(q, k, times, q_out, k_out)
+    prm = rotate_from_dict(rp)
+    _check(lib.snls_rotate(_ptr(q), _ptr(k), _ptr(times), ctypes.byref(prm), int(inverse), _ptr(q_out), _ptr(k_out),
+                           _stream(stream)), "snls_rotate")
+    return q_out, k_out
+
+
+def snls_rotate_points(q, points, rp: dict, times=None, inverse: bool = False, out=None, stream=None):
+    """The same for tokens q (n, C) at points int32 (n, 3) = video, row, column; times int64 (B), or None for 0."""
+    lib = load_library()
+    _dev(q, "q")
+    n = q.shape[0]
+    _dev(q, "q", (n, rp["C"]))
+    _dev_as(points, "points", (n, 3), (torch.int32,))
+    if times is not None:
+        _dev_as(times, "times", (rp["B"],), (torch.int64,))
+    out = _dev(out, "out", (n, rp["C"])) if out is not None else _new((n, rp["C"]), q, stream)
+    _here(q, points, times, out)
+    prm = rotate_from_dict(rp)
+    _check(lib.snls_rotate_points(_ptr(q), _ptr(points), n, _ptr(times), ctypes.byref(prm), int(inverse), _ptr(out),
+                                  _stream(stream)), "snls_rotate_points")
+    return out
+
+
+# ------------------------------------------------------------- 8-bit projections --
+
+_PROJECT_SIZE = ctypes.sizeof(SnlsProjectParams)
+
+
+def snls_project_pack(w, codes=None, scales=None, stream=None):
+    """Weights (cout, cin) as int8 codes and a scale per output channel: (codes, scales)."""
+    lib = load_library()
+    _dev(w, "w")
+    if w.dim() != 2:
+        raise ValueError("w must be (cout, cin)")
+    cout, cin = w.shape
+    if codes is None:
+        codes = torch.empty(w.shape, device=w.device, dtype=torch.int8)
+        if stream is not None:
+            codes.record_stream(stream)
+    _dev_as(codes, "codes", w.shape, (torch.int8,))
+    scales = _dev(scales, "scales", (cout,)) if scales is not None else _new((cout,), w, stream)
+    _here(w, codes, scales)
+    prm = SnlsProjectParams(_PROJECT_SIZE, cin, cout, 1, 0, 1)
+    _check(lib.snls_project_pack(_ptr(w), ctypes.byref(prm), _ptr(codes), _ptr(scales), _stream(stream)),
+           "snls_project_pack")
+    return codes, scales
+
+
+def snls_project(x, codes, scales, bias=None, parts: int = 1, out=None, stream=None):
+    """Product of features (..., cin, H, W) or tokens (n, cin) with 8-bit weights (cout, cin); returns
+    (parts, ..., cout / parts, H, W) or (parts, n, cout / parts): parts tensors, one after the other."""
+    lib = load_library()
+    frames, cin, pixels, _ = _features(x, "x")
+    if not isinstance(codes, torch.Tensor) or codes.dim() != 2:
+        raise ValueError("codes must be (cout, cin)")
+    cout, parts = codes.shape[0], int(parts)
+    _dev_as(codes, "codes", (cout, cin), (torch.int8,))
+    _per_channel(cout, scales=scales, bias=bias)
+    if parts < 1 or cout % parts:
+        raise ValueError("parts must divide cout")
+    tail = (cout // parts,) + tuple(x.shape[-2:]) if x.dim() > 2 else (cout // parts,)
+    shp = (parts,) + tuple(x.shape[:-3] if x.dim() > 2 else x.shape[:1]) + tail
+    out = _dev(out, "out", shp) if out is not None else _new(shp, x, stream)
+    _here(x, codes, scales, bias, out)
+    prm = SnlsProjectParams(_PROJECT_SIZE, cin, cout, parts, frames, pixels or 1)
+    if pixels:
+        _check(lib.snls_project(_ptr(x), _ptr(codes), _ptr(scales), _ptr(bias), ctypes.byref(prm), _ptr(out),
+                                _stream(stream)), "snls_project")
     return out
