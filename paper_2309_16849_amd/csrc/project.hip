@@ -29,29 +29,188 @@ struct Quant {
   }
 };
 
-// 64 pixels (or tokens) a workgroup: a thread quantises one into LDS and sums
-// its products.
-__global__ void __launch_bounds__(64) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
-                                                     const float* __restrict__ scales, const float* __restrict__ bias,
-                                                     snls_project_params p, float* __restrict__ out) {
-  extern __shared__ int8_t codes[];
-  const long long P = p.pixels, px = p.frames * P;
-  const int per = p.cout / p.parts;
-  for (long long i0 = blockIdx.x * 64LL; i0 < px; i0 += gridDim.x * 64LL) {
-    const long long i = i0 + threadIdx.x;
-    if (i >= px) continue;
-    const long long f = i / P, at = f * p.cin * P + (i - f * P);
-    unsigned most = 0;
-    for (int c = 0; c < p.cin; ++c) most = max(most, magnitude(x[at + c * P]));
-    const Quant q(most);
-    const bool ok = most < kInfBits;
-    for (int c = 0; c < p.cin; ++c) codes[c * 64 + threadIdx.x] = ok ? (int8_t)q.code(x[at + c * P]) : 0;
-    for (int o = 0; o < p.cout; ++o) {
-      int acc = 0;
-      for (int c = 0; c < p.cin; ++c) acc += (int)codes[c * 64 + threadIdx.x] * (int)w[(long long)o * p.cin + c];
-      const int part = o / per;
-      const long long to = (((long long)part * p.frames + f) * per + (o - part * per)) * P + (i - f * P);
-      out[to] = fmaf((float)acc * q.s, scales[o], bias ? bias[o] : 0.f);
+typedef int Int4 __attribute__((ext_vector_type(4)));
+typedef int Int16 __attribute__((ext_vector_type(16)));
+
+// A call's sizes on the device.  span: tiles of 32 output channels a workgroup
+// takes; hold: of these, how many lie in LDS at a time.
+struct ProjectGeo {
+  long long px, P, groups;  // pixels in all, of a frame; groups of 128 of them
+  long long F;              // frames
+  int cin, cout, per;       // per: output channels of a part
+  int span, hold;
+};
+
+// What the epilogue needs of an output channel: where its plane starts (a
+// token's: its place in the row), scale and bias.
+struct OutChannel {
+  long long at;
+  float scale, bias;
+};
+
+// 16 consecutive weights of a channel as a lane of the matrix instruction takes
+// them; 0 behind the last channel of either side.
+SNLS_DEV Int4 weights16(const int8_t* __restrict__ w, int o, int c, const ProjectGeo& g) {
+  Int4 v = {0, 0, 0, 0};
+  if (o >= g.cout || c >= g.cin) return v;
+  const int8_t* from = w + (long long)o * g.cin + c;
+  if (c + 16 <= g.cin && !((uintptr_t)from & 15)) return *reinterpret_cast<const Int4*>(from);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const unsigned b = c + i < g.cin ? (unsigned)(uint8_t)from[i] : 0u;
+    v[i / 4] = (int)((unsigned)v[i / 4] | b << (8 * (i % 4)));
+  }
+  return v;
+}
+
+// The product on the matrix cores, 32 x 32 outputs an instruction over 32
+// channels: the weights' tile is one operand, the codes of 32 pixels the other.
+// Both give a lane 16 consecutive channels of one row (lane mod 32; the upper
+// lanes have the upper 16), so a lane loads its pixel's channels, finds the
+// largest with its partner and packs the codes where the instruction wants them:
+// they never leave the registers.  The weights lie in LDS in the order of the
+// lanes.  NK: steps of 32 channels.  TOK: a list of tokens (pixels == 1), whose
+// rows and columns change places so that stores run along the output channels.
+// Up to KEEP steps, the values stay in registers between the maximum and the
+// codes; beyond, they are read again.
+template <int NK, bool TOK>
+__global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
+                                                      const float* __restrict__ scales,
+                                                      const float* __restrict__ bias, ProjectGeo g,
+                                                      float* __restrict__ out) {
+  extern __shared__ char lds[];
+  constexpr bool KEEP = NK <= 8;
+  Int4* const wt = reinterpret_cast<Int4*>(lds);
+  OutChannel* const chan = reinterpret_cast<OutChannel*>(lds + g.hold * NK * 1024);
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, wv = threadIdx.x >> 6;
+  const int tiles = (g.cout + 31) / 32, t0 = blockIdx.y * g.span, t1 = min(t0 + g.span, tiles);
+  const bool once = t1 - t0 <= g.hold;
+
+  // tiles [from, to) into LDS
+  auto stage = [&](int from, int to) {
+    const int n = (to - from) * NK * 64;
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const int l = i & 63, ks = (i >> 6) % NK, t = from + (i >> 6) / NK;
+      wt[i] = weights16(w, t * 32 + (l & 31), ks * 32 + (l >> 5) * 16, g);
+    }
+    for (int i = threadIdx.x; i < (to - from) * 32; i += 256) {
+      const int o = from * 32 + i;
+      if (o < g.cout) {
+        const int part = o / g.per;
+        chan[i] = TOK ? OutChannel{(long long)part * g.F * g.per + (o - part * g.per), scales[o], bias ? bias[o] : 0.f}
+                      : OutChannel{(o + part * (g.F - 1) * g.per) * g.P, scales[o], bias ? bias[o] : 0.f};
+      }
+    }
+  };
+
+  if (once) {
+    stage(t0, t1);
+    __syncthreads();
+  }
+  for (long long grp = blockIdx.x; grp < g.groups; grp += gridDim.x) {
+    const long long i0 = grp * 128 + wv * 32;
+    const bool any = i0 < g.px;  // of this wave
+    const bool mine = i0 + col < g.px;
+    long long f = 0, p = 0;
+    Int4 codes[NK];
+    float ts = 0.f;
+    if (any) {
+      const long long f0 = TOK ? i0 : i0 / g.P;
+      const unsigned rel = TOK ? 0 : (unsigned)(i0 - f0 * g.P) + (mine ? col : 0);
+      f = TOK ? i0 + (mine ? col : 0) : f0 + rel / (unsigned)g.P;
+      p = TOK ? 0 : rel % (unsigned)g.P;
+      const long long step = TOK ? 1 : g.P;
+      const float* const first = x + f * g.cin * g.P + p;  // channel 0 of this lane's pixel
+      int upper = half * 16;
+      asm volatile("" : "+v"(upper));  // (else every guard below is held in registers across the groups)
+      // this lane's 16 channels of step ks
+      auto load16 = [&](int ks, float* v) {
+        const int c = ks * 32 + upper;
+        if (ks * 32 + 32 <= g.cin) {
+          const float* from = first + c * step;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = from[j * step];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float u = first[min(c + j, g.cin - 1) * step];
+            v[j] = c + j < g.cin ? u : 0.f;
+          }
+        }
+      };
+      unsigned most = 0;
+      float v[KEEP ? NK * 16 : 16];
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) load16(ks, v + ks * 16);
+#pragma unroll
+        for (int j = 0; j < NK * 16; ++j) most = max(most, magnitude(v[j]));
+      } else {
+#pragma unroll 1
+        for (int ks = 0; ks < NK; ++ks) {
+          load16(ks, v);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) most = max(most, magnitude(v[j]));
+        }
+      }
+      most = max(most, (unsigned)__shfl_xor((int)most, 32));
+      const bool ok = most < kInfBits;
+      const Quant q(most);
+      ts = q.s;
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        if constexpr (!KEEP) {
+          __builtin_amdgcn_sched_barrier(0);  // one step's values at a time: all at once do not fit
+          load16(ks, v);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          unsigned u = 0;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) u |= ((unsigned)q.code(v[(KEEP ? ks * 16 : 0) + j * 4 + b]) & 0xffu) << (8 * b);
+          codes[ks][j] = ok ? (int)u : 0;
+        }
+      }
+    }
+    for (int from = t0; from < t1; from += g.hold) {
+      const int to = min(from + g.hold, t1);
+      if (!once) {
+        __syncthreads();
+        stage(from, to);
+        __syncthreads();
+      }
+      if (!any) continue;
+      for (int t = from; t < to; ++t) {
+        Int16 acc = {};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+          const Int4 a = wt[((t - from) * NK + ks) * 64 + lane];
+          acc = TOK ? __builtin_amdgcn_mfma_i32_32x32x32_i8(codes[ks], a, acc, 0, 0, 0)
+                    : __builtin_amdgcn_mfma_i32_32x32x32_i8(a, codes[ks], acc, 0, 0, 0);
+        }
+        // register r: row 8 * (r / 4) + 4 * half + r % 4, column lane mod 32
+        if constexpr (TOK) {
+          const OutChannel ch = chan[(t - from) * 32 + col];
+          float* const to_row = out + ch.at + (i0 + 4 * half) * g.per;
+          const int rows = t * 32 + col < g.cout ? (int)min(32LL, g.px - i0) - 4 * half : 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r / 4) + r % 4;
+            const float s = __shfl(ts, row + 4 * half);
+            if (row < rows) to_row[(long long)row * g.per] = fmaf((float)acc[r] * s, ch.scale, ch.bias);
+          }
+        } else {
+          float* const to_px = out + f * g.per * g.P + p;
+          const OutChannel* const ch = chan + (t - from) * 32 + 4 * half;
+          const int rows = mine ? g.cout - t * 32 - 4 * half : 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r / 4) + r % 4;
+            const OutChannel c = ch[row];
+            if (row < rows) to_px[c.at] = fmaf((float)acc[r] * ts, c.scale, c.bias);
+          }
+        }
+      }
     }
   }
 }
@@ -74,11 +233,43 @@ snls_status launch_project_pack(const float* w, int cin, int cout, int8_t* codes
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
+template <int NK>
+static void run_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
+                        const ProjectGeo& g, bool tokens, dim3 grid, float* out, hipStream_t s) {
+  const size_t lds = (size_t)g.hold * (NK * 1024 + 32 * sizeof(OutChannel));
+  if (tokens)
+    hipLaunchKernelGGL((project_kernel<NK, true>), grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
+  else
+    hipLaunchKernelGGL((project_kernel<NK, false>), grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
+}
+
 snls_status launch_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
                            const snls_project_params& pp, float* out, hipStream_t s) {
-  const long long groups = (pp.frames * pp.pixels + 63) / 64;
-  hipLaunchKernelGGL(project_kernel, dim3((unsigned)(groups < 16384 ? groups : 16384)), dim3(64), 64 * pp.cin, s, x,
-                     codes, scales, bias, pp, out);
+  const int steps = (pp.cin + 31) / 32;
+  const int nk = steps <= 4 ? steps : steps <= 6 ? 6 : steps <= 8 ? 8 : steps <= 16 ? 16 : 32;
+  ProjectGeo g;
+  g.px = pp.frames * pp.pixels, g.P = pp.pixels, g.F = pp.frames;
+  g.groups = (g.px + 127) / 128;
+  g.cin = pp.cin, g.cout = pp.cout, g.per = pp.cout / pp.parts;
+  const int tiles = (pp.cout + 31) / 32;
+  // few pixels: the output channels are shared out too, until the chip has two workgroups a CU
+  const long long want = (512 + g.groups - 1) / g.groups;
+  const int split = (int)(want < tiles ? want : tiles);
+  g.span = (tiles + split - 1) / split;
+  const int fit = 60 / nk;  // 60 KB of weights
+  g.hold = g.span < fit ? g.span : fit;
+  const dim3 grid((unsigned)(g.groups < 1280 ? g.groups : 1280), (unsigned)((tiles + g.span - 1) / g.span));
+  const bool tokens = pp.pixels == 1;
+  switch (nk) {
+    case 1: run_project<1>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 2: run_project<2>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 3: run_project<3>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 4: run_project<4>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 6: run_project<6>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 8: run_project<8>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 16: run_project<16>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    default: run_project<32>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+  }
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
