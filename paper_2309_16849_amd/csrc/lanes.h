@@ -1,0 +1,45 @@
+// lanes.h -- runs of consecutive floats that a lane loads and stores at once
+// (device side), at any 4-byte address.
+#pragma once
+
+#include "snls_internal.h"
+
+#ifdef __HIPCC__
+
+namespace snls {
+
+template <int V>
+struct __attribute__((packed, aligned(4))) Run {
+  float v[V];
+};
+
+// The first cnt of V floats at `from`, 0 for the others.
+template <int V>
+SNLS_DEV void load_run(const float* from, int cnt, float* to) {
+  if (cnt >= V) {
+    const Run<V> r = *reinterpret_cast<const Run<V>*>(from);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = i < cnt ? from[i] : 0.f;
+  }
+}
+
+template <int V>
+SNLS_DEV void store_run(float* to, int cnt, const float* from) {
+  if (cnt >= V) {
+    Run<V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = from[i];
+    *reinterpret_cast<Run<V>*>(to) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < cnt) to[i] = from[i];
+  }
+}
+
+}  // namespace snls
+
+#endif  // __HIPCC__

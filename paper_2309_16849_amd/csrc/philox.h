@@ -37,11 +37,23 @@ struct Philox {
     }
     return {{c0, c1, c2, c3}};
   }
-  // Word of element i.
-  SNLS_DEV unsigned word(long long i) const {
-    const Words b = block(i >> 2);
+  // Words of elements i .. i+V-1, V = 1, 2 or 4.
+  template <int V>
+  SNLS_DEV void run(long long i, unsigned* w) const {
     const int j = (int)(i & 3);
-    return j == 0 ? b.w[0] : j == 1 ? b.w[1] : j == 2 ? b.w[2] : b.w[3];
+    const Words a = block(i >> 2);
+    if constexpr (V == 1) {
+      w[0] = j == 0 ? a.w[0] : j == 1 ? a.w[1] : j == 2 ? a.w[2] : a.w[3];
+    } else if (j + V <= 4) {
+#pragma unroll
+      for (int n = 0; n < V; ++n) w[n] = V == 2 && j == 1 ? a.w[n + 1] : V == 2 && j == 2 ? a.w[n + 2] : a.w[n];
+    } else {
+      const Words b = block((i >> 2) + 1);
+#pragma unroll
+      for (int n = 0; n < V; ++n)
+        w[n] = j == 1 ? (n < 3 ? a.w[n + 1 & 3] : b.w[0])
+                      : j == 2 ? (n < 2 ? a.w[n + 2 & 3] : b.w[n - 2 & 3]) : (n < 1 ? a.w[3] : b.w[n - 1 & 3]);
+    }
   }
 };
 
