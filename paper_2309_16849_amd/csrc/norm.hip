@@ -4,6 +4,7 @@
 
 #include "lanes.h"
 #include "philox.h"
+#include "row16.h"
 
 namespace snls {
 
@@ -102,6 +103,44 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
       store_run<V>(stats + (g.frames + f) * g.P + (cnt > 0 ? p : 0), cnt, rstd);
     }
   }
+}
+
+// One step of the sum of a list over the lanes: a lane with bit M set goes on
+// with b, the others with a, each plus what its partner (lane ^ M) has of it.
+template <int M>
+SNLS_DEV float halve(float a, float b, int lane) {
+  if constexpr (M >= 16) {
+    // the rows of a whose lanes have the bit change places with those of b whose
+    // lanes have not
+    const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+    const auto r = M == 32 ? __builtin_amdgcn_permlane32_swap(ua, ub, false, false)
+                           : __builtin_amdgcn_permlane16_swap(ua, ub, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    const bool up = lane & M;
+    const float give = up ? a : b, keep = up ? b : a;
+    return keep + __uint_as_float(grp_xor<M>(__float_as_uint(give), lane & 15));
+  }
+}
+
+// Sums over the 64 lanes of LEN values each (a power of two up to 64): lane l
+// returns that of value `listed<LEN>(l)`.
+template <int LEN, int M = 32>
+SNLS_DEV float list_sum(float* v, int lane) {
+  if constexpr (M == 0) {
+    return v[0];
+  } else if constexpr (LEN > 1) {
+#pragma unroll
+    for (int i = 0; i < LEN / 2; ++i) v[i] = halve<M>(v[i], v[i + LEN / 2], lane);
+    return list_sum<LEN / 2, M / 2>(v, lane);
+  } else {
+    v[0] += __uint_as_float(grp_xor<M>(__float_as_uint(v[0]), lane & 15));
+    return list_sum<1, M / 2>(v, lane);
+  }
+}
+template <int LEN>
+SNLS_DEV int listed(int lane) {
+  return lane / (64 / LEN);
 }
 
 // Sum over the G lanes of a group.
@@ -212,6 +251,191 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
   }
 }
 
+// Gradients of frames: tiles, waves and channels as in the forward pass.  Both
+// the scaled gradients and the normalised values stay in registers, one join of
+// two sums a tile.  A workgroup walks every gridDim.x-th tile; a wave sums its
+// channels' 2 R terms over the tile's pixels, so that each of its lanes is left
+// with one of the sums, which it adds up over the tiles in 64 bits, and a
+// workgroup writes one row of partial sums.
+template <int V, int R, bool HOLD>
+__global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_y, const float* grad_total,
+                                                              const float* __restrict__ total,
+                                                              const float* __restrict__ stats,
+                                                              const float* __restrict__ gamma, Drop d, NormGeo g,
+                                                              float* grad_x, float* grad_branch,
+                                                              double* __restrict__ sums) {
+  extern __shared__ float part[];  // two tables of two rows a wave, taken in turn
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Philox gen(d);
+  const int c0 = wv * g.n, n = min(g.n, g.C - c0);
+  double acc = 0.0;  // this lane's of the wave's 2 R sums
+  float over[2 * R] = {};
+  int turn = 0;
+  for (long long tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+    const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
+    const int cnt = (int)max(0LL, min((long long)V, g.P - p));
+    const long long px = f * g.P + (cnt > 0 ? p : 0), at = (f * g.C + c0) * g.P + (cnt > 0 ? p : 0);
+    float mean[V], rstd[V], gy[R][V], xh[R][V], sum[2][V] = {};
+    if constexpr (!HOLD)
+#pragma unroll
+      for (int c = 0; c < 2 * R; ++c) over[c] = 0.f;
+#pragma unroll
+    for (int c = 0; c < R; ++c)
+      if (c < n) {
+        load_run<V>(grad_y + at + c * g.P, cnt, gy[c]);
+        load_run<V>(total + at + c * g.P, cnt, xh[c]);
+      }
+    load_run<V>(stats + px, cnt, mean);
+    load_run<V>(stats + g.frames * g.P + px, cnt, rstd);
+#pragma unroll
+    for (int c = 0; c < R; ++c)
+      if (c < n) {
+        const float ga = gamma ? gamma[c0 + c] : 1.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xh[c][j] = (xh[c][j] - mean[j]) * rstd[j];
+          over[c] = fmaf(gy[c][j], xh[c][j], over[c]);
+          over[R + c] += gy[c][j];
+          gy[c][j] *= ga;
+          sum[0][j] += gy[c][j];
+          sum[1][j] = fmaf(gy[c][j], xh[c][j], sum[1][j]);
+        }
+      }
+    if constexpr (!HOLD)
+      if (sums) acc += (double)list_sum<2 * R>(over, lane);
+    if (waves > 1) {
+      float* const rows = part + turn * 2 * waves * V * 64;
+      turn ^= 1;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        rows[(wv * V + j) * 64 + lane] = sum[0][j];
+        rows[((waves + wv) * V + j) * 64 + lane] = sum[1][j];
+        sum[0][j] = sum[1][j] = 0.f;
+      }
+      __syncthreads();
+      for (int w = 0; w < waves; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          sum[0][j] += rows[(w * V + j) * 64 + lane];
+          sum[1][j] += rows[((waves + w) * V + j) * 64 + lane];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[0][j] /= g.C, sum[1][j] /= g.C;
+#pragma unroll
+    for (int c = 0; c < R; ++c)
+      if (c < n) {
+        const long long e = at + c * g.P;
+        float r[V], t[V];
+        if (grad_total) load_run<V>(grad_total + e, cnt, t);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          r[j] = rstd[j] * (gy[c][j] - sum[0][j] - xh[c][j] * sum[1][j]);
+          if (grad_total) r[j] += t[j];
+        }
+        store_run<V>(grad_x + e, cnt, r);
+        if (grad_branch) {
+          if (d.rng) {
+            unsigned w[V];
+            gen.run<V>(e, w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[j] = dropped(r[j], w[j], d);
+          }
+          store_run<V>(grad_branch + e, cnt, r);
+        }
+      }
+  }
+  if (!sums) return;
+  if constexpr (HOLD) acc = (double)list_sum<2 * R>(over, lane);
+  const int which = listed<2 * R>(lane), c = which % R;
+  if (lane % (32 / R) == 0 && c < n) sums[((long long)blockIdx.x * 2 + which / R) * g.C + c0 + c] = acc;
+}
+
+// Gradients of tokens: G lanes a token, as in the forward pass; a workgroup
+// walks rows and keeps its channels' sums, joined over its groups at the end.
+template <int G, int N>
+__global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_y, const float* grad_total,
+                                                              const float* __restrict__ total,
+                                                              const float* __restrict__ stats,
+                                                              const float* __restrict__ gamma, Drop d, NormGeo g,
+                                                              float* grad_x, float* grad_branch,
+                                                              double* __restrict__ sums) {
+  __shared__ float rows[2][256 / G][G * N * 4];
+  const int l = threadIdx.x & (G - 1), group = threadIdx.x / G;
+  const Philox gen(d);
+  float acc[2][N][4] = {}, ga[N][4];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int c = (k * G + l) * 4, cnt = max(0, min(4, g.C - c));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ga[k][j] = 1.f;
+    if (gamma && cnt > 0) load_run<4>(gamma + c, cnt, ga[k]);
+  }
+  for (long long row = blockIdx.x * (256LL / G) + group; row < g.frames; row += gridDim.x * (256LL / G)) {
+    const long long at = row * g.C;
+    const float mean = stats[row], rstd = stats[g.frames + row];
+    float gy[N][4], xh[N][4], s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (k * G + l) * 4, cnt = max(0, min(4, g.C - c));
+      load_run<4>(grad_y + at + (cnt > 0 ? c : 0), cnt, gy[k]);
+      load_run<4>(total + at + (cnt > 0 ? c : 0), cnt, xh[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = (k * G + l) * 4 + j < g.C;
+        xh[k][j] = in ? (xh[k][j] - mean) * rstd : 0.f;
+        acc[0][k][j] = fmaf(gy[k][j], xh[k][j], acc[0][k][j]);
+        acc[1][k][j] += gy[k][j];
+        gy[k][j] *= ga[k][j];
+        s0 += gy[k][j];
+        s1 = fmaf(gy[k][j], xh[k][j], s1);
+      }
+    s0 = group_sum<G>(s0) / g.C, s1 = group_sum<G>(s1) / g.C;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (k * G + l) * 4, cnt = min(4, g.C - c);
+      if (cnt <= 0) continue;
+      float r[4], t[4] = {};
+      if (grad_total) load_run<4>(grad_total + at + c, cnt, t);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        r[j] = rstd * (gy[k][j] - s0 - xh[k][j] * s1);
+        if (grad_total) r[j] += t[j];
+      }
+      store_run<4>(grad_x + at + c, cnt, r);
+      if (grad_branch) {
+        if (d.rng) {
+          unsigned w[4];
+          gen.run<4>(at + c, w);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) r[j] = dropped(r[j], w[j], d);
+        }
+        store_run<4>(grad_branch + at + c, cnt, r);
+      }
+    }
+  }
+  if (!sums) return;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      rows[0][group][(k * G + l) * 4 + j] = acc[0][k][j];
+      rows[1][group][(k * G + l) * 4 + j] = acc[1][k][j];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * g.C; i += 256) {
+    const int which = i >= g.C, c = i - which * g.C;
+    double s = 0.0;
+    for (int k = 0; k < 256 / G; ++k) s += (double)rows[which][k][c];
+    sums[(long long)blockIdx.x * 2 * g.C + i] = s;
+  }
+}
+
+// More channels than registers hold.
 // A thread per pixel: gradients of the input and the branch.
 __global__ void __launch_bounds__(256) norm_grad_kernel(const float* grad_y, const float* grad_total,
                                                         const float* __restrict__ total,
@@ -272,29 +496,69 @@ __global__ void __launch_bounds__(256) norm_weights_kernel(const float* __restri
   if (threadIdx.x < 2) part[((long long)blockIdx.y * 2 + threadIdx.x) * C + c] = sums[threadIdx.x][0];
 }
 
-__global__ void __launch_bounds__(256) norm_weights_sum_kernel(const double* __restrict__ part, int slices, int C,
-                                                               float* __restrict__ grad_gamma,
-                                                               float* __restrict__ grad_beta) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= 2 * C) return;
+// The 2 C sums of all slices: 8 entries a workgroup, 128 lanes in turn over the
+// slices of each.
+constexpr int kEntries = 8;
+__global__ void __launch_bounds__(1024) norm_weights_sum_kernel(const double* __restrict__ part, int slices, int C,
+                                                                float* __restrict__ grad_gamma,
+                                                                float* __restrict__ grad_beta) {
+  __shared__ double sums[1024];
+  const int i = blockIdx.x * kEntries + (threadIdx.x % kEntries), group = threadIdx.x / kEntries;
   double s = 0.0;
-  for (int k = 0; k < slices; ++k) s += part[(long long)k * 2 * C + i];
-  (i < C ? grad_gamma : grad_beta)[i < C ? i : i - C] = (float)s;
+  if (i < 2 * C)
+    for (int k = group; k < slices; k += 1024 / kEntries) s += part[(long long)k * 2 * C + i];
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  for (int half = 512 / kEntries; half > 0; half /= 2) {
+    if (group < half) sums[threadIdx.x] += sums[threadIdx.x + half * kEntries];
+    __syncthreads();
+  }
+  if (group == 0 && i < 2 * C) (i < C ? grad_gamma : grad_beta)[i < C ? i : i - C] = (float)sums[threadIdx.x];
 }
 
-constexpr int kSlices = 64;
+constexpr long long kMostGroups = 1 << 21;  // a launch holds less than 2^32 threads
 
-size_t norm_backward_ws_bytes(const snls_norm_params& np) { return (size_t)kSlices * 2 * np.C * sizeof(double); }
+// Waves that share a tile's channels, n each, if 16 are enough.
+static int tile_waves(int C, int n) { return std::min(16, (C + n - 1) / n); }
+
+// How the gradients of a call are cut.  slices: rows of partial sums.
+struct GradCut {
+  enum { Tokens, Tiles, Pixels } form;
+  int V, R, waves;
+  long long units;  // tiles, or groups of tokens
+  long long slices;
+};
+
+static GradCut grad_cut(const snls_norm_params& np) {
+  GradCut c = {};
+  if (np.pixels == 1 && np.C <= 1024) {
+    c.form = GradCut::Tokens;
+    const int per = np.C <= 128 ? 16 : 4;
+    c.units = (np.frames + per - 1) / per;
+  } else if (np.pixels > 1 && np.C <= 512) {
+    c.form = GradCut::Tiles;
+    c.V = np.C <= 128 ? 4 : np.C <= 256 ? 2 : 1;
+    c.R = np.C <= 128 ? 8 : np.C <= 256 ? 16 : 32;
+    c.waves = tile_waves(np.C, 8);
+    c.units = np.frames * ((np.pixels + 64 * c.V - 1) / (64 * c.V));
+  } else {
+    c.form = GradCut::Pixels;
+    c.slices = 64;
+    return c;
+  }
+  // the chip is full with 512; 64 units a workgroup at most
+  c.slices = std::max(std::min(c.units, 512LL), (c.units + 63) / 64);
+  return c;
+}
+
+size_t norm_backward_ws_bytes(const snls_norm_params& np) {
+  return (size_t)std::max(grad_cut(np).slices, 1LL) * 2 * np.C * sizeof(double);
+}
 
 static unsigned pixel_groups(const snls_norm_params& np) {
   const long long groups = (np.frames * np.pixels + 255) / 256;
   return (unsigned)(groups < 16384 ? groups : 16384);
 }
-
-constexpr long long kMostGroups = 1 << 21;  // a launch holds less than 2^32 threads
-
-// Waves of a tile of V pixels a lane, R channels a wave at most.
-static int tile_waves(int C, int R) { return (C + R - 1) / R; }
 
 snls_status launch_norm(const float* x, const float* branch, const Drop& drop, const float* gamma, const float* beta,
                         const snls_norm_params& np, float* total, float* y, float* stats, hipStream_t s) {
@@ -314,18 +578,17 @@ snls_status launch_norm(const float* x, const float* branch, const Drop& drop, c
     else
       hipLaunchKernelGGL((norm_token_kernel<64, 8>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
   } else if (np.pixels > 1 && np.C <= 512) {
-    const bool wide = np.C <= 256 && np.frames * ((np.pixels + 255) / 256) >= 1024;
-    const int V = wide ? 4 : 1, waves = wide ? tile_waves(np.C, 16) : std::min(16, tile_waves(np.C, 4));
+    const int waves = tile_waves(np.C, 8);
     g.n = (np.C + waves - 1) / waves;
-    g.per_frame = (np.pixels + 64 * V - 1) / (64 * V), g.tiles = g.per_frame * np.frames;
+    g.per_frame = (np.pixels + 127) / 128, g.tiles = g.per_frame * np.frames;
     const dim3 grid((unsigned)std::min(g.tiles, kMostGroups)), block(64 * waves);
-    const size_t lds = waves > 1 ? 2 * waves * V * 64 * sizeof(float) : 0;
-    if (wide)
-      hipLaunchKernelGGL((norm_tile_kernel<4, 16>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else if (np.C <= 256)
-      hipLaunchKernelGGL((norm_tile_kernel<1, 16>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else
-      hipLaunchKernelGGL((norm_tile_kernel<1, 32>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats);
+    const size_t lds = waves > 1 ? 2 * waves * 128 * sizeof(float) : 0;
+#define SNLS_TILES(R)                                                                                              \
+  hipLaunchKernelGGL((norm_tile_kernel<2, R>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats)
+    if (g.n <= 8) SNLS_TILES(8);
+    else if (g.n <= 16) SNLS_TILES(16);
+    else SNLS_TILES(32);
+#undef SNLS_TILES
   } else {
     hipLaunchKernelGGL(norm_kernel, dim3(pixel_groups(np)), dim3(256), 0, s, x, branch, drop, gamma, beta, np.frames,
                        np.C, np.pixels, np.eps, total, y, stats);
@@ -333,19 +596,46 @@ snls_status launch_norm(const float* x, const float* branch, const Drop& drop, c
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
-// The sums over the pixels come first: grad_x may be grad_y.
 snls_status launch_norm_backward(const float* grad_y, const float* grad_total, const float* total, const float* stats,
                                  const float* gamma, const Drop& drop, const snls_norm_params& np, float* grad_x,
                                  float* grad_branch, float* grad_gamma, float* grad_beta, double* ws, hipStream_t s) {
-  if (grad_gamma) {
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)np.C, kSlices), dim3(256), 0, s, grad_y, total, stats,
-                       np.frames, np.C, np.pixels, ws);
-    hipLaunchKernelGGL(norm_weights_sum_kernel, dim3((unsigned)((2 * np.C + 255) / 256)), dim3(256), 0, s, ws, kSlices,
-                       np.C, grad_gamma, grad_beta);
+  const GradCut cut = grad_cut(np);
+  double* const sums = grad_gamma ? ws : nullptr;
+  NormGeo g = {np.frames, np.pixels, cut.units, 0, np.C, 0, np.eps};
+  const dim3 grid((unsigned)cut.slices);
+  if (np.frames > 0 && cut.form == GradCut::Tiles) {
+    g.n = (np.C + cut.waves - 1) / cut.waves;
+    g.per_frame = cut.units / np.frames;
+    const dim3 block(64 * cut.waves);
+    const size_t lds = cut.waves > 1 ? 4 * cut.waves * cut.V * 64 * sizeof(float) : 0;
+#define SNLS_TILES(V, R, H)                                                                                            \
+  hipLaunchKernelGGL((norm_grad_tile_kernel<V, R, H>), grid, block, lds, s, grad_y, grad_total, total, stats, gamma,    \
+                     drop, g, grad_x, grad_branch, sums)
+    if (cut.R == 8) SNLS_TILES(4, 8, true);
+    else if (cut.R == 16) SNLS_TILES(2, 16, true);
+    else SNLS_TILES(1, 32, false);
+#undef SNLS_TILES
+  } else if (np.frames > 0 && cut.form == GradCut::Tokens) {
+#define SNLS_TOKENS(G, N)                                                                                           \
+  hipLaunchKernelGGL((norm_grad_token_kernel<G, N>), grid, dim3(256), 0, s, grad_y, grad_total, total, stats, gamma, \
+                     drop, g, grad_x, grad_branch, sums)
+    if (np.C <= 64) SNLS_TOKENS(16, 1);
+    else if (np.C <= 128) SNLS_TOKENS(16, 2);
+    else if (np.C <= 256) SNLS_TOKENS(64, 1);
+    else SNLS_TOKENS(64, 4);
+#undef SNLS_TOKENS
+  } else {
+    // the sums over the pixels come first: grad_x may be grad_y
+    if (sums && np.frames > 0)
+      hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)np.C, (unsigned)cut.slices), dim3(256), 0, s, grad_y,
+                         total, stats, np.frames, np.C, np.pixels, ws);
+    if (np.frames > 0)
+      hipLaunchKernelGGL(norm_grad_kernel, dim3(pixel_groups(np)), dim3(256), 0, s, grad_y, grad_total, total, stats,
+                         gamma, drop, np.frames, np.C, np.pixels, grad_x, grad_branch);
   }
-  if (np.frames > 0)
-    hipLaunchKernelGGL(norm_grad_kernel, dim3(pixel_groups(np)), dim3(256), 0, s, grad_y, grad_total, total, stats,
-                       gamma, drop, np.frames, np.C, np.pixels, grad_x, grad_branch);
+  if (sums)
+    hipLaunchKernelGGL(norm_weights_sum_kernel, dim3((unsigned)((2 * np.C + kEntries - 1) / kEntries)), dim3(1024), 0,
+                       s, ws, np.frames > 0 ? (int)cut.slices : 0, np.C, grad_gamma, grad_beta);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 

@@ -18,6 +18,15 @@ struct Words {
   unsigned w[4];
 };
 
+// Both halves of a product of 32-bit numbers in one instruction (the compiler
+// takes one for each half).
+SNLS_DEV void wide_product(unsigned a, unsigned b, unsigned* hi, unsigned* lo) {
+  unsigned long long r;
+  unsigned long long carry;
+  asm("v_mad_u64_u32 %0, %1, %2, %3, 0" : "=v"(r), "=s"(carry) : "s"(a), "v"(b));
+  *hi = (unsigned)(r >> 32), *lo = (unsigned)r;
+}
+
 // The generator of a call: key and the counter's upper half.
 struct Philox {
   unsigned k0, k1, step, site;
@@ -30,8 +39,9 @@ struct Philox {
     unsigned c0 = (unsigned)b, c1 = (unsigned)(b >> 32), c2 = step, c3 = site, a = k0, e = k1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
-      const unsigned h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0;
-      const unsigned h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
+      unsigned h0, l0, h1, l1;
+      wide_product(0xD2511F53u, c0, &h0, &l0);
+      wide_product(0xCD9E8D57u, c2, &h1, &l1);
       c0 = h1 ^ c1 ^ a, c1 = l1, c2 = h0 ^ c3 ^ e, c3 = l0;
       a += 0x9E3779B9u, e += 0xBB67AE85u;
     }
