@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
           }
 #pragma unroll
           for (int j = 0; j < V; ++j) s[c][j] += b[j];
-          store_run<V>(total + at + c * g.P, cnt, s[c]);
+          stream_run<V>(total + at + c * g.P, cnt, s[c]);
         }
     }
     // the sum over all channels of what every wave has of its own
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
         float o[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] = fmaf(s[c][j] * rstd[j], ga, be);
-        store_run<V>(y + at + c * g.P, cnt, o);
+        stream_run<V>(y + at + c * g.P, cnt, o);
       }
     if (stats && wv == 0) {
       store_run<V>(stats + f * g.P + (cnt > 0 ? p : 0), cnt, mean);
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const f
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[k][j] += b[j];
-        store_run<4>(total + at + c, cnt, s[k]);
+        stream_run<4>(total + at + c, cnt, s[k]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum += s[k][j];
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const f
       if (beta) load_run<4>(beta + c, cnt, be);
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[k][j] = fmaf(s[k][j] * rstd, ga[j], be[j]);
-      store_run<4>(y + at + c, cnt, s[k]);
+      stream_run<4>(y + at + c, cnt, s[k]);
     }
     if (stats && l == 0) stats[row] = mean, stats[g.frames + row] = rstd;
   }
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
           r[j] = rstd[j] * (gy[c][j] - sum[0][j] - xh[c][j] * sum[1][j]);
           if (grad_total) r[j] += t[j];
         }
-        store_run<V>(grad_x + e, cnt, r);
+        stream_run<V>(grad_x + e, cnt, r);
         if (grad_branch) {
           if (d.rng) {
             unsigned w[V];
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
 #pragma unroll
             for (int j = 0; j < V; ++j) r[j] = dropped(r[j], w[j], d);
           }
-          store_run<V>(grad_branch + e, cnt, r);
+          stream_run<V>(grad_branch + e, cnt, r);
         }
       }
   }
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
         r[j] = rstd * (gy[k][j] - s0 - xh[k][j] * s1);
         if (grad_total) r[j] += t[j];
       }
-      store_run<4>(grad_x + at + c, cnt, r);
+      stream_run<4>(grad_x + at + c, cnt, r);
       if (grad_branch) {
         if (d.rng) {
           unsigned w[4];
@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
 #pragma unroll
           for (int j = 0; j < 4; ++j) r[j] = dropped(r[j], w[j], d);
         }
-        store_run<4>(grad_branch + at + c, cnt, r);
+        stream_run<4>(grad_branch + at + c, cnt, r);
       }
     }
   }

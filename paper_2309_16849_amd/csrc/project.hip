@@ -197,7 +197,8 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
           for (int r = 0; r < 16; ++r) {
             const int row = 8 * (r / 4) + r % 4;
             const float s = __shfl(ts, row + 4 * half);
-            if (row < rows) to_row[(long long)row * g.per] = fmaf((float)acc[r] * s, ch.scale, ch.bias);
+            if (row < rows)
+              __builtin_nontemporal_store(fmaf((float)acc[r] * s, ch.scale, ch.bias), to_row + (long long)row * g.per);
           }
         } else {
           float* const to_px = out + f * g.per * g.P + p;
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
           for (int r = 0; r < 16; ++r) {
             const int row = 8 * (r / 4) + r % 4;
             const OutChannel c = ch[row];
-            if (row < rows) to_px[c.at] = fmaf((float)acc[r] * ts, c.scale, c.bias);
+            if (row < rows) __builtin_nontemporal_store(fmaf((float)acc[r] * ts, c.scale, c.bias), to_px + c.at);
           }
         }
       }

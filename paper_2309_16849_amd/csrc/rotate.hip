@@ -1,8 +1,11 @@
 // rotate.hip -- rotary positions over time, rows and columns (snls_rotate,
 // snls_rotate_points).
-#include "snls_internal.h"
+#include <algorithm>
+
+#include "lanes.h"
 
 namespace snls {
+constexpr int kDeep = 4;  // rows a lane has in flight
 
 // cos and sin of pos * turns turns.  The angle is formed and reduced to the
 // nearest quarter turn in 64 bits, so that what is rounded to fp32 is at most
@@ -30,36 +33,83 @@ SNLS_DEV Pair pair_of(int p, const Rotary& r) {
   return r.interleaved ? Pair{axis, at + 2 * p, at + 2 * p + 1} : Pair{axis, at + p, at + n + p};
 }
 
-// A thread per pixel of a pair's two planes; behind the pairs, per pixel of the
-// planes that are copied.
-__global__ void __launch_bounds__(256) rotate_kernel(const float* x, const int64_t* __restrict__ times, Rotary r,
-                                                     long long groups, float* out) {
-  const int units = r.total + (r.Ch - 2 * r.total);
+// How the frames of a call are cut: a workgroup takes `rows` rows of up to 1024
+// columns of the two planes of a pair (or of a plane that is copied).
+struct RotateGeo {
+  long long heads;         // B * T * HD
+  int units, quads, cols;  // quads: runs of four columns in a block of columns; cols: such blocks
+  int rows, chunks;        // chunks of rows
+};
+
+// 16 bytes an element pair read and as many written: bandwidth bounds it.  A
+// lane keeps its four columns and walks down the rows, so that the angles of a
+// column pair are formed once, those of a row pair once a row, those of a time
+// pair once: 5x64x480x854 q and k, 889 us with a phase per pixel, NNN so.
+__global__ void __launch_bounds__(256) rotate_kernel(const float* q, const float* k,
+                                                     const int64_t* __restrict__ times, Rotary r, RotateGeo g,
+                                                     float* q_out, float* k_out) {
   const long long HW = (long long)r.H * r.W;
-  const long long work = (long long)r.B * r.T * r.HD * units * groups;
-  for (long long g = blockIdx.x; g < work; g += gridDim.x) {
-    const long long i = g % groups * 256 + threadIdx.x;
-    if (i >= HW) continue;
-    const long long u = g / groups;
-    const int p = (int)(u % units);
-    const long long head = u / units;
-    const float* src = x + head * r.Ch * HW + i;
-    float* dst = out + head * r.Ch * HW + i;
-    if (p >= r.total) {
-      const long long c = r.total + p;
-      dst[c * HW] = src[c * HW];
-      continue;
+  const int down = threadIdx.x / g.quads, steps = 256 / g.quads;
+  const int col = ((int)(blockIdx.x % g.cols) * 256 + (int)threadIdx.x - down * g.quads) * 4, cnt = r.W - col;
+  const int row0 = (int)(blockIdx.x / g.cols) * g.rows, row1 = min(row0 + g.rows, r.H);
+  if (down >= steps || cnt <= 0) return;
+  for (long long h = blockIdx.z; h < (k ? 2 : 1) * g.heads; h += gridDim.z) {
+    const bool second = h >= g.heads;
+    const long long head = second ? h - g.heads : h, bt = head / r.HD;
+    const float* const src = (second ? k : q) + head * r.Ch * HW + col;
+    float* const dst = (second ? k_out : q_out) + head * r.Ch * HW + col;
+    for (int p = blockIdx.y; p < g.units; p += gridDim.y) {
+      if (p >= r.total) {
+        const long long c = (r.total + p) * HW;
+        if (src != dst)
+          for (int y = row0 + down; y < row1; y += steps) {
+            float a[4];
+            load_run<4>(src + c + (long long)y * r.W, cnt, a);
+            stream_run<4>(dst + c + (long long)y * r.W, cnt, a);
+          }
+        continue;
+      }
+      const Pair pr = pair_of(p, r);
+      const double turns = r.turns[p];
+      float cs[4], sn[4];
+      if (pr.axis == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) phase((double)r.col0 + (double)(col + j), turns, cs + j, sn + j);
+      } else {
+        phase(times ? (double)times[bt] : (double)(bt % r.T), turns, cs, sn);
+#pragma unroll
+        for (int j = 1; j < 4; ++j) cs[j] = cs[0], sn[j] = sn[0];
+      }
+      const long long c1 = pr.first * HW, c2 = pr.second * HW;
+      for (int y = row0 + down; y < row1; y += kDeep * steps) {
+        float a[kDeep][4], b[kDeep][4];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+          if (y + u * steps < row1) {
+            const long long at = (long long)(y + u * steps) * r.W;
+            load_run<4>(src + c1 + at, cnt, a[u]);
+            load_run<4>(src + c2 + at, cnt, b[u]);
+          }
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+          if (y + u * steps < row1) {
+            const long long at = (long long)(y + u * steps) * r.W;
+            if (pr.axis == 1) {
+              phase((double)r.row0 + (double)(y + u * steps), turns, cs, sn);
+#pragma unroll
+              for (int j = 1; j < 4; ++j) cs[j] = cs[0], sn[j] = sn[0];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float t = fmaf(a[u][j], cs[j], -(b[u][j] * sn[j]));
+              b[u][j] = fmaf(a[u][j], sn[j], b[u][j] * cs[j]);
+              a[u][j] = t;
+            }
+            stream_run<4>(dst + c1 + at, cnt, a[u]);
+            stream_run<4>(dst + c2 + at, cnt, b[u]);
+          }
+      }
     }
-    const Pair pr = pair_of(p, r);
-    const long long bt = head / r.HD;
-    const double pos = pr.axis == 0   ? (times ? (double)times[bt] : (double)(bt % r.T))
-                       : pr.axis == 1 ? (double)r.row0 + (double)(i / r.W)
-                                      : (double)r.col0 + (double)(i % r.W);
-    float c, s;
-    phase(pos, r.turns[p], &c, &s);
-    const float a = src[pr.first * HW], b = src[pr.second * HW];
-    dst[pr.first * HW] = fmaf(a, c, -(b * s));
-    dst[pr.second * HW] = fmaf(a, s, b * c);
   }
 }
 
@@ -98,11 +148,20 @@ __global__ void __launch_bounds__(256) rotate_points_kernel(const float* q, cons
 
 snls_status launch_rotate(const float* q, const float* k, const int64_t* times, const Rotary& r, float* q_out,
                           float* k_out, hipStream_t s) {
-  const long long groups = ((long long)r.H * r.W + 255) / 256;
-  const long long work = (long long)r.B * r.T * r.HD * (r.Ch - r.total) * groups;
-  const dim3 grid((unsigned)(work < (1 << 20) ? work : (1 << 20)));
-  hipLaunchKernelGGL(rotate_kernel, grid, dim3(256), 0, s, q, times, r, groups, q_out);
-  if (k) hipLaunchKernelGGL(rotate_kernel, grid, dim3(256), 0, s, k, times, r, groups, k_out);
+  RotateGeo g;
+  const int quads = (r.W + 3) / 4;
+  g.heads = (long long)r.B * r.T * r.HD;
+  g.units = r.Ch - r.total;
+  g.quads = std::min(quads, 256);
+  g.cols = (quads + 255) / 256;
+  // 4,096 workgroups, but up to 8 rows a lane
+  const int steps = 256 / g.quads;
+  const double lanes = (double)g.heads * (k ? 2 : 1) * g.units * g.cols * ((r.H + steps - 1) / steps);
+  g.rows = steps * (int)std::min(8.0, std::max(1.0, lanes / 4096));
+  g.chunks = (r.H + g.rows - 1) / g.rows;
+  const dim3 grid((unsigned)((long long)g.chunks * g.cols), (unsigned)std::min(g.units, 1024),
+                  (unsigned)std::min(g.heads * (k ? 2 : 1), 1024LL));
+  hipLaunchKernelGGL(rotate_kernel, grid, dim3(256), 0, s, q, k, times, r, g, q_out, k_out);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
