@@ -194,6 +194,16 @@ def _new(shape, like, stream):
     return t
 
 
+def _like(t, given, name, stream):
+    """An output of t's shape: the given one, or a new one as by _new."""
+    if given is not None:
+        return _dev(given, name, t.shape)
+    new = torch.empty_like(t)
+    if stream is not None:
+        new.record_stream(stream)
+    return new
+
+
 # the current stream's handle without a Stream object around it (3 us a call)
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -691,10 +701,10 @@ def snls_norm(x, gamma=None, beta=None, eps: float = 1e-5, branch=None, drop: fl
     _per_channel(C, gamma=gamma, beta=beta)
     if branch is not None:
         _dev(branch, "branch", x.shape)
-        total = _dev(total, "total", x.shape) if total is not None else _new(x.shape, x, stream)
+        total = _like(x, total, "total", stream)
     elif total is not None:
         raise ValueError("total goes with branch")
-    y = _dev(y, "y", x.shape) if y is not None else _new(x.shape, x, stream)
+    y = _like(x, y, "y", stream)
     stats = _dev(stats, "stats", (2,) + px) if stats is not None else _new((2,) + px, x, stream)
     _here(x, gamma, beta, branch, rng, y, total, stats)
     prm = SnlsNormParams(_NORM_SIZE, C, frames, pixels or 1, float(eps), float(drop), int(site))
@@ -715,11 +725,9 @@ def snls_norm_backward(grad_y, total, stats, gamma=None, grad_total=None, drop: 
     _per_channel(C, gamma=gamma)
     if grad_total is not None:
         _dev(grad_total, "grad_total", total.shape)
-    grad_x = _dev(grad_x, "grad_x", total.shape) if grad_x is not None else _new(total.shape, total, stream)
-    if grad_branch is not None:
-        _dev(grad_branch, "grad_branch", total.shape)
-    elif drop > 0:
-        grad_branch = _new(total.shape, total, stream)
+    grad_x = _like(total, grad_x, "grad_x", stream)
+    if grad_branch is not None or drop > 0:
+        grad_branch = _like(total, grad_branch, "grad_branch", stream)
     prm = SnlsNormParams(_NORM_SIZE, C, frames if pixels else 0, pixels or 1, 0.0, float(drop), int(site))
     gg, gb, room = None, None, (None, 0)
     if weights:
@@ -744,7 +752,7 @@ def snls_dropout(x, rng, drop: float, site: int = 0, residual=None, out=None, st
     _dev(x, "x")
     if residual is not None:
         _dev(residual, "residual", x.shape)
-    out = _dev(out, "out", x.shape) if out is not None else _new(x.shape, x, stream)
+    out = _like(x, out, "out", stream)
     _here(x, residual, rng, out)
     _check(lib.snls_dropout(_ptr(x), _ptr(residual), _rng(rng, drop), x.numel(), float(drop), int(site), _ptr(out),
                             _stream(stream)), "snls_dropout")
@@ -770,10 +778,10 @@ def snls_rotate(q, k, rp: dict, times=None, inverse: bool = False, q_out=None, k
     lib = load_library()
     shp = video_shape(rp)
     _dev(q, "q", shp)
-    q_out = _dev(q_out, "q_out", shp) if q_out is not None else _new(shp, q, stream)
+    q_out = _like(q, q_out, "q_out", stream)
     if k is not None:
         _dev(k, "k", shp)
-        k_out = _dev(k_out, "k_out", shp) if k_out is not None else _new(shp, k, stream)
+        k_out = _like(k, k_out, "k_out", stream)
     elif k_out is not None:
         raise ValueError("k_out goes with k")
     if times is not None:
@@ -794,7 +802,7 @@ def snls_rotate_points(q, points, rp: dict, times=None, inverse: bool = False, o
     _dev_as(points, "points", (n, 3), (torch.int32,))
     if times is not None:
         _dev_as(times, "times", (rp["B"],), (torch.int64,))
-    out = _dev(out, "out", (n, rp["C"])) if out is not None else _new((n, rp["C"]), q, stream)
+    out = _like(q, out, "out", stream)
     _here(q, points, times, out)
     prm = rotate_from_dict(rp)
     _check(lib.snls_rotate_points(_ptr(q), _ptr(points), n, _ptr(times), ctypes.byref(prm), int(inverse), _ptr(out),
