@@ -9,23 +9,45 @@ SNLS_DEV unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; 
 constexpr unsigned kInfBits = 0x7f800000u;
 
 // Scale of the codes of values up to the magnitude `most` (NaN where that is
-// not finite) and their rounding.  A code is the whole number nearest to the
-// exact quotient x / s, ties to even: the product with the rounded reciprocal
-// is off by at most 127 * 2^-23, so the number it rounds to is off by at most
-// one, and x - code * s, which a fused multiply-add gives exactly where it
-// counts, says in which direction.
+// not finite) and their rounding: a code is the whole number nearest to the
+// exact quotient x / s, ties to even.  The sum of x * inv and 1.5 * 2^23, in one
+// rounding, has the nearest whole number to that product in its last bits; inv
+// is a rounded reciprocal, so it is the quotient's too unless the quotient lies
+// within 127 * 2^-24 of a half.  The remainder x - code * s, exact where it
+// counts, tells: beyond 0.49999 s, one value in 50,000, the code is settled by
+// comparing it with half a step.
 struct Quant {
-  float s, inv, half;
+  float s, inv, near, half;
   SNLS_DEV explicit Quant(unsigned most) {
     s = most < kInfBits ? fmaxf(__uint_as_float(most), 0x1p-100f) / 127.f : NAN;
-    inv = 1.f / s, half = 0.5f * s;
+    inv = 1.f / s, near = 0.49999f * s, half = 0.5f * s;
   }
-  SNLS_DEV int code(float x) const {
-    float c = rintf(x * inv);
-    const float r = fmaf(-c, s, x), m = fabsf(r);
-    const bool odd = (int)c & 1;
-    if (m > half || (m == half && odd)) c += copysignf(1.f, r);
-    return (int)c;
+  static constexpr float kMagic = 12582912.f;
+  SNLS_DEV float settle(float f, float x) const {
+    const float r = fmaf(-(f - kMagic), s, x), m = fabsf(r);
+    return m > half || (m == half && (__float_as_uint(f) & 1)) ? f + copysignf(1.f, r) : f;
+  }
+  SNLS_DEV int code(float x) const {  // of one value
+    return (int)(settle(fmaf(x, inv, kMagic), x) - kMagic);
+  }
+  // Codes of 16 values, four a register.
+  template <class Codes>
+  SNLS_DEV void codes16(const float* x, Codes& out) const {
+    float f[16], far = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      f[j] = fmaf(x[j], inv, kMagic);
+      far = fmaxf(far, fabsf(fmaf(-(f[j] - kMagic), s, x[j])));
+    }
+    if (far > near)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) f[j] = settle(f[j], x[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned a = __builtin_amdgcn_perm(__float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j]), 0x0c0c0400u);
+      const unsigned b = __builtin_amdgcn_perm(__float_as_uint(f[4 * j + 3]), __float_as_uint(f[4 * j + 2]), 0x04000c0cu);
+      out[j] = (int)(a | b);
+    }
   }
 };
 
@@ -103,54 +125,55 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
     }
   };
 
-  if (once) {
-    stage(t0, t1);
-    __syncthreads();
-  }
+  bool staged = false;
   for (long long grp = blockIdx.x; grp < g.groups; grp += gridDim.x) {
     const long long i0 = grp * 128 + wv * 32;
     const bool any = i0 < g.px;  // of this wave
     const bool mine = i0 + col < g.px;
-    long long f = 0, p = 0;
+    const long long f0 = TOK || !any ? i0 : i0 / g.P;
+    const unsigned rel = TOK || !any ? 0 : (unsigned)(i0 - f0 * g.P) + (mine ? col : 0);
+    const long long f = TOK ? i0 + (mine ? col : 0) : f0 + rel / (unsigned)g.P;
+    const long long p = TOK ? 0 : rel % (unsigned)g.P;
+    const long long step = TOK ? 1 : g.P;
+    const float* const first = x + f * g.cin * g.P + p;  // channel 0 of this lane's pixel
+    int upper = half * 16;
+    asm volatile("" : "+v"(upper));  // (else every guard below is held in registers across the groups)
+    // this lane's 16 channels of step ks
+    auto load16 = [&](int ks, float* v) {
+      const int c = ks * 32 + upper;
+      if (ks * 32 + 32 <= g.cin) {
+        const float* from = first + c * step;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = from[j * step];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float u = first[min(c + j, g.cin - 1) * step];
+          v[j] = c + j < g.cin ? u : 0.f;
+        }
+      }
+    };
+    float v[KEEP ? NK * 16 : 64];
+    if (KEEP && any)
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) load16(ks, v + ks * 16);
+    // (the weights' way to LDS goes by while the values come in)
+    const bool now = once && !staged;
+    if (now) stage(t0, t1);
     Int4 codes[NK];
     float ts = 0.f;
     if (any) {
-      const long long f0 = TOK ? i0 : i0 / g.P;
-      const unsigned rel = TOK ? 0 : (unsigned)(i0 - f0 * g.P) + (mine ? col : 0);
-      f = TOK ? i0 + (mine ? col : 0) : f0 + rel / (unsigned)g.P;
-      p = TOK ? 0 : rel % (unsigned)g.P;
-      const long long step = TOK ? 1 : g.P;
-      const float* const first = x + f * g.cin * g.P + p;  // channel 0 of this lane's pixel
-      int upper = half * 16;
-      asm volatile("" : "+v"(upper));  // (else every guard below is held in registers across the groups)
-      // this lane's 16 channels of step ks
-      auto load16 = [&](int ks, float* v) {
-        const int c = ks * 32 + upper;
-        if (ks * 32 + 32 <= g.cin) {
-          const float* from = first + c * step;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = from[j * step];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float u = first[min(c + j, g.cin - 1) * step];
-            v[j] = c + j < g.cin ? u : 0.f;
-          }
-        }
-      };
       unsigned most = 0;
-      float v[KEEP ? NK * 16 : 16];
       if constexpr (KEEP) {
-#pragma unroll
-        for (int ks = 0; ks < NK; ++ks) load16(ks, v + ks * 16);
 #pragma unroll
         for (int j = 0; j < NK * 16; ++j) most = max(most, magnitude(v[j]));
       } else {
 #pragma unroll 1
-        for (int ks = 0; ks < NK; ++ks) {
-          load16(ks, v);
+        for (int ks = 0; ks < NK; ks += 4) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) most = max(most, magnitude(v[j]));
+          for (int b = 0; b < 4; ++b) load16(ks + b, v + b * 16);
+#pragma unroll
+          for (int j = 0; j < 64; ++j) most = max(most, magnitude(v[j]));
         }
       }
       most = max(most, (unsigned)__shfl_xor((int)most, 32));
@@ -159,19 +182,18 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
       ts = q.s;
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
-        if constexpr (!KEEP) {
-          __builtin_amdgcn_sched_barrier(0);  // one step's values at a time: all at once do not fit
-          load16(ks, v);
-        }
+        if constexpr (!KEEP)
+          if (ks % 4 == 0) {
+            __builtin_amdgcn_sched_barrier(0);  // four steps' values at a time: all at once do not fit
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          unsigned u = 0;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) u |= ((unsigned)q.code(v[(KEEP ? ks * 16 : 0) + j * 4 + b]) & 0xffu) << (8 * b);
-          codes[ks][j] = ok ? (int)u : 0;
-        }
+            for (int b = 0; b < 4; ++b) load16(ks + b, v + b * 16);
+          }
+        q.codes16(v + (KEEP ? ks : ks % 4) * 16, codes[ks]);
+        if (!ok) codes[ks] = Int4{0, 0, 0, 0};
       }
     }
+    if (now) __syncthreads();
+    staged = true;
     for (int from = t0; from < t1; from += g.hold) {
       const int to = min(from + g.hold, t1);
       if (!once) {
@@ -247,7 +269,7 @@ static void run_project(const float* x, const int8_t* codes, const float* scales
 snls_status launch_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
                            const snls_project_params& pp, float* out, hipStream_t s) {
   const int steps = (pp.cin + 31) / 32;
-  const int nk = steps <= 4 ? steps : steps <= 6 ? 6 : steps <= 8 ? 8 : steps <= 16 ? 16 : 32;
+  const int nk = steps <= 4 ? steps : steps <= 6 ? 6 : steps <= 8 ? 8 : steps <= 12 ? 12 : steps <= 16 ? 16 : 32;
   ProjectGeo g;
   g.px = pp.frames * pp.pixels, g.P = pp.pixels, g.F = pp.frames;
   g.groups = (g.px + 127) / 128;
@@ -268,6 +290,7 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
     case 4: run_project<4>(x, codes, scales, bias, g, tokens, grid, out, s); break;
     case 6: run_project<6>(x, codes, scales, bias, g, tokens, grid, out, s); break;
     case 8: run_project<8>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 12: run_project<12>(x, codes, scales, bias, g, tokens, grid, out, s); break;
     case 16: run_project<16>(x, codes, scales, bias, g, tokens, grid, out, s); break;
     default: run_project<32>(x, codes, scales, bias, g, tokens, grid, out, s); break;
   }
