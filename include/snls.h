@@ -635,7 +635,7 @@ snls_status snls_project_pack(const float* w, const snls_project_params* pp, voi
  *           overlaps no input; nothing is touched when frames == 0
  * |x| * 127 * cin has to stay in fp32's range.  The result does not depend on
  * scheduling.  Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for cin above
- * SNLS_PROJECT_MAX_CIN, cout of 2^16 or more, pixels of 2^30 or more, 2^38
+ * SNLS_PROJECT_MAX_CIN, cout of 2^16 or more, pixels of 2^26 or more, 2^38
  * elements of x or out or more; SNLS_ERR_HIP. */
 snls_status snls_project(const float* x, const void* codes, const float* scales, const float* bias,
                          const snls_project_params* pp, float* out, void* stream);

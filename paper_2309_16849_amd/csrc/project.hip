@@ -1,6 +1,6 @@
 // project.hip -- projections in 8-bit integers: tokens quantised on the way, a
 // scale per token and per output channel (snls_project, snls_project_pack).
-#include "snls_internal.h"
+#include "lanes.h"
 
 namespace snls {
 
@@ -54,21 +54,24 @@ struct Quant {
 typedef int Int4 __attribute__((ext_vector_type(4)));
 typedef int Int16 __attribute__((ext_vector_type(16)));
 
-// A call's sizes on the device.  span: tiles of 32 output channels a workgroup
-// takes; hold: of these, how many lie in LDS at a time.
+// A call's sizes on the device.  A group is 128 pixels of one frame (or 128
+// tokens), so that a wave's loads and stores have one base and 32-bit offsets.
 struct ProjectGeo {
-  long long px, P, groups;  // pixels in all, of a frame; groups of 128 of them
-  long long F;              // frames
-  int cin, cout, per;       // per: output channels of a part
-  int span, hold;
+  long long P, groups, per_frame;  // pixels of a frame; groups in all, of a frame
+  long long F;                     // frames
+  int cin, cout, per;              // per: output channels of a part
+  int span, hold, buffers;         // tiles of 32 output channels a workgroup takes, that lie in LDS at a time, in one
+                                   // buffer (all of them) or two
+  bool aligned;                    // rows of weights at 16 bytes
 };
 
-// What the epilogue needs of an output channel: where its plane starts (a
-// token's: its place in the row), scale and bias.
-struct OutChannel {
-  long long at;
-  float scale, bias;
-};
+// The float at `base` (the same for the wave) and a lane's offset in bytes.
+SNLS_DEV float load_at(const float* base, unsigned bytes) {
+  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes);
+}
+SNLS_DEV void stream_at(float* base, unsigned bytes, float v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes));
+}
 
 // 16 consecutive weights of a channel as a lane of the matrix instruction takes
 // them; 0 behind the last channel of either side.
@@ -96,70 +99,97 @@ SNLS_DEV Int4 weights16(const int8_t* __restrict__ w, int o, int c, const Projec
 // Up to KEEP steps, the values stay in registers between the maximum and the
 // codes; beyond, they are read again.
 template <int NK, bool TOK>
-__global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
-                                                      const float* __restrict__ scales,
-                                                      const float* __restrict__ bias, ProjectGeo g,
-                                                      float* __restrict__ out) {
+__global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
+                                                         const float* __restrict__ scales,
+                                                         const float* __restrict__ bias, ProjectGeo g,
+                                                         float* __restrict__ out) {
   extern __shared__ char lds[];
   constexpr bool KEEP = NK <= 8;
+  constexpr int STEPS = KEEP ? NK : 4;  // whose values are held at a time
   Int4* const wt = reinterpret_cast<Int4*>(lds);
-  OutChannel* const chan = reinterpret_cast<OutChannel*>(lds + g.hold * NK * 1024);
-  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, wv = threadIdx.x >> 6;
+  // a tile's scales, its biases, and where its channels' planes start in a frame 0
+  float* const sb = reinterpret_cast<float*>(lds + g.buffers * g.hold * NK * 1024);
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tiles = (g.cout + 31) / 32, t0 = blockIdx.y * g.span, t1 = min(t0 + g.span, tiles);
   const bool once = t1 - t0 <= g.hold;
 
-  // tiles [from, to) into LDS
-  auto stage = [&](int from, int to) {
-    const int n = (to - from) * NK * 64;
-    for (int i = threadIdx.x; i < n; i += 256) {
-      const int l = i & 63, ks = (i >> 6) % NK, t = from + (i >> 6) / NK;
-      wt[i] = weights16(w, t * 32 + (l & 31), ks * 32 + (l >> 5) * 16, g);
-    }
-    for (int i = threadIdx.x; i < (to - from) * 32; i += 256) {
-      const int o = from * 32 + i;
-      if (o < g.cout) {
-        const int part = o / g.per;
-        chan[i] = TOK ? OutChannel{(long long)part * g.F * g.per + (o - part * g.per), scales[o], bias ? bias[o] : 0.f}
-                      : OutChannel{(o + part * (g.F - 1) * g.per) * g.P, scales[o], bias ? bias[o] : 0.f};
+  // Tiles [from, to) into buffer b; aligned rows without a detour over registers
+  // (past the last row and channel others are read: those sums are not stored,
+  // and those codes are 0).
+  auto stage = [&](int from, int to, int b) {
+    Int4* const wb = wt + b * g.hold * NK * 64;
+    float* const tb = sb + b * g.hold * 128;
+    if (g.aligned) {
+      for (int n = wv; n < (to - from) * NK; n += 4) {
+        const int o = min((from + n / NK) * 32 + col, g.cout - 1), c = min(n % NK * 32 + half * 16, g.cin - 16);
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(w + (long long)o * g.cin + c),
+            (__attribute__((address_space(3))) void*)(wb + n * 64), 16, 0, 0);
+      }
+    } else {
+      for (int i = threadIdx.x; i < (to - from) * NK * 64; i += 256) {
+        const int l = i & 63, ks = (i >> 6) % NK, t = from + (i >> 6) / NK;
+        wb[i] = weights16(w, t * 32 + (l & 31), ks * 32 + (l >> 5) * 16, g);
       }
     }
+    for (int i = threadIdx.x; i < (to - from) * 32; i += 256) {
+      const int o = min(from * 32 + i, g.cout - 1);
+      float* const to = tb + (i >> 5) * 128 + (i & 31);
+      to[0] = scales[o], to[32] = bias ? bias[o] : 0.f;
+      const long long part = o / g.per;
+      reinterpret_cast<long long*>(tb + (i >> 5) * 128 + 64)[i & 31] = (part * (g.F - 1) * g.per + o) * (TOK ? 1 : g.P);
+    }
+  };
+  // what this wave has on the way to LDS is there, and then everyone's
+  auto all_staged = [] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
   };
 
   bool staged = false;
   for (long long grp = blockIdx.x; grp < g.groups; grp += gridDim.x) {
-    const long long i0 = grp * 128 + wv * 32;
-    const bool any = i0 < g.px;  // of this wave
-    const bool mine = i0 + col < g.px;
-    const long long f0 = TOK || !any ? i0 : i0 / g.P;
-    const unsigned rel = TOK || !any ? 0 : (unsigned)(i0 - f0 * g.P) + (mine ? col : 0);
-    const long long f = TOK ? i0 + (mine ? col : 0) : f0 + rel / (unsigned)g.P;
-    const long long p = TOK ? 0 : rel % (unsigned)g.P;
-    const long long step = TOK ? 1 : g.P;
-    const float* const first = x + f * g.cin * g.P + p;  // channel 0 of this lane's pixel
+    const long long f = TOK ? 0 : grp / g.per_frame;
+    const long long p0 = (TOK ? grp : grp - f * g.per_frame) * 128 + wv * 32;  // this wave's first pixel or token
+    const int have = (int)max(0LL, min(32LL, (TOK ? g.F : g.P) - p0));         // of its 32
+    const bool any = have > 0;
+    const int mine = min(col, have - 1);
+    const float* const base = TOK ? x + p0 * g.cin : x + f * g.cin * g.P + p0;
+    long long step = TOK ? 1 : g.P;  // from channel to channel
+    unsigned at = (TOK ? mine * g.cin + half * 16 : (unsigned)(half * 16 * g.P) + mine) * 4u;
     int upper = half * 16;
-    asm volatile("" : "+v"(upper));  // (else every guard below is held in registers across the groups)
+    // (else every channel's offset and guard is held in registers across the groups)
+    asm volatile("" : "+v"(upper), "+v"(at));
+    if constexpr (!TOK) asm volatile("" : "+s"(step));
     // this lane's 16 channels of step ks
     auto load16 = [&](int ks, float* v) {
-      const int c = ks * 32 + upper;
       if (ks * 32 + 32 <= g.cin) {
-        const float* from = first + c * step;
+        const float* from = base + ks * 32 * step;
+        if constexpr (TOK) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = from[j * step];
+          for (int j = 0; j < 16; j += 4)
+            load_run<4>(reinterpret_cast<const float*>(reinterpret_cast<const char*>(from + j) + at), 4, v + j);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j, from += step) v[j] = load_at(from, at);
+        }
       } else {
+        const float* from = base + ks * 32 * step;
+        const int left = g.cin - ks * 32 - upper;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float u = first[min(c + j, g.cin - 1) * step];
-          v[j] = c + j < g.cin ? u : 0.f;
+        for (int j = 0; j < 16; ++j, from += step) {
+          v[j] = 0.f;
+          if (j < left) v[j] = load_at(from, at);
         }
       }
     };
-    float v[KEEP ? NK * 16 : 64];
+    float v[STEPS * 16];
     if (KEEP && any)
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) load16(ks, v + ks * 16);
     // (the weights' way to LDS goes by while the values come in)
     const bool now = once && !staged;
-    if (now) stage(t0, t1);
+    if (now) stage(t0, t1, 0);
     Int4 codes[NK];
     float ts = 0.f;
     if (any) {
@@ -169,11 +199,11 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
         for (int j = 0; j < NK * 16; ++j) most = max(most, magnitude(v[j]));
       } else {
 #pragma unroll 1
-        for (int ks = 0; ks < NK; ks += 4) {
+        for (int ks = 0; ks < NK; ks += STEPS) {
 #pragma unroll
-          for (int b = 0; b < 4; ++b) load16(ks + b, v + b * 16);
+          for (int b = 0; b < STEPS; ++b) load16(ks + b, v + b * 16);
 #pragma unroll
-          for (int j = 0; j < 64; ++j) most = max(most, magnitude(v[j]));
+          for (int j = 0; j < STEPS * 16; ++j) most = max(most, magnitude(v[j]));
         }
       }
       most = max(most, (unsigned)__shfl_xor((int)most, 32));
@@ -183,57 +213,76 @@ __global__ void __launch_bounds__(256) project_kernel(const float* __restrict__ 
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
         if constexpr (!KEEP)
-          if (ks % 4 == 0) {
-            __builtin_amdgcn_sched_barrier(0);  // four steps' values at a time: all at once do not fit
+          if (ks % STEPS == 0) {
+            __builtin_amdgcn_sched_barrier(0);  // so many values at a time: all at once do not fit
 #pragma unroll
-            for (int b = 0; b < 4; ++b) load16(ks + b, v + b * 16);
+            for (int b = 0; b < STEPS; ++b) load16(ks + b, v + b * 16);
           }
-        q.codes16(v + (KEEP ? ks : ks % 4) * 16, codes[ks]);
+        q.codes16(v + ks % STEPS * 16, codes[ks]);
         if (!ok) codes[ks] = Int4{0, 0, 0, 0};
       }
     }
-    if (now) __syncthreads();
+    if (now) all_staged();
     staged = true;
-    for (int from = t0; from < t1; from += g.hold) {
+    int b = 0;
+    if (!once) {
+      __syncthreads();  // (the last group's tiles are read)
+      stage(t0, min(t0 + g.hold, t1), 0);
+      all_staged();
+    }
+    for (int from = t0; from < t1; from += g.hold, b ^= 1) {
       const int to = min(from + g.hold, t1);
-      if (!once) {
-        __syncthreads();
-        stage(from, to);
-        __syncthreads();
-      }
-      if (!any) continue;
-      for (int t = from; t < to; ++t) {
+      // the next tiles come in while these are used
+      if (to < t1) stage(to, min(to + g.hold, t1), b ^ 1);
+      for (int t = from; t < (any ? to : from); ++t) {
+        const Int4* const wb = wt + (b * g.hold + t - from) * NK * 64;
+        const float* const tb = sb + (b * g.hold + t - from) * 128;
         Int16 acc = {};
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) {
-          const Int4 a = wt[((t - from) * NK + ks) * 64 + lane];
+          const Int4 a = wb[ks * 64 + lane];
           acc = TOK ? __builtin_amdgcn_mfma_i32_32x32x32_i8(codes[ks], a, acc, 0, 0, 0)
                     : __builtin_amdgcn_mfma_i32_32x32x32_i8(a, codes[ks], acc, 0, 0, 0);
         }
         // register r: row 8 * (r / 4) + 4 * half + r % 4, column lane mod 32
+        const int o0 = t * 32, left = g.cout - o0;
+        const long long* const planes = reinterpret_cast<const long long*>(tb + 64);
         if constexpr (TOK) {
-          const OutChannel ch = chan[(t - from) * 32 + col];
-          float* const to_row = out + ch.at + (i0 + 4 * half) * g.per;
-          const int rows = t * 32 + col < g.cout ? (int)min(32LL, g.px - i0) - 4 * half : 0;
+          const float sc = tb[col], be = tb[32 + col];
+          float* const to_row = out + planes[col] + (p0 + 4 * half) * g.per;
+          const int rows = col < left ? have - 4 * half : 0;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int row = 8 * (r / 4) + r % 4;
             const float s = __shfl(ts, row + 4 * half);
             if (row < rows)
-              __builtin_nontemporal_store(fmaf((float)acc[r] * s, ch.scale, ch.bias), to_row + (long long)row * g.per);
+              __builtin_nontemporal_store(fmaf((float)acc[r] * s, sc, be), to_row + (long long)row * g.per);
           }
-        } else {
-          float* const to_px = out + f * g.per * g.P + p;
-          const OutChannel* const ch = chan + (t - from) * 32 + 4 * half;
-          const int rows = mine ? g.cout - t * 32 - 4 * half : 0;
+        } else if (const int part = o0 / g.per; left >= 32 && have == 32 && o0 + 32 <= (part + 1) * g.per) {
+          // the whole tile, in one part
+          float* to_px = out + (((long long)part * g.F + f) * g.per + (o0 - part * g.per)) * step + p0;
+          const unsigned lane_at = ((unsigned)(4 * half * g.P) + col) * 4u;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            float sc[4], be[4];
+            load_run<4>(tb + 8 * n + 4 * half, 4, sc);
+            load_run<4>(tb + 32 + 8 * n + 4 * half, 4, be);
+#pragma unroll
+            for (int r = 0; r < 4; ++r, to_px += step)
+              stream_at(to_px, lane_at, fmaf((float)acc[4 * n + r] * ts, sc[r], be[r]));
+            to_px += 4 * step;
+          }
+        } else if (col < have) {
+          float* const to_px = out + f * g.per * g.P + p0 + col;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int row = 8 * (r / 4) + r % 4;
-            const OutChannel c = ch[row];
-            if (row < rows) __builtin_nontemporal_store(fmaf((float)acc[r] * ts, c.scale, c.bias), to_px + c.at);
+            const int row = 8 * (r / 4) + 4 * half + r % 4;
+            if (row < left)
+              __builtin_nontemporal_store(fmaf((float)acc[r] * ts, tb[row], tb[32 + row]), to_px + planes[row]);
           }
         }
       }
+      if (to < t1) all_staged();
     }
   }
 }
@@ -259,7 +308,7 @@ snls_status launch_project_pack(const float* w, int cin, int cout, int8_t* codes
 template <int NK>
 static void run_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
                         const ProjectGeo& g, bool tokens, dim3 grid, float* out, hipStream_t s) {
-  const size_t lds = (size_t)g.hold * (NK * 1024 + 32 * sizeof(OutChannel));
+  const size_t lds = (size_t)g.buffers * g.hold * (NK * 1024 + 128 * sizeof(float));
   if (tokens)
     hipLaunchKernelGGL((project_kernel<NK, true>), grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
   else
@@ -271,18 +320,20 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   const int steps = (pp.cin + 31) / 32;
   const int nk = steps <= 4 ? steps : steps <= 6 ? 6 : steps <= 8 ? 8 : steps <= 12 ? 12 : steps <= 16 ? 16 : 32;
   ProjectGeo g;
-  g.px = pp.frames * pp.pixels, g.P = pp.pixels, g.F = pp.frames;
-  g.groups = (g.px + 127) / 128;
+  const bool tokens = pp.pixels == 1;
+  g.P = pp.pixels, g.F = pp.frames;
+  g.per_frame = ((tokens ? g.F : g.P) + 127) / 128, g.groups = tokens ? g.per_frame : g.per_frame * g.F;
   g.cin = pp.cin, g.cout = pp.cout, g.per = pp.cout / pp.parts;
   const int tiles = (pp.cout + 31) / 32;
   // few pixels: the output channels are shared out too, until the chip has two workgroups a CU
   const long long want = (512 + g.groups - 1) / g.groups;
   const int split = (int)(want < tiles ? want : tiles);
   g.span = (tiles + split - 1) / split;
-  const int fit = 60 / nk;  // 60 KB of weights
-  g.hold = g.span < fit ? g.span : fit;
+  const int fit = 60 / nk;  // 60 KB of weights at once, or two buffers of 32 KB
+  g.buffers = g.span <= fit ? 1 : 2;
+  g.hold = g.span <= fit ? g.span : 32 / nk;
+  g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
   const dim3 grid((unsigned)(g.groups < 1280 ? g.groups : 1280), (unsigned)((tiles + g.span - 1) / g.span));
-  const bool tokens = pp.pixels == 1;
   switch (nk) {
     case 1: run_project<1>(x, codes, scales, bias, g, tokens, grid, out, s); break;
     case 2: run_project<2>(x, codes, scales, bias, g, tokens, grid, out, s); break;

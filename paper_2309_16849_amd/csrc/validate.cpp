@@ -153,7 +153,7 @@ snls_status check_project(const snls_project_params* pp) {
   if (!pp || pp->struct_size != sizeof(snls_project_params)) return SNLS_ERR_INVALID_ARG;
   if (pp->cin < 1 || pp->cout < 1 || pp->parts < 1 || pp->frames < 0 || pp->pixels < 1) return SNLS_ERR_INVALID_ARG;
   if (pp->cout % pp->parts != 0) return SNLS_ERR_INVALID_ARG;
-  if (pp->cin > SNLS_PROJECT_MAX_CIN || pp->cout >= 1 << 16 || pp->pixels >= kMaxPlane) return SNLS_ERR_UNSUPPORTED;
+  if (pp->cin > SNLS_PROJECT_MAX_CIN || pp->cout >= 1 << 16 || pp->pixels >= 1 << 26) return SNLS_ERR_UNSUPPORTED;
   if (too_many(pp->frames, pp->cin, pp->pixels) || too_many(pp->frames, pp->cout, pp->pixels))
     return SNLS_ERR_UNSUPPORTED;
   return SNLS_OK;

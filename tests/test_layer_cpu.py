@@ -130,7 +130,7 @@ def test_rotate_refuses_bad_arguments(lib):
 BAD_PROJ = [
     (dict(cin=0), BAD), (dict(cout=0, parts=1), BAD), (dict(parts=0), BAD), (dict(parts=5), BAD), (dict(frames=-1), BAD),
     (dict(pixels=0), BAD), (dict(size=28), BAD), (dict(cin=1025), BEYOND), (dict(cout=3 << 15), BEYOND),
-    (dict(pixels=1 << 30), BEYOND), (dict(frames=1 << 36), BEYOND), (dict(frames=1 << 50, pixels=1 << 20), BEYOND),
+    (dict(pixels=1 << 26), BEYOND), (dict(frames=1 << 36), BEYOND), (dict(frames=1 << 50, pixels=1 << 20), BEYOND),
 ]
 
 
