@@ -60,6 +60,14 @@ SNLS_DEV void stream_run(float* to, int cnt, const float* from) {
   }
 }
 
+// Workgroup b of n in an order that gives each of the 8 XCDs, which take
+// workgroups in turn, a run of neighbours: what two of them write of one cache
+// line meets in one L2.
+SNLS_DEV unsigned by_xcd(unsigned b, unsigned n) {
+  const unsigned per = n / 8;
+  return b < per * 8 ? (b & 7) * per + b / 8 : b;
+}
+
 }  // namespace snls
 
 #endif  // __HIPCC__

@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Philox gen(d);
   // (a row of sums is written again only behind a barrier that follows its last read)
-  for (long long tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+  for (long long tile = g.P % 32 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; tile < g.tiles; tile += gridDim.x) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const int c0 = wv * g.n, n = min(g.n, g.C - c0);
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
   double acc = 0.0;  // this lane's of the wave's 2 R sums
   float over[2 * R] = {};
   int turn = 0;
-  for (long long tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+  for (long long tile = g.P % 32 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; tile < g.tiles; tile += gridDim.x) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const long long px = f * g.P + (cnt > 0 ? p : 0), at = (f * g.C + c0) * g.P + (cnt > 0 ? p : 0);

@@ -69,9 +69,21 @@ struct ProjectGeo {
 SNLS_DEV float load_at(const float* base, unsigned bytes) {
   return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes);
 }
-SNLS_DEV void stream_at(float* base, unsigned bytes, float v) {
-  __builtin_nontemporal_store(v, reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes));
+template <bool PAST>
+SNLS_DEV void store_at(float* base, unsigned bytes, float v) {
+  float* const to = reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes);
+  if constexpr (PAST)
+    __builtin_nontemporal_store(v, to);
+  else
+    *to = v;
 }
+
+// Forms of a call.  Whole: every plane of the output starts a cache line, which
+// a wave's stores fill, past the caches.  Odd: they do not, and ordinary stores
+// let the L2 join the parts of a line that two waves write (4x48x271x483 to 96
+// channels: 99 us, 134 past the caches; at 272x480, whole lines, 79 and 54).
+// Tokens: a list of them (pixels == 1).
+enum class Form { Whole, Odd, Tokens };
 
 // 16 consecutive weights of a channel as a lane of the matrix instruction takes
 // them; 0 behind the last channel of either side.
@@ -94,17 +106,17 @@ SNLS_DEV Int4 weights16(const int8_t* __restrict__ w, int o, int c, const Projec
 // lanes have the upper 16), so a lane loads its pixel's channels, finds the
 // largest with its partner and packs the codes where the instruction wants them:
 // they never leave the registers.  The weights lie in LDS in the order of the
-// lanes.  NK: steps of 32 channels.  TOK: a list of tokens (pixels == 1), whose
-// rows and columns change places so that stores run along the output channels.
+// lanes.  NK: steps of 32 channels.  A list of tokens has rows and columns in each
+// other's place, so that stores run along the output channels.
 // Up to KEEP steps, the values stay in registers between the maximum and the
 // codes; beyond, they are read again.
-template <int NK, bool TOK>
+template <int NK, Form FORM>
 __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
                                                          const float* __restrict__ scales,
                                                          const float* __restrict__ bias, ProjectGeo g,
                                                          float* __restrict__ out) {
   extern __shared__ char lds[];
-  constexpr bool KEEP = NK <= 8;
+  constexpr bool KEEP = NK <= 8, TOK = FORM == Form::Tokens;
   constexpr int STEPS = KEEP ? NK : 4;  // whose values are held at a time
   Int4* const wt = reinterpret_cast<Int4*>(lds);
   // a tile's scales, its biases, and where its channels' planes start in a frame 0
@@ -148,7 +160,7 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
   };
 
   bool staged = false;
-  for (long long grp = blockIdx.x; grp < g.groups; grp += gridDim.x) {
+  for (long long grp = FORM == Form::Odd ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; grp < g.groups; grp += gridDim.x) {
     const long long f = TOK ? 0 : grp / g.per_frame;
     const long long p0 = (TOK ? grp : grp - f * g.per_frame) * 128 + wv * 32;  // this wave's first pixel or token
     const int have = (int)max(0LL, min(32LL, (TOK ? g.F : g.P) - p0));         // of its 32
@@ -269,7 +281,7 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
             load_run<4>(tb + 32 + 8 * n + 4 * half, 4, be);
 #pragma unroll
             for (int r = 0; r < 4; ++r, to_px += step)
-              stream_at(to_px, lane_at, fmaf((float)acc[4 * n + r] * ts, sc[r], be[r]));
+              store_at<FORM == Form::Whole>(to_px, lane_at, fmaf((float)acc[4 * n + r] * ts, sc[r], be[r]));
             to_px += 4 * step;
           }
         } else if (col < have) {
@@ -278,7 +290,7 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
           for (int r = 0; r < 16; ++r) {
             const int row = 8 * (r / 4) + 4 * half + r % 4;
             if (row < left)
-              __builtin_nontemporal_store(fmaf((float)acc[r] * ts, tb[row], tb[32 + row]), to_px + planes[row]);
+              to_px[planes[row]] = fmaf((float)acc[r] * ts, tb[row], tb[32 + row]);
           }
         }
       }
@@ -307,12 +319,12 @@ snls_status launch_project_pack(const float* w, int cin, int cout, int8_t* codes
 
 template <int NK>
 static void run_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
-                        const ProjectGeo& g, bool tokens, dim3 grid, float* out, hipStream_t s) {
+                        const ProjectGeo& g, Form form, dim3 grid, float* out, hipStream_t s) {
   const size_t lds = (size_t)g.buffers * g.hold * (NK * 1024 + 128 * sizeof(float));
-  if (tokens)
-    hipLaunchKernelGGL((project_kernel<NK, true>), grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
-  else
-    hipLaunchKernelGGL((project_kernel<NK, false>), grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
+  const auto kernel = form == Form::Tokens ? project_kernel<NK, Form::Tokens>
+                      : form == Form::Odd  ? project_kernel<NK, Form::Odd>
+                                           : project_kernel<NK, Form::Whole>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, x, codes, scales, bias, g, out);
 }
 
 snls_status launch_project(const float* x, const int8_t* codes, const float* scales, const float* bias,
@@ -334,16 +346,18 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   g.hold = g.span <= fit ? g.span : 32 / nk;
   g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
   const dim3 grid((unsigned)(g.groups < 1280 ? g.groups : 1280), (unsigned)((tiles + g.span - 1) / g.span));
+  const bool whole = pp.pixels % 32 == 0 && !(reinterpret_cast<uintptr_t>(out) & 127);
+  const Form form = tokens ? Form::Tokens : whole ? Form::Whole : Form::Odd;
   switch (nk) {
-    case 1: run_project<1>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 2: run_project<2>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 3: run_project<3>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 4: run_project<4>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 6: run_project<6>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 8: run_project<8>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 12: run_project<12>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    case 16: run_project<16>(x, codes, scales, bias, g, tokens, grid, out, s); break;
-    default: run_project<32>(x, codes, scales, bias, g, tokens, grid, out, s); break;
+    case 1: run_project<1>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 2: run_project<2>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 3: run_project<3>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 4: run_project<4>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 6: run_project<6>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 8: run_project<8>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 12: run_project<12>(x, codes, scales, bias, g, form, grid, out, s); break;
+    case 16: run_project<16>(x, codes, scales, bias, g, form, grid, out, s); break;
+    default: run_project<32>(x, codes, scales, bias, g, form, grid, out, s); break;
   }
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
