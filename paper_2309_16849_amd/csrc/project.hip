@@ -1,5 +1,7 @@
 // project.hip -- projections in 8-bit integers: tokens quantised on the way, a
 // scale per token and per output channel (snls_project, snls_project_pack).
+#include <algorithm>
+
 #include "lanes.h"
 
 namespace snls {
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
                                                          const float* __restrict__ bias, ProjectGeo g,
                                                          float* __restrict__ out) {
   extern __shared__ char lds[];
-  constexpr bool KEEP = NK <= 8, TOK = FORM == Form::Tokens;
+  constexpr bool KEEP = NK <= 6, TOK = FORM == Form::Tokens;
   constexpr int STEPS = KEEP ? NK : 4;  // whose values are held at a time
   Int4* const wt = reinterpret_cast<Int4*>(lds);
   // a tile's scales, its biases, and where its channels' planes start in a frame 0
@@ -338,7 +340,7 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   g.cin = pp.cin, g.cout = pp.cout, g.per = pp.cout / pp.parts;
   const int tiles = (pp.cout + 31) / 32;
   // few pixels: the output channels are shared out too, until the chip has two workgroups a CU
-  const long long want = (512 + g.groups - 1) / g.groups;
+  const long long want = std::max(1LL, 512 / g.groups);
   const int split = (int)(want < tiles ? want : tiles);
   g.span = (tiles + split - 1) / split;
   const int fit = 60 / nk;  // 60 KB of weights at once, or two buffers of 32 KB
