@@ -38,6 +38,7 @@ SNLS_DEV Pair pair_of(int p, const Rotary& r) {
 struct RotateGeo {
   long long heads;         // B * T * HD
   int units, quads, cols;  // quads: runs of four columns in a block of columns; cols: such blocks
+  int steps;               // rows a workgroup takes at once, a lane a run
   int rows, chunks;        // chunks of rows
 };
 
@@ -45,30 +46,38 @@ struct RotateGeo {
 // lane keeps its four columns and walks down the rows, so that the angles of a
 // column pair are formed once, those of a row pair once a row, those of a time
 // pair once: 5x64x480x854 q and k, 889 us with a phase per pixel, NNN so.
-__global__ void __launch_bounds__(256) rotate_kernel(const float* q, const float* k,
+__global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float* k,
                                                      const int64_t* __restrict__ times, Rotary r, RotateGeo g,
                                                      float* q_out, float* k_out) {
   const long long HW = (long long)r.H * r.W;
-  const int down = threadIdx.x / g.quads, steps = 256 / g.quads;
+  const int down = threadIdx.x / g.quads, steps = g.steps;
   const int col = ((int)(blockIdx.x % g.cols) * 256 + (int)threadIdx.x - down * g.quads) * 4, cnt = r.W - col;
   const int row0 = (int)(blockIdx.x / g.cols) * g.rows, row1 = min(row0 + g.rows, r.H);
-  if (down >= steps || cnt <= 0) return;
   for (long long h = blockIdx.z; h < (k ? 2 : 1) * g.heads; h += gridDim.z) {
     const bool second = h >= g.heads;
     const long long head = second ? h - g.heads : h, bt = head / r.HD;
-    const float* const src = (second ? k : q) + head * r.Ch * HW + col;
-    float* const dst = (second ? k_out : q_out) + head * r.Ch * HW + col;
+    const float* const src = (second ? k : q) + head * r.Ch * HW;
+    float* const dst = (second ? k_out : q_out) + head * r.Ch * HW;
     for (int p = blockIdx.y; p < g.units; p += gridDim.y) {
       if (p >= r.total) {
-        const long long c = (r.total + p) * HW;
+        // (rows are one run of floats here, shared out over the blocks of columns)
+        const long long c = (r.total + p) * HW, at = (long long)row0 * r.W, n = (long long)(row1 - row0) * r.W;
+        const float* const a = src + (c + at);
+        float* const o = dst + (c + at);
+        const long long stride = (long long)g.cols * blockDim.x * 4;
         if (src != dst)
-          for (int y = row0 + down; y < row1; y += steps) {
-            float a[4];
-            load_run<4>(src + c + (long long)y * r.W, cnt, a);
-            stream_run<4>(dst + c + (long long)y * r.W, cnt, a);
+          for (long long i = (blockIdx.x % g.cols * blockDim.x + threadIdx.x) * 4LL; i < n; i += kDeep * stride) {
+            float v[kDeep][4];
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
+              if (i + u * stride < n) load_run<4>(a + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
+              if (i + u * stride < n) stream_run<4>(o + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
           }
         continue;
       }
+      if (down >= steps || cnt <= 0) continue;
       const Pair pr = pair_of(p, r);
       const double turns = r.turns[p];
       float cs[4], sn[4];
@@ -80,7 +89,7 @@ __global__ void __launch_bounds__(256) rotate_kernel(const float* q, const float
 #pragma unroll
         for (int j = 1; j < 4; ++j) cs[j] = cs[0], sn[j] = sn[0];
       }
-      const long long c1 = pr.first * HW, c2 = pr.second * HW;
+      const long long c1 = pr.first * HW + col, c2 = pr.second * HW + col;
       for (int y = row0 + down; y < row1; y += kDeep * steps) {
         float a[kDeep][4], b[kDeep][4];
 #pragma unroll
@@ -154,14 +163,21 @@ snls_status launch_rotate(const float* q, const float* k, const int64_t* times, 
   g.units = r.Ch - r.total;
   g.quads = std::min(quads, 256);
   g.cols = (quads + 255) / 256;
+  // rows at once: what leaves the fewest lanes of whole waves without a run
+  // (131 runs a row: 2 rows on 320 lanes)
+  g.steps = 1;
+  int threads = (g.quads + 63) / 64 * 64;
+  for (int n = 2; n * g.quads <= 512; ++n) {
+    const int t = (n * g.quads + 63) / 64 * 64;
+    if ((double)n * g.quads / t > (double)g.steps * g.quads / threads + 0.01) g.steps = n, threads = t;
+  }
   // 4,096 workgroups, but up to 8 rows a lane
-  const int steps = 256 / g.quads;
-  const double lanes = (double)g.heads * (k ? 2 : 1) * g.units * g.cols * ((r.H + steps - 1) / steps);
-  g.rows = steps * (int)std::min(8.0, std::max(1.0, lanes / 4096));
+  const double lanes = (double)g.heads * (k ? 2 : 1) * g.units * g.cols * ((r.H + g.steps - 1) / g.steps);
+  g.rows = g.steps * (int)std::min(8.0, std::max(1.0, lanes / 4096));
   g.chunks = (r.H + g.rows - 1) / g.rows;
   const dim3 grid((unsigned)((long long)g.chunks * g.cols), (unsigned)std::min(g.units, 1024),
                   (unsigned)std::min(g.heads * (k ? 2 : 1), 1024LL));
-  hipLaunchKernelGGL(rotate_kernel, grid, dim3(256), 0, s, q, k, times, r, g, q_out, k_out);
+  hipLaunchKernelGGL(rotate_kernel, grid, dim3(threads), 0, s, q, k, times, r, g, q_out, k_out);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
