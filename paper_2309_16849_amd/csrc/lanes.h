@@ -60,6 +60,20 @@ SNLS_DEV void stream_run(float* to, int cnt, const float* from) {
   }
 }
 
+// The float at `base` (the same for the wave: two scalar registers) and a lane's
+// offset in bytes.
+SNLS_DEV float load_at(const float* base, unsigned bytes) {
+  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes);
+}
+template <bool PAST>
+SNLS_DEV void store_at(float* base, unsigned bytes, float v) {
+  float* const to = reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes);
+  if constexpr (PAST)
+    __builtin_nontemporal_store(v, to);
+  else
+    *to = v;
+}
+
 // Workgroup b of n in an order that gives each of the 8 XCDs, which take
 // workgroups in turn, a run of neighbours: what two of them write of one cache
 // line meets in one L2.

@@ -20,11 +20,12 @@ struct NormGeo {
 // every wave up to R channels of them; the values stay in registers from their
 // only read on, and the sums over the channels are joined in LDS: first the
 // mean, then the squares of the differences from it.
-template <int V, int R>
+template <int R>
 __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const float* branch, Drop d,
                                                          const float* __restrict__ gamma,
                                                          const float* __restrict__ beta, NormGeo g, float* total,
                                                          float* y, float* stats) {
+  constexpr int V = 2;
   extern __shared__ float part[];  // sums, then squares: a row a wave
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -40,21 +41,26 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
     for (int c = 0; c < R; ++c)
       if (c < n) load_run<V>(x + at + c * g.P, cnt, s[c]);
     if (branch) {
+      const bool shared = !(g.P & 3);  // two lanes, one block in every plane
 #pragma unroll
-      for (int c = 0; c < R; ++c)
-        if (c < n) {
-          float b[V];
-          load_run<V>(branch + at + c * g.P, cnt, b);
-          if (d.rng) {
-            unsigned w[V];
-            gen.run<V>(at + c * g.P, w);
+      for (int c2 = 0; c2 < R; c2 += 2) {
+        unsigned w[2][V];
+        if (d.rng && shared && c2 < n) share_blocks(gen.block((at + (c2 + (lane & 1)) * g.P) >> 2), lane & 1, w);
 #pragma unroll
-            for (int j = 0; j < V; ++j) b[j] = dropped(b[j], w[j], d);
+        for (int c = c2; c < c2 + 2; ++c)
+          if (c < n) {
+            float b[V];
+            load_run<V>(branch + at + c * g.P, cnt, b);
+            if (d.rng) {
+              if (!shared) gen.run<V>(at + c * g.P, w[c - c2]);
+#pragma unroll
+              for (int j = 0; j < V; ++j) b[j] = dropped(b[j], w[c - c2][j], d);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[c][j] += b[j];
+            stream_run<V>(total + at + c * g.P, cnt, s[c]);
           }
-#pragma unroll
-          for (int j = 0; j < V; ++j) s[c][j] += b[j];
-          stream_run<V>(total + at + c * g.P, cnt, s[c]);
-        }
+      }
     }
     // the sum over all channels of what every wave has of its own
     auto joined = [&](float* own, float* rows) {
@@ -257,29 +263,26 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
 // channels' 2 R terms over the tile's pixels, so that each of its lanes is left
 // with one of the sums, which it adds up over the tiles in 64 bits, and a
 // workgroup writes one row of partial sums.
-template <int V, int R, bool HOLD>
+template <int R>
 __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_y, const float* grad_total,
                                                               const float* __restrict__ total,
                                                               const float* __restrict__ stats,
                                                               const float* __restrict__ gamma, Drop d, NormGeo g,
                                                               float* grad_x, float* grad_branch,
                                                               double* __restrict__ sums) {
+  constexpr int V = 4;
   extern __shared__ float part[];  // two tables of two rows a wave, taken in turn
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Philox gen(d);
   const int c0 = wv * g.n, n = min(g.n, g.C - c0);
-  double acc = 0.0;  // this lane's of the wave's 2 R sums
-  float over[2 * R] = {};
+  float over[2 * R] = {};  // this lane's sums over the tiles
   int turn = 0;
   for (long long tile = g.P % 32 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; tile < g.tiles; tile += gridDim.x) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const long long px = f * g.P + (cnt > 0 ? p : 0), at = (f * g.C + c0) * g.P + (cnt > 0 ? p : 0);
     float mean[V], rstd[V], gy[R][V], xh[R][V], sum[2][V] = {};
-    if constexpr (!HOLD)
-#pragma unroll
-      for (int c = 0; c < 2 * R; ++c) over[c] = 0.f;
 #pragma unroll
     for (int c = 0; c < R; ++c)
       if (c < n) {
@@ -302,8 +305,6 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
           sum[1][j] = fmaf(gy[c][j], xh[c][j], sum[1][j]);
         }
       }
-    if constexpr (!HOLD)
-      if (sums) acc += (double)list_sum<2 * R>(over, lane);
     if (waves > 1) {
       float* const rows = part + turn * 2 * waves * V * 64;
       turn ^= 1;
@@ -347,9 +348,117 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
       }
   }
   if (!sums) return;
-  if constexpr (HOLD) acc = (double)list_sum<2 * R>(over, lane);
+  const double acc = (double)list_sum<2 * R>(over, lane);  // this lane's of the 2 R sums
   const int which = listed<2 * R>(lane), c = which % R;
   if (lane % (32 / R) == 0 && c < n) sums[((long long)blockIdx.x * 2 + which / R) * g.C + c0 + c] = acc;
+}
+
+// Gradients of frames of many channels: one pixel a lane, L = 64 pixels a tile up
+// to 256 channels, 32 and two channels side by side in a wave up to 512, so that
+// 64 registers hold a wave's tile and two workgroups of 8 waves fit a CU, one
+// loading while the other stores (5x256x128x128 without dropout 59 us, with one
+// workgroup of 16 waves 75; 5x384x96x96 60 and 77).  Where planes do not start a
+// cache line (WHOLE false) the stores are ordinary ones, whose parts of a line
+// the L2 joins (2x384x289x252 with dropout 278 us, past the caches 384).
+template <int L, int R, bool WHOLE>
+__global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* grad_y, const float* grad_total,
+                                                                const float* __restrict__ total,
+                                                                const float* __restrict__ stats,
+                                                                const float* __restrict__ gamma, Drop d, NormGeo g,
+                                                                float* grad_x, float* grad_branch,
+                                                                double* __restrict__ sums) {
+  constexpr int SIDE = 64 / L;     // channels a step; R steps a wave
+  extern __shared__ float part[];  // two tables of two rows a wave, taken in turn, and gamma
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, l = lane & (L - 1), side = lane / L;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Philox gen(d);
+  const int c0 = wv * g.n * SIDE, n = min(g.n, (g.C - c0 + SIDE - 1) / SIDE);
+  const int own = min(n, (g.C - c0 - side + SIDE - 1) / SIDE);  // this lane's steps: n, or one less
+  float* const scale = part + 4 * waves * 64;
+  for (int c = threadIdx.x; c < waves * g.n * SIDE; c += blockDim.x) scale[c] = gamma && c < g.C ? gamma[c] : 1.f;
+  __syncthreads();
+  double acc[R / 8] = {};
+  int turn = 0;
+  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
+    const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * L;
+    const bool in = l < g.P - p;
+    const unsigned here = in ? l : 0;
+    const long long at = (f * g.C + c0) * g.P + p;  // the wave's first element
+    // a lane without a pixel, or without a channel in the last step, reads another's
+    unsigned off = (here + side * (unsigned)g.P) * 4u;
+    auto place = [&](int k) { return SIDE > 1 && k == n - 1 && own < n ? here * 4u : off; };
+    long long step = SIDE * g.P;
+    asm volatile("" : "+s"(step), "+v"(off));  // (else every step's offset is held in registers across the tiles)
+    float gy[R], xh[R];
+    {
+      const float *a = grad_y + at, *b = total + at;
+#pragma unroll
+      for (int k = 0; k < R; ++k, a += step, b += step)
+        if (k < n) gy[k] = load_at(a, place(k)), xh[k] = load_at(b, place(k));
+    }
+    const float mean = load_at(stats + f * g.P + p, here * 4u), rstd = load_at(stats + (g.frames + f) * g.P + p, here * 4u);
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int k0 = 0; k0 < R; k0 += 8)
+      if (k0 < n) {
+        float over[16] = {};
+#pragma unroll
+        for (int k = k0; k < k0 + 8; ++k)
+          if (k < n) {
+            const bool ok = in && k < own;
+            gy[k] = ok ? gy[k] : 0.f;
+            xh[k] = ok ? (xh[k] - mean) * rstd : 0.f;
+            over[k - k0] = gy[k] * xh[k];
+            over[8 + k - k0] = gy[k];
+            gy[k] *= scale[c0 + k * SIDE + side];
+            s0 += gy[k];
+            s1 = fmaf(gy[k], xh[k], s1);
+          }
+        if (sums) acc[k0 / 8] += (double)list_sum<16, L / 2>(over, lane);
+      }
+    if (L == 32) s0 += __shfl_xor(s0, 32), s1 += __shfl_xor(s1, 32);
+    float* const rows = part + turn * 2 * waves * 64;
+    turn ^= 1;
+    rows[wv * 64 + lane] = s0, rows[(waves + wv) * 64 + lane] = s1;
+    __syncthreads();
+    s0 = s1 = 0.f;
+    for (int w = 0; w < waves; ++w) s0 += rows[w * 64 + lane], s1 += rows[(waves + w) * 64 + lane];
+    s0 /= g.C, s1 /= g.C;
+    const bool shared = !(g.P & 3);  // four lanes, one block in every plane
+    long long e = at;
+#pragma unroll
+    for (int k0 = 0; k0 < R; k0 += 4)
+      if (k0 < n) {
+        float t[4];
+        if (grad_total) {
+          const float* a = grad_total + e;
+#pragma unroll
+          for (int k = 0; k < 4; ++k, a += step)
+            if (k0 + k < n) t[k] = load_at(a, place(k0 + k));
+        }
+        unsigned w[4];
+        if (d.rng && shared) share_blocks(gen.block((e + off / 4 + (lane & 3) * step) >> 2), (int)(l & 3), w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k, e += step)
+          if (k0 + k < n) {
+            float r = rstd * (gy[k0 + k] - s0 - xh[k0 + k] * s1);
+            if (grad_total) r += t[k];
+            if (d.rng && !shared) gen.run<1>(e + off / 4, w + k);
+            if (in && k0 + k < own) {
+              store_at<WHOLE>(grad_x + e, off, r);
+              if (grad_branch) store_at<WHOLE>(grad_branch + e, off, d.rng ? dropped(r, w[k], d) : r);
+            }
+          }
+      }
+  }
+  if (!sums) return;
+  const int which = l / (L / 16);  // of the 16 sums of 8 steps
+#pragma unroll
+  for (int k0 = 0; k0 < R; k0 += 8) {
+    const int k = k0 + which % 8;
+    if (l % (L / 16) == 0 && k < own)
+      sums[((long long)blockIdx.x * 2 + which / 8) * g.C + c0 + k * SIDE + side] = acc[k0 / 8];
+  }
 }
 
 // Gradients of tokens: G lanes a token, as in the forward pass; a workgroup
@@ -524,7 +633,8 @@ static int tile_waves(int C, int n) { return std::min(16, (C + n - 1) / n); }
 // How the gradients of a call are cut.  slices: rows of partial sums.
 struct GradCut {
   enum { Tokens, Tiles, Pixels } form;
-  int V, R, waves;
+  bool wide;       // more than 128 channels
+  int run, waves;  // pixels a tile, waves
   long long units;  // tiles, or groups of tokens
   long long slices;
 };
@@ -537,10 +647,10 @@ static GradCut grad_cut(const snls_norm_params& np) {
     c.units = (np.frames + per - 1) / per;
   } else if (np.pixels > 1 && np.C <= 512) {
     c.form = GradCut::Tiles;
-    c.V = np.C <= 128 ? 4 : np.C <= 256 ? 2 : 1;
-    c.R = np.C <= 128 ? 8 : np.C <= 256 ? 16 : 32;
-    c.waves = tile_waves(np.C, 8);
-    c.units = np.frames * ((np.pixels + 64 * c.V - 1) / (64 * c.V));
+    c.wide = np.C > 128;
+    c.run = !c.wide ? 256 : np.C <= 256 ? 64 : 32;
+    c.waves = !c.wide ? tile_waves(np.C, 8) : 8;
+    c.units = np.frames * ((np.pixels + c.run - 1) / c.run);
   } else {
     c.form = GradCut::Pixels;
     c.slices = 64;
@@ -584,9 +694,10 @@ snls_status launch_norm(const float* x, const float* branch, const Drop& drop, c
     const dim3 grid((unsigned)std::min(g.tiles, kMostGroups)), block(64 * waves);
     const size_t lds = waves > 1 ? 2 * waves * 128 * sizeof(float) : 0;
 #define SNLS_TILES(R)                                                                                              \
-  hipLaunchKernelGGL((norm_tile_kernel<2, R>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats)
+  hipLaunchKernelGGL((norm_tile_kernel<R>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats)
     if (g.n <= 8) SNLS_TILES(8);
     else if (g.n <= 16) SNLS_TILES(16);
+    else if (g.n <= 24) SNLS_TILES(24);
     else SNLS_TILES(32);
 #undef SNLS_TILES
   } else {
@@ -604,17 +715,20 @@ snls_status launch_norm_backward(const float* grad_y, const float* grad_total, c
   NormGeo g = {np.frames, np.pixels, cut.units, 0, np.C, 0, np.eps};
   const dim3 grid((unsigned)cut.slices);
   if (np.frames > 0 && cut.form == GradCut::Tiles) {
-    g.n = (np.C + cut.waves - 1) / cut.waves;
+    const int side = cut.wide && cut.run == 32 ? 2 : 1;
+    g.n = (np.C + side * cut.waves - 1) / (side * cut.waves);
     g.per_frame = cut.units / np.frames;
     const dim3 block(64 * cut.waves);
-    const size_t lds = cut.waves > 1 ? 4 * cut.waves * cut.V * 64 * sizeof(float) : 0;
-#define SNLS_TILES(V, R, H)                                                                                            \
-  hipLaunchKernelGGL((norm_grad_tile_kernel<V, R, H>), grid, block, lds, s, grad_y, grad_total, total, stats, gamma,    \
-                     drop, g, grad_x, grad_branch, sums)
-    if (cut.R == 8) SNLS_TILES(4, 8, true);
-    else if (cut.R == 16) SNLS_TILES(2, 16, true);
-    else SNLS_TILES(1, 32, false);
-#undef SNLS_TILES
+    const size_t lds = cut.waves > 1 ? 4 * cut.waves * (cut.wide ? 1 : 4) * 64 * sizeof(float) + (cut.wide ? 2048 + 64 : 0) : 0;
+    const bool whole = np.pixels % 32 == 0;
+#define SNLS_WIDE(L, R) (whole ? norm_grad_wide_kernel<L, R, true> : norm_grad_wide_kernel<L, R, false>)
+    const auto kernel = !cut.wide     ? norm_grad_tile_kernel<8>
+                        : np.C <= 256 ? SNLS_WIDE(64, 32)
+                        : np.C <= 384 ? SNLS_WIDE(32, 24)
+                                      : SNLS_WIDE(32, 32);
+#undef SNLS_WIDE
+    hipLaunchKernelGGL(kernel, grid, block, lds, s, grad_y, grad_total, total, stats, gamma, drop, g, grad_x,
+                       grad_branch, sums);
   } else if (np.frames > 0 && cut.form == GradCut::Tokens) {
 #define SNLS_TOKENS(G, N)                                                                                           \
   hipLaunchKernelGGL((norm_grad_token_kernel<G, N>), grid, dim3(256), 0, s, grad_y, grad_total, total, stats, gamma, \

@@ -67,6 +67,32 @@ struct Philox {
   }
 };
 
+// Value of lane M of the four lanes this one is among.
+template <int M>
+SNLS_DEV unsigned of_four(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, M * 0x55, 0xf, 0xf, false);
+}
+
+// Words of a lane's element in each of four lists, where four lanes hold four
+// consecutive elements of a block in all of them (mine: this lane's place in its
+// block, 0 .. 3): each forms the block of one list, `b`, and they exchange.
+SNLS_DEV void share_blocks(const Words& b, int mine, unsigned* w) {
+  auto pick = [&](unsigned a, unsigned c, unsigned d, unsigned e) { return mine & 2 ? (mine & 1 ? e : d) : (mine & 1 ? c : a); };
+  w[0] = pick(of_four<0>(b.w[0]), of_four<0>(b.w[1]), of_four<0>(b.w[2]), of_four<0>(b.w[3]));
+  w[1] = pick(of_four<1>(b.w[0]), of_four<1>(b.w[1]), of_four<1>(b.w[2]), of_four<1>(b.w[3]));
+  w[2] = pick(of_four<2>(b.w[0]), of_four<2>(b.w[1]), of_four<2>(b.w[2]), of_four<2>(b.w[3]));
+  w[3] = pick(of_four<3>(b.w[0]), of_four<3>(b.w[1]), of_four<3>(b.w[2]), of_four<3>(b.w[3]));
+}
+
+// The same for two lanes with two elements each (odd: this lane has the second
+// two) in two lists.
+SNLS_DEV void share_blocks(const Words& b, int odd, unsigned (*w)[2]) {
+  auto partner = [](unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false); };
+  const unsigned x = partner(odd ? b.w[0] : b.w[2]), y = partner(odd ? b.w[1] : b.w[3]);
+  w[0][0] = odd ? x : b.w[0], w[0][1] = odd ? y : b.w[1];
+  w[1][0] = odd ? b.w[2] : x, w[1][1] = odd ? b.w[3] : y;
+}
+
 SNLS_DEV float dropped(float x, unsigned word, const Drop& d) { return word >= d.thr ? x * d.keep : 0.f; }
 
 }  // namespace snls

@@ -67,19 +67,6 @@ struct ProjectGeo {
   bool aligned;                    // rows of weights at 16 bytes
 };
 
-// The float at `base` (the same for the wave) and a lane's offset in bytes.
-SNLS_DEV float load_at(const float* base, unsigned bytes) {
-  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes);
-}
-template <bool PAST>
-SNLS_DEV void store_at(float* base, unsigned bytes, float v) {
-  float* const to = reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes);
-  if constexpr (PAST)
-    __builtin_nontemporal_store(v, to);
-  else
-    *to = v;
-}
-
 // Forms of a call.  Whole: every plane of the output starts a cache line, which
 // a wave's stores fill, past the caches.  Odd: they do not, and ordinary stores
 // let the L2 join the parts of a line that two waves write (4x48x271x483 to 96
