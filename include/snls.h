@@ -501,7 +501,8 @@ typedef struct {
 /* snls_norm -- layer norm over the channels of every pixel, of x or of a
  * residual sum: total = x + dropout(branch), mean and rstd = 1 / sqrt(variance
  * + eps) over the C channels of a pixel of total (of x without branch), y =
- * (total - mean) * rstd * gamma + beta.  The variance is the mean of the squared
+ * (total - mean) * rstd * gamma + beta (NaN where eps is 0 and a pixel's channels
+ * are all alike).  The variance is the mean of the squared
  * differences from the mean.  Sums of C values and of their squares stay in
  * fp32: |x| * C and (x - mean)^2 * C have to stay in its range.
  *   x       device, (frames, C, pixels)
@@ -515,8 +516,8 @@ typedef struct {
  *           no backward pass follows
  * Nothing is touched when frames == 0.  The result does not depend on
  * scheduling.
- * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for pixels of 2^30 or more
- * or 2^38 elements or more; SNLS_ERR_HIP. */
+ * Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for pixels of 2^29 or more,
+ * C of 2^16 or more, 2^38 elements or more; SNLS_ERR_HIP. */
 snls_status snls_norm(const float* x, const float* branch, const uint64_t* rng, const float* gamma, const float* beta,
                       const snls_norm_params* np, float* total, float* y, float* stats, void* stream);
 
@@ -536,8 +537,8 @@ snls_status snls_norm(const float* x, const float* branch, const uint64_t* rng, 
  *               0), or both NULL
  *   workspace   device scratch of at least snls_norm_workspace_size(np) bytes,
  *               256-byte aligned; not needed without grad_gamma
- * The sums over pixels are held in 64 bits behind the first few hundred terms
- * of each and the result does not depend on scheduling.
+ * No sum over pixels chains more than a few hundred additions in fp32 before 64
+ * bits take over, and the result does not depend on scheduling.
  * Errors: as snls_norm; SNLS_ERR_WORKSPACE. */
 snls_status snls_norm_backward(const float* grad_y, const float* grad_total, const float* total, const float* stats,
                                const float* gamma, const uint64_t* rng, const snls_norm_params* np, float* grad_x,
@@ -635,7 +636,7 @@ snls_status snls_project_pack(const float* w, const snls_project_params* pp, voi
  *           overlaps no input; nothing is touched when frames == 0
  * |x| * 127 * cin has to stay in fp32's range.  The result does not depend on
  * scheduling.  Errors: SNLS_ERR_INVALID_ARG; SNLS_ERR_UNSUPPORTED for cin above
- * SNLS_PROJECT_MAX_CIN, cout of 2^16 or more, pixels of 2^26 or more, 2^38
+ * SNLS_PROJECT_MAX_CIN, cout of 2^16 or more, pixels of 2^25 or more, 2^38
  * elements of x or out or more; SNLS_ERR_HIP. */
 snls_status snls_project(const float* x, const void* codes, const float* scales, const float* bias,
                          const snls_project_params* pp, float* out, void* stream);

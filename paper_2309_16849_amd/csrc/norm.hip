@@ -11,7 +11,7 @@ namespace snls {
 // What a call's kernels share.
 struct NormGeo {
   long long frames, P;
-  long long tiles, per_frame;  // runs of 64 * V pixels, of a frame
+  long long tiles, per_frame;  // runs of pixels, of a frame
   int C, n;                    // n: channels a wave takes
   float eps;
 };
@@ -19,7 +19,13 @@ struct NormGeo {
 // Frames: a workgroup of W waves takes 64 * V consecutive pixels, V a lane, and
 // every wave up to R channels of them; the values stay in registers from their
 // only read on, and the sums over the channels are joined in LDS: first the
-// mean, then the squares of the differences from it.
+// mean, then the squares of the differences from it.  16 bytes an element of a
+// residual sum, 8 without: bandwidth bounds it.  V = 2 keeps more waves on the
+// chip than V = 4 does (5x64x480x854: 201 and 243 us) and needs half the
+// instructions of V = 1 (633 us); 8 channels a wave where 16 waves are enough.
+// Measured: the residual sum with dropout 400 us, 5.3 TB/s.  Where planes do not
+// start a cache line, neighbouring tiles lie on one XCD (4x48x271x483: 72 us, 82
+// in the order of the tiles; at 480x854 that order is the faster, 399 and 426).
 template <int R>
 __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const float* branch, Drop d,
                                                          const float* __restrict__ gamma,
@@ -129,8 +135,8 @@ SNLS_DEV float halve(float a, float b, int lane) {
   }
 }
 
-// Sums over the 64 lanes of LEN values each (a power of two up to 64): lane l
-// returns that of value `listed<LEN>(l)`.
+// Sums over 2 M lanes of LEN values each (a power of two up to 2 M): lane l of
+// them returns that of value l / (2 M / LEN).
 template <int LEN, int M = 32>
 SNLS_DEV float list_sum(float* v, int lane) {
   if constexpr (M == 0) {
@@ -144,11 +150,6 @@ SNLS_DEV float list_sum(float* v, int lane) {
     return list_sum<1, M / 2>(v, lane);
   }
 }
-template <int LEN>
-SNLS_DEV int listed(int lane) {
-  return lane / (64 / LEN);
-}
-
 // Sum over the G lanes of a group.
 template <int G>
 SNLS_DEV float group_sum(float v) {
@@ -259,10 +260,10 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
 
 // Gradients of frames: tiles, waves and channels as in the forward pass.  Both
 // the scaled gradients and the normalised values stay in registers, one join of
-// two sums a tile.  A workgroup walks every gridDim.x-th tile; a wave sums its
-// channels' 2 R terms over the tile's pixels, so that each of its lanes is left
-// with one of the sums, which it adds up over the tiles in 64 bits, and a
-// workgroup writes one row of partial sums.
+// two sums a tile.  A workgroup walks every gridDim.x-th tile, at most 64 of them,
+// and a lane adds up its pixels' 2 R terms of the weights' gradients; at the end
+// a wave's lanes are left with one sum each, and a workgroup writes one row of
+// partial sums.
 template <int R>
 __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_y, const float* grad_total,
                                                               const float* __restrict__ total,
@@ -349,7 +350,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
   }
   if (!sums) return;
   const double acc = (double)list_sum<2 * R>(over, lane);  // this lane's of the 2 R sums
-  const int which = listed<2 * R>(lane), c = which % R;
+  const int which = lane / (32 / R), c = which % R;
   if (lane % (32 / R) == 0 && c < n) sums[((long long)blockIdx.x * 2 + which / R) * g.C + c0 + c] = acc;
 }
 
@@ -544,8 +545,7 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
   }
 }
 
-// More channels than registers hold.
-// A thread per pixel: gradients of the input and the branch.
+// More channels than registers hold: a thread per pixel, gradients of the input and the branch.
 __global__ void __launch_bounds__(256) norm_grad_kernel(const float* grad_y, const float* grad_total,
                                                         const float* __restrict__ total,
                                                         const float* __restrict__ stats,
@@ -656,8 +656,9 @@ static GradCut grad_cut(const snls_norm_params& np) {
     c.slices = 64;
     return c;
   }
-  // the chip is full with 512; 64 units a workgroup at most
-  c.slices = std::max(std::min(c.units, 512LL), (c.units + 63) / 64);
+  // the chip is full with 512; 64 units a workgroup at most, but for lists that no
+  // launch of so many workgroups holds
+  c.slices = std::min(std::max(std::min(c.units, 512LL), (c.units + 63) / 64), 1LL << 20);
   return c;
 }
 

@@ -330,9 +330,11 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   const long long want = std::max(1LL, 512 / g.groups);
   const int split = (int)(want < tiles ? want : tiles);
   g.span = (tiles + split - 1) / split;
-  const int fit = 60 / nk;  // 60 KB of weights at once, or two buffers of 32 KB
-  g.buffers = g.span <= fit ? 1 : 2;
-  g.hold = g.span <= fit ? g.span : 32 / nk;
+  // 60 KB of weights and what goes with them at once, or two buffers of 32 KB, of
+  // one tile at least (33 KB with 1,024 channels)
+  const int tile = nk * 1024 + 512;
+  g.buffers = g.span * tile <= 60 * 1024 ? 1 : 2;
+  g.hold = g.buffers == 1 ? g.span : std::max(1, 32 * 1024 / tile);
   g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
   const dim3 grid((unsigned)(g.groups < 1280 ? g.groups : 1280), (unsigned)((tiles + g.span - 1) / g.span));
   const bool whole = pp.pixels % 32 == 0 && !(reinterpret_cast<uintptr_t>(out) & 127);

@@ -104,7 +104,8 @@ snls_status check_norm(const snls_norm_params* np) {
   if (np->C < 1 || np->frames < 0 || np->pixels < 1) return SNLS_ERR_INVALID_ARG;
   if (!isfinite(np->eps) || np->eps < 0.f) return SNLS_ERR_INVALID_ARG;
   if (!(np->drop >= 0.f && np->drop < 1.f)) return SNLS_ERR_INVALID_ARG;
-  if (np->pixels >= kMaxPlane || too_many(np->frames, np->C, np->pixels)) return SNLS_ERR_UNSUPPORTED;
+  // (the place of a lane in its plane, and in the next, is a 32-bit offset in bytes)
+  if (np->pixels >= 1 << 29 || np->C >= 1 << 16 || too_many(np->frames, np->C, np->pixels)) return SNLS_ERR_UNSUPPORTED;
   return SNLS_OK;
 }
 
@@ -153,7 +154,8 @@ snls_status check_project(const snls_project_params* pp) {
   if (!pp || pp->struct_size != sizeof(snls_project_params)) return SNLS_ERR_INVALID_ARG;
   if (pp->cin < 1 || pp->cout < 1 || pp->parts < 1 || pp->frames < 0 || pp->pixels < 1) return SNLS_ERR_INVALID_ARG;
   if (pp->cout % pp->parts != 0) return SNLS_ERR_INVALID_ARG;
-  if (pp->cin > SNLS_PROJECT_MAX_CIN || pp->cout >= 1 << 16 || pp->pixels >= 1 << 26) return SNLS_ERR_UNSUPPORTED;
+  // (the place of a lane in its plane, or 16 planes on, is a 32-bit offset in bytes)
+  if (pp->cin > SNLS_PROJECT_MAX_CIN || pp->cout >= 1 << 16 || pp->pixels >= 1 << 25) return SNLS_ERR_UNSUPPORTED;
   if (too_many(pp->frames, pp->cin, pp->pixels) || too_many(pp->frames, pp->cout, pp->pixels))
     return SNLS_ERR_UNSUPPORTED;
   return SNLS_OK;

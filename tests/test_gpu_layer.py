@@ -50,7 +50,8 @@ SHAPES = [(1, 1, 1, 1, 1), (1, 1, 3, 1, 1), (1, 1, 16, 1, 2), (2, 3, 16, 13, 17)
           (1, 1, 64, 5, 103), (2, 1, 65, 8, 33), (1, 1, 192, 15, 17), (1, 2, 256, 6, 43), (1, 1, 257, 3, 22),
           (1, 1, 300, 9, 32), (1, 1, 1030, 3, 23), (3, 20, 1, 1), (2, 100, 1, 3),
           (1, 1), (1, 7), (1, 64), (2, 192), (3, 193), (65, 48), (257, 64), (300, 16), (5, 256), (7, 1000), (3, 1024),
-          (2, 1500), (1000, 20)]
+          (2, 1500), (1000, 20), (1, 2, 128, 9, 15), (1, 1, 129, 8, 12), (2, 1, 384, 5, 13), (1, 1, 385, 4, 16), (1, 1, 512, 3, 20),
+          (1, 1, 513, 2, 9), (4, 2050)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
@@ -276,7 +277,8 @@ def test_rotate_points(dev, n, rp, interleaved):
 # (shape of x, cout, parts): channels around the matrix instructions' steps, odd pixels
 PROJ = [((1, 1, 1, 1, 1), 1, 1), ((1, 2, 16, 5, 7), 48, 3), ((2, 1, 64, 9, 33), 192, 3), ((1, 1, 48, 11, 12), 33, 1),
         ((1, 1, 33, 3, 41), 66, 2), ((1, 1, 192, 8, 9), 64, 1), ((1, 1, 250, 4, 8), 100, 4), ((1, 1, 256, 8, 8), 256, 2),
-        ((1, 1, 300, 5, 5), 31, 1), ((1, 1, 1024, 3, 11), 40, 2), ((2, 3, 100, 1, 3), 70, 2),
+        ((1, 1, 300, 5, 5), 31, 1), ((1, 1, 1024, 3, 11), 40, 2), ((2, 3, 100, 1, 3), 70, 2), ((1, 1, 16, 5, 8), 2100, 3), ((1, 2, 384, 4, 32), 390, 2), ((1, 1, 20, 1, 64), 2048, 1),
+        ((1, 3, 240, 8, 16), 96, 3),
         ((1, 1), 1, 1), ((1, 192), 576, 3), ((2, 64), 192, 3), ((33, 48), 144, 3), ((65, 20), 34, 2), ((1, 1023), 96, 1),
         ((130, 256), 300, 3), ((1, 1024), 4097, 1), ((1000, 16), 32, 1), ((3, 130), 5, 5)]
 

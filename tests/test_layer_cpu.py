@@ -51,8 +51,8 @@ def test_the_package_offers_them():
 BAD_NORM = [
     (dict(C=0), BAD), (dict(frames=-1), BAD), (dict(pixels=0), BAD), (dict(eps=-1e-5), BAD), (dict(eps=math.inf), BAD),
     (dict(eps=math.nan), BAD), (dict(drop=1.0), BAD), (dict(drop=-0.1), BAD), (dict(drop=math.nan), BAD),
-    (dict(size=36), BAD), (dict(pixels=1 << 30), BEYOND), (dict(C=1 << 20, frames=1 << 18), BEYOND),
-    (dict(frames=1 << 60, pixels=1 << 29), BEYOND),
+    (dict(size=36), BAD), (dict(pixels=1 << 29), BEYOND), (dict(C=1 << 16), BEYOND), (dict(C=1 << 15, frames=1 << 20), BEYOND),
+    (dict(frames=1 << 60, pixels=1 << 28), BEYOND),
 ]
 
 
@@ -130,7 +130,7 @@ def test_rotate_refuses_bad_arguments(lib):
 BAD_PROJ = [
     (dict(cin=0), BAD), (dict(cout=0, parts=1), BAD), (dict(parts=0), BAD), (dict(parts=5), BAD), (dict(frames=-1), BAD),
     (dict(pixels=0), BAD), (dict(size=28), BAD), (dict(cin=1025), BEYOND), (dict(cout=3 << 15), BEYOND),
-    (dict(pixels=1 << 26), BEYOND), (dict(frames=1 << 36), BEYOND), (dict(frames=1 << 50, pixels=1 << 20), BEYOND),
+    (dict(pixels=1 << 25), BEYOND), (dict(frames=1 << 36), BEYOND), (dict(frames=1 << 50, pixels=1 << 20), BEYOND),
 ]
 
 
