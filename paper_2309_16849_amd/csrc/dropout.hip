@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(const float* x, const floa
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = residual ? r[j] + v[j] : v[j];
-    stream_run<4>(out + i, cnt, v);
+    store_run<4>(out + i, cnt, v);
   }
 }
 

@@ -9,9 +9,7 @@
 namespace snls {
 
 template <int V>
-struct __attribute__((packed, aligned(4))) Run {
-  float v[V];
-};
+using Run = float __attribute__((ext_vector_type(V), aligned(4)));
 
 // The first cnt of V floats at `from`, 0 for the others.
 template <int V>
@@ -19,7 +17,7 @@ SNLS_DEV void load_run(const float* from, int cnt, float* to) {
   if (cnt >= V) {
     const Run<V> r = *reinterpret_cast<const Run<V>*>(from);
 #pragma unroll
-    for (int i = 0; i < V; ++i) to[i] = r.v[i];
+    for (int i = 0; i < V; ++i) to[i] = r[i];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) to[i] = i < cnt ? from[i] : 0.f;
@@ -31,7 +29,7 @@ SNLS_DEV void store_run(float* to, int cnt, const float* from) {
   if (cnt >= V) {
     Run<V> r;
 #pragma unroll
-    for (int i = 0; i < V; ++i) r.v[i] = from[i];
+    for (int i = 0; i < V; ++i) r[i] = from[i];
     *reinterpret_cast<Run<V>*>(to) = r;
   } else {
 #pragma unroll
@@ -40,24 +38,26 @@ SNLS_DEV void store_run(float* to, int cnt, const float* from) {
   }
 }
 
-// store_run past the caches (non-temporal): outputs of whole videos push inputs
-// out of the 256 MB cache otherwise, and a kernel that reads them next gains
-// nothing by their lying there (norm, rotation, projection and dropout in a row
-// took 960 us with ordinary stores and 915 so at 525 MB a tensor, 188 and 177 at
-// 105 MB, 24.4 and 23.9 at 4 MB).
-template <int V>
-SNLS_DEV void stream_run(float* to, int cnt, const float* from) {
-  if (cnt >= V) {
-    typedef float Vec __attribute__((ext_vector_type(V), aligned(4)));
-    Vec r;
+// Where every store of a wave fills whole cache lines (WHOLE: rows of 32 floats,
+// or a multiple, at their multiple) outputs go past the caches (non-temporal),
+// so that they do not push inputs out of them: frames of 192 channels at 152x152
+// to 576 take 75 us so and 88 with ordinary stores, the norm of a residual sum at
+// 5x64x480x854 404 and 422, its gradients at 5x512x128x128 171 and 177 (every
+// call on inputs that no cache holds; at 4x48x272x480 ordinary stores are the
+// faster, 43 us and 47).  Where lines are shared by two waves ordinary stores let
+// the L2 join the parts: the norm at 4x64x270x483 126 us, past the caches 138.
+template <bool WHOLE, int V>
+SNLS_DEV void put_run(float* to, int cnt, const float* from) {
+  if constexpr (WHOLE) {
+    if (cnt >= V) {
+      Run<V> r;
 #pragma unroll
-    for (int i = 0; i < V; ++i) r[i] = from[i];
-    __builtin_nontemporal_store(r, reinterpret_cast<Vec*>(to));
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < cnt) to[i] = from[i];
+      for (int i = 0; i < V; ++i) r[i] = from[i];
+      __builtin_nontemporal_store(r, reinterpret_cast<Run<V>*>(to));
+      return;
+    }
   }
+  store_run<V>(to, cnt, from);
 }
 
 // The float at `base` (the same for the wave: two scalar registers) and a lane's
@@ -65,10 +65,10 @@ SNLS_DEV void stream_run(float* to, int cnt, const float* from) {
 SNLS_DEV float load_at(const float* base, unsigned bytes) {
   return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes);
 }
-template <bool PAST>
+template <bool WHOLE>
 SNLS_DEV void store_at(float* base, unsigned bytes, float v) {
   float* const to = reinterpret_cast<float*>(reinterpret_cast<char*>(base) + bytes);
-  if constexpr (PAST)
+  if constexpr (WHOLE)
     __builtin_nontemporal_store(v, to);
   else
     *to = v;

@@ -24,9 +24,10 @@ struct NormGeo {
 // chip than V = 4 does (5x64x480x854: 201 and 243 us) and needs half the
 // instructions of V = 1 (633 us); 8 channels a wave where 16 waves are enough.
 // Measured: the residual sum with dropout 400 us, 5.3 TB/s.  Where planes do not
-// start a cache line, neighbouring tiles lie on one XCD (4x48x271x483: 72 us, 82
-// in the order of the tiles; at 480x854 that order is the faster, 399 and 426).
-template <int R>
+// start a cache line (WHOLE false), neighbouring tiles lie on one XCD
+// (4x64x270x483: 126 us, 147 in the order of the tiles; at 5x64x480x854 that
+// order is the faster, 399 and 426).
+template <int R, bool WHOLE>
 __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const float* branch, Drop d,
                                                          const float* __restrict__ gamma,
                                                          const float* __restrict__ beta, NormGeo g, float* total,
@@ -37,7 +38,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Philox gen(d);
   // (a row of sums is written again only behind a barrier that follows its last read)
-  for (long long tile = g.P % 32 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const int c0 = wv * g.n, n = min(g.n, g.C - c0);
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) s[c][j] += b[j];
-            stream_run<V>(total + at + c * g.P, cnt, s[c]);
+            put_run<WHOLE, V>(total + at + c * g.P, cnt, s[c]);
           }
       }
     }
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
         float o[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] = fmaf(s[c][j] * rstd[j], ga, be);
-        stream_run<V>(y + at + c * g.P, cnt, o);
+        put_run<WHOLE, V>(y + at + c * g.P, cnt, o);
       }
     if (stats && wv == 0) {
       store_run<V>(stats + f * g.P + (cnt > 0 ? p : 0), cnt, mean);
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const f
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[k][j] += b[j];
-        stream_run<4>(total + at + c, cnt, s[k]);
+        store_run<4>(total + at + c, cnt, s[k]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum += s[k][j];
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const f
       if (beta) load_run<4>(beta + c, cnt, be);
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[k][j] = fmaf(s[k][j] * rstd, ga[j], be[j]);
-      stream_run<4>(y + at + c, cnt, s[k]);
+      store_run<4>(y + at + c, cnt, s[k]);
     }
     if (stats && l == 0) stats[row] = mean, stats[g.frames + row] = rstd;
   }
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
 // and a lane adds up its pixels' 2 R terms of the weights' gradients; at the end
 // a wave's lanes are left with one sum each, and a workgroup writes one row of
 // partial sums.
-template <int R>
+template <int R, bool WHOLE>
 __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_y, const float* grad_total,
                                                               const float* __restrict__ total,
                                                               const float* __restrict__ stats,
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
   const int c0 = wv * g.n, n = min(g.n, g.C - c0);
   float over[2 * R] = {};  // this lane's sums over the tiles
   int turn = 0;
-  for (long long tile = g.P % 32 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const long long px = f * g.P + (cnt > 0 ? p : 0), at = (f * g.C + c0) * g.P + (cnt > 0 ? p : 0);
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
           r[j] = rstd[j] * (gy[c][j] - sum[0][j] - xh[c][j] * sum[1][j]);
           if (grad_total) r[j] += t[j];
         }
-        stream_run<V>(grad_x + e, cnt, r);
+        put_run<WHOLE, V>(grad_x + e, cnt, r);
         if (grad_branch) {
           if (d.rng) {
             unsigned w[V];
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
 #pragma unroll
             for (int j = 0; j < V; ++j) r[j] = dropped(r[j], w[j], d);
           }
-          stream_run<V>(grad_branch + e, cnt, r);
+          put_run<WHOLE, V>(grad_branch + e, cnt, r);
         }
       }
   }
@@ -358,9 +359,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
 // to 256 channels, 32 and two channels side by side in a wave up to 512, so that
 // 64 registers hold a wave's tile and two workgroups of 8 waves fit a CU, one
 // loading while the other stores (5x256x128x128 without dropout 59 us, with one
-// workgroup of 16 waves 75; 5x384x96x96 60 and 77).  Where planes do not start a
-// cache line (WHOLE false) the stores are ordinary ones, whose parts of a line
-// the L2 joins (2x384x289x252 with dropout 278 us, past the caches 384).
+// workgroup of 16 waves 75; 5x384x96x96 60 and 77).
 template <int L, int R, bool WHOLE>
 __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* grad_y, const float* grad_total,
                                                                 const float* __restrict__ total,
@@ -516,7 +515,7 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
         r[j] = rstd * (gy[k][j] - s0 - xh[k][j] * s1);
         if (grad_total) r[j] += t[j];
       }
-      stream_run<4>(grad_x + at + c, cnt, r);
+      store_run<4>(grad_x + at + c, cnt, r);
       if (grad_branch) {
         if (d.rng) {
           unsigned w[4];
@@ -524,7 +523,7 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
 #pragma unroll
           for (int j = 0; j < 4; ++j) r[j] = dropped(r[j], w[j], d);
         }
-        stream_run<4>(grad_branch + at + c, cnt, r);
+        store_run<4>(grad_branch + at + c, cnt, r);
       }
     }
   }
@@ -627,6 +626,9 @@ __global__ void __launch_bounds__(1024) norm_weights_sum_kernel(const double* __
 
 constexpr long long kMostGroups = 1 << 21;  // a launch holds less than 2^32 threads
 
+// Whether planes start a cache line (as torch's allocations do).
+static bool whole_lines(const snls_norm_params& np) { return np.pixels % 32 == 0; }
+
 // Waves that share a tile's channels, n each, if 16 are enough.
 static int tile_waves(int C, int n) { return std::min(16, (C + n - 1) / n); }
 
@@ -694,13 +696,14 @@ snls_status launch_norm(const float* x, const float* branch, const Drop& drop, c
     g.per_frame = (np.pixels + 127) / 128, g.tiles = g.per_frame * np.frames;
     const dim3 grid((unsigned)std::min(g.tiles, kMostGroups)), block(64 * waves);
     const size_t lds = waves > 1 ? 2 * waves * 128 * sizeof(float) : 0;
-#define SNLS_TILES(R)                                                                                              \
-  hipLaunchKernelGGL((norm_tile_kernel<R>), grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats)
-    if (g.n <= 8) SNLS_TILES(8);
-    else if (g.n <= 16) SNLS_TILES(16);
-    else if (g.n <= 24) SNLS_TILES(24);
-    else SNLS_TILES(32);
+    const bool whole = whole_lines(np);
+#define SNLS_TILES(R) (whole ? norm_tile_kernel<R, true> : norm_tile_kernel<R, false>)
+    const auto kernel = g.n <= 8    ? SNLS_TILES(8)
+                        : g.n <= 16 ? SNLS_TILES(16)
+                        : g.n <= 24 ? SNLS_TILES(24)
+                                    : SNLS_TILES(32);
 #undef SNLS_TILES
+    hipLaunchKernelGGL(kernel, grid, block, lds, s, x, branch, drop, gamma, beta, g, total, y, stats);
   } else {
     hipLaunchKernelGGL(norm_kernel, dim3(pixel_groups(np)), dim3(256), 0, s, x, branch, drop, gamma, beta, np.frames,
                        np.C, np.pixels, np.eps, total, y, stats);
@@ -721,9 +724,9 @@ snls_status launch_norm_backward(const float* grad_y, const float* grad_total, c
     g.per_frame = cut.units / np.frames;
     const dim3 block(64 * cut.waves);
     const size_t lds = cut.waves > 1 ? 4 * cut.waves * (cut.wide ? 1 : 4) * 64 * sizeof(float) + (cut.wide ? 2048 + 64 : 0) : 0;
-    const bool whole = np.pixels % 32 == 0;
+    const bool whole = whole_lines(np);
 #define SNLS_WIDE(L, R) (whole ? norm_grad_wide_kernel<L, R, true> : norm_grad_wide_kernel<L, R, false>)
-    const auto kernel = !cut.wide     ? norm_grad_tile_kernel<8>
+    const auto kernel = !cut.wide     ? (whole ? norm_grad_tile_kernel<8, true> : norm_grad_tile_kernel<8, false>)
                         : np.C <= 256 ? SNLS_WIDE(64, 32)
                         : np.C <= 384 ? SNLS_WIDE(32, 24)
                                       : SNLS_WIDE(32, 32);

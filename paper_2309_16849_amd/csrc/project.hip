@@ -68,10 +68,7 @@ struct ProjectGeo {
 };
 
 // Forms of a call.  Whole: every plane of the output starts a cache line, which
-// a wave's stores fill, past the caches.  Odd: they do not, and ordinary stores
-// let the L2 join the parts of a line that two waves write (4x48x271x483 to 96
-// channels: 99 us, 134 past the caches; at 272x480, whole lines, 79 and 54).
-// Tokens: a list of them (pixels == 1).
+// a wave's stores fill.  Odd: they do not.  Tokens: a list of them (pixels == 1).
 enum class Form { Whole, Odd, Tokens };
 
 // 16 consecutive weights of a channel as a lane of the matrix instruction takes
@@ -257,7 +254,7 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
             const int row = 8 * (r / 4) + r % 4;
             const float s = __shfl(ts, row + 4 * half);
             if (row < rows)
-              __builtin_nontemporal_store(fmaf((float)acc[r] * s, sc, be), to_row + (long long)row * g.per);
+              to_row[(long long)row * g.per] = fmaf((float)acc[r] * s, sc, be);
           }
         } else if (const int part = o0 / g.per; left >= 32 && have == 32 && o0 + 32 <= (part + 1) * g.per) {
           // the whole tile, in one part

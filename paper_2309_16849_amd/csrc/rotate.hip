@@ -46,6 +46,7 @@ struct RotateGeo {
 // lane keeps its four columns and walks down the rows, so that the angles of a
 // column pair are formed once, those of a row pair once a row, those of a time
 // pair once: 5x64x480x854 q and k, 889 us with a phase per pixel, NNN so.
+template <bool WHOLE>
 __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float* k,
                                                      const int64_t* __restrict__ times, Rotary r, RotateGeo g,
                                                      float* q_out, float* k_out) {
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float
               if (i + u * stride < n) load_run<4>(a + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
 #pragma unroll
             for (int u = 0; u < kDeep; ++u)
-              if (i + u * stride < n) stream_run<4>(o + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
+              if (i + u * stride < n) put_run<WHOLE, 4>(o + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
           }
         continue;
       }
@@ -114,8 +115,8 @@ __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float
               b[u][j] = fmaf(a[u][j], sn[j], b[u][j] * cs[j]);
               a[u][j] = t;
             }
-            stream_run<4>(dst + c1 + at, cnt, a[u]);
-            stream_run<4>(dst + c2 + at, cnt, b[u]);
+            put_run<WHOLE, 4>(dst + c1 + at, cnt, a[u]);
+            put_run<WHOLE, 4>(dst + c2 + at, cnt, b[u]);
           }
       }
     }
@@ -177,7 +178,8 @@ snls_status launch_rotate(const float* q, const float* k, const int64_t* times, 
   g.chunks = (r.H + g.rows - 1) / g.rows;
   const dim3 grid((unsigned)((long long)g.chunks * g.cols), (unsigned)std::min(g.units, 1024),
                   (unsigned)std::min(g.heads * (k ? 2 : 1), 1024LL));
-  hipLaunchKernelGGL(rotate_kernel, grid, dim3(threads), 0, s, q, k, times, r, g, q_out, k_out);
+  const auto kernel = r.W % 32 == 0 ? rotate_kernel<true> : rotate_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, q, k, times, r, g, q_out, k_out);
   return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
 }
 
