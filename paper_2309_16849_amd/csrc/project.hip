@@ -333,7 +333,12 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   g.buffers = g.span * tile <= 60 * 1024 ? 1 : 2;
   g.hold = g.buffers == 1 ? g.span : std::max(1, 32 * 1024 / tile);
   g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
-  const dim3 grid((unsigned)(g.groups < 1280 ? g.groups : 1280), (unsigned)((tiles + g.span - 1) / g.span));
+  // as many workgroups as the chip holds at once, by registers and by LDS (64 ->
+  // 192 channels at 480x854: 90 us, 94 with 5 a CU, where 4 fit; 48 -> 96 at
+  // 271x483 73 and 89)
+  const int by_regs = nk <= 2 ? 4 : nk == 3 ? 3 : 2, by_lds = 160 * 1024 / (g.buffers * g.hold * tile);
+  const dim3 grid((unsigned)std::min(g.groups, 256LL * std::min(by_regs, by_lds)),
+                  (unsigned)((tiles + g.span - 1) / g.span));
   const bool whole = pp.pixels % 32 == 0 && !(reinterpret_cast<uintptr_t>(out) & 127);
   const Form form = tokens ? Form::Tokens : whole ? Form::Whole : Form::Odd;
   switch (nk) {
