@@ -74,12 +74,20 @@ SNLS_DEV void store_at(float* base, unsigned bytes, float v) {
     *to = v;
 }
 
-// Workgroup b of n in an order that gives each of the 8 XCDs, which take
-// workgroups in turn, a run of neighbours: what two of them write of one cache
-// line meets in one L2.
-SNLS_DEV unsigned by_xcd(unsigned b, unsigned n) {
-  const unsigned per = n / 8;
-  return b < per * 8 ? (b & 7) * per + b / 8 : b;
+// The items this workgroup takes of `items`.  By the 8 XCDs, which take
+// workgroups in turn, neighbours lie on one of them: what two workgroups write of
+// one cache line meets in one L2.  Every XCD has its eighth of the items, and its
+// workgroups walk it together.
+struct Walk {
+  long long first, end, step;
+};
+template <bool BY_XCD>
+SNLS_DEV Walk walk(long long items) {
+  const unsigned b = blockIdx.x, n = gridDim.x, x = b & 7;
+  if (!BY_XCD || n < 8) return {b, items, n};
+  if (n % 8 == 0) return {items * x / 8 + b / 8, items * (x + 1) / 8, n / 8};
+  const unsigned per = n / 8;  // (as many workgroups as items, or nearly)
+  return {b < per * 8 ? x * per + b / 8 : b, items, n};
 }
 
 }  // namespace snls

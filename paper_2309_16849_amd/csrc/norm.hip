@@ -38,7 +38,8 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Philox gen(d);
   // (a row of sums is written again only behind a barrier that follows its last read)
-  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
+  const Walk way = walk<!WHOLE>(g.tiles);
+  for (long long tile = way.first; tile < way.end; tile += way.step) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const int c0 = wv * g.n, n = min(g.n, g.C - c0);
@@ -280,7 +281,8 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
   const int c0 = wv * g.n, n = min(g.n, g.C - c0);
   float over[2 * R] = {};  // this lane's sums over the tiles
   int turn = 0;
-  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
+  const Walk way = walk<!WHOLE>(g.tiles);
+  for (long long tile = way.first; tile < way.end; tile += way.step) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * (64 * V) + lane * V;
     const int cnt = (int)max(0LL, min((long long)V, g.P - p));
     const long long px = f * g.P + (cnt > 0 ? p : 0), at = (f * g.C + c0) * g.P + (cnt > 0 ? p : 0);
@@ -379,7 +381,8 @@ __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* gra
   __syncthreads();
   double acc[R / 8] = {};
   int turn = 0;
-  for (long long tile = WHOLE ? blockIdx.x : by_xcd(blockIdx.x, gridDim.x); tile < g.tiles; tile += gridDim.x) {
+  const Walk way = walk<!WHOLE>(g.tiles);
+  for (long long tile = way.first; tile < way.end; tile += way.step) {
     const long long f = tile / g.per_frame, p = (tile - f * g.per_frame) * L;
     const bool in = l < g.P - p;
     const unsigned here = in ? l : 0;

@@ -146,7 +146,8 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
   };
 
   bool staged = false;
-  for (long long grp = FORM == Form::Odd ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x; grp < g.groups; grp += gridDim.x) {
+  const Walk way = walk<FORM == Form::Odd>(g.groups);
+  for (long long grp = way.first; grp < way.end; grp += way.step) {
     const long long f = TOK ? 0 : grp / g.per_frame;
     const long long p0 = (TOK ? grp : grp - f * g.per_frame) * 128 + wv * 32;  // this wave's first pixel or token
     const int have = (int)max(0LL, min(32LL, (TOK ? g.F : g.P) - p0));         // of its 32
