@@ -399,7 +399,8 @@ __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* gra
       for (int k = 0; k < R; ++k, a += step, b += step)
         if (k < n) gy[k] = load_at(a, place(k)), xh[k] = load_at(b, place(k));
     }
-    const float mean = load_at(stats + f * g.P + p, here * 4u), rstd = load_at(stats + (g.frames + f) * g.P + p, here * 4u);
+    const float mean = load_at(stats + f * g.P + p, here * 4u);
+    const float rstd = load_at(stats + (g.frames + f) * g.P + p, here * 4u);
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int k0 = 0; k0 < R; k0 += 8)
@@ -686,16 +687,12 @@ snls_status launch_norm(const float* x, const float* branch, const Drop& drop, c
     const int per = np.C <= 128 ? 16 : 4;
     const long long groups = (np.frames + per - 1) / per;
     const dim3 grid((unsigned)std::min(groups, kMostGroups));
-    if (np.C <= 64)
-      hipLaunchKernelGGL((norm_token_kernel<16, 1>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else if (np.C <= 128)
-      hipLaunchKernelGGL((norm_token_kernel<16, 2>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else if (np.C <= 256)
-      hipLaunchKernelGGL((norm_token_kernel<64, 1>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else if (np.C <= 1024)
-      hipLaunchKernelGGL((norm_token_kernel<64, 4>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
-    else
-      hipLaunchKernelGGL((norm_token_kernel<64, 8>), grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
+    const auto kernel = np.C <= 64     ? norm_token_kernel<16, 1>
+                        : np.C <= 128  ? norm_token_kernel<16, 2>
+                        : np.C <= 256  ? norm_token_kernel<64, 1>
+                        : np.C <= 1024 ? norm_token_kernel<64, 4>
+                                       : norm_token_kernel<64, 8>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, x, branch, drop, gamma, beta, g, total, y, stats);
   } else if (np.pixels > 1 && np.C <= 512) {
     const int waves = tile_waves(np.C, 8);
     g.n = (np.C + waves - 1) / waves;
@@ -729,7 +726,8 @@ snls_status launch_norm_backward(const float* grad_y, const float* grad_total, c
     g.n = (np.C + side * cut.waves - 1) / (side * cut.waves);
     g.per_frame = cut.units / np.frames;
     const dim3 block(64 * cut.waves);
-    const size_t lds = cut.waves > 1 ? 4 * cut.waves * (cut.wide ? 1 : 4) * 64 * sizeof(float) + (cut.wide ? 2048 + 64 : 0) : 0;
+    // two tables of two rows a wave, one pixel or four a lane; many channels: gamma
+    const size_t lds = cut.waves > 1 ? 4 * cut.waves * (cut.wide ? 1 : 4) * 256 + (cut.wide ? 512 * 4 : 0) : 0;
     const bool whole = whole_lines(np);
 #define SNLS_WIDE(L, R) (whole ? norm_grad_wide_kernel<L, R, true> : norm_grad_wide_kernel<L, R, false>)
     const auto kernel = !cut.wide     ? (whole ? norm_grad_tile_kernel<8, true> : norm_grad_tile_kernel<8, false>)
@@ -740,14 +738,12 @@ snls_status launch_norm_backward(const float* grad_y, const float* grad_total, c
     hipLaunchKernelGGL(kernel, grid, block, lds, s, grad_y, grad_total, total, stats, gamma, drop, g, grad_x,
                        grad_branch, sums);
   } else if (np.frames > 0 && cut.form == GradCut::Tokens) {
-#define SNLS_TOKENS(G, N)                                                                                           \
-  hipLaunchKernelGGL((norm_grad_token_kernel<G, N>), grid, dim3(256), 0, s, grad_y, grad_total, total, stats, gamma, \
-                     drop, g, grad_x, grad_branch, sums)
-    if (np.C <= 64) SNLS_TOKENS(16, 1);
-    else if (np.C <= 128) SNLS_TOKENS(16, 2);
-    else if (np.C <= 256) SNLS_TOKENS(64, 1);
-    else SNLS_TOKENS(64, 4);
-#undef SNLS_TOKENS
+    const auto kernel = np.C <= 64    ? norm_grad_token_kernel<16, 1>
+                        : np.C <= 128 ? norm_grad_token_kernel<16, 2>
+                        : np.C <= 256 ? norm_grad_token_kernel<64, 1>
+                                      : norm_grad_token_kernel<64, 4>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, grad_y, grad_total, total, stats, gamma, drop, g, grad_x,
+                       grad_branch, sums);
   } else {
     // the sums over the pixels come first: grad_x may be grad_y
     if (sums && np.frames > 0)

@@ -77,7 +77,9 @@ SNLS_DEV unsigned of_four(unsigned v) {
 // consecutive elements of a block in all of them (mine: this lane's place in its
 // block, 0 .. 3): each forms the block of one list, `b`, and they exchange.
 SNLS_DEV void share_blocks(const Words& b, int mine, unsigned* w) {
-  auto pick = [&](unsigned a, unsigned c, unsigned d, unsigned e) { return mine & 2 ? (mine & 1 ? e : d) : (mine & 1 ? c : a); };
+  auto pick = [&](unsigned a, unsigned c, unsigned d, unsigned e) {
+    return mine & 2 ? (mine & 1 ? e : d) : (mine & 1 ? c : a);
+  };
   w[0] = pick(of_four<0>(b.w[0]), of_four<0>(b.w[1]), of_four<0>(b.w[2]), of_four<0>(b.w[3]));
   w[1] = pick(of_four<1>(b.w[0]), of_four<1>(b.w[1]), of_four<1>(b.w[2]), of_four<1>(b.w[3]));
   w[2] = pick(of_four<2>(b.w[0]), of_four<2>(b.w[1]), of_four<2>(b.w[2]), of_four<2>(b.w[3]));

@@ -46,9 +46,10 @@ struct Quant {
       for (int j = 0; j < 16; ++j) f[j] = settle(f[j], x[j]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned a = __builtin_amdgcn_perm(__float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j]), 0x0c0c0400u);
-      const unsigned b = __builtin_amdgcn_perm(__float_as_uint(f[4 * j + 3]), __float_as_uint(f[4 * j + 2]), 0x04000c0cu);
-      out[j] = (int)(a | b);
+      unsigned u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(f[4 * j + i]);
+      out[j] = (int)(__builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u) | __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu));
     }
   }
 };
@@ -94,8 +95,12 @@ SNLS_DEV Int4 weights16(const int8_t* __restrict__ w, int o, int c, const Projec
 // they never leave the registers.  The weights lie in LDS in the order of the
 // lanes.  NK: steps of 32 channels.  A list of tokens has rows and columns in each
 // other's place, so that stores run along the output channels.
-// Up to KEEP steps, the values stay in registers between the maximum and the
-// codes; beyond, they are read again.
+// 4 bytes an input and an output channel a pixel: up to some hundred channels
+// bandwidth bounds it (64 -> 192 at 480x854 86 us, 4.9 TB/s; 192 -> 576 at
+// 5x152x152 75 us, 4.7), beyond the values' second read and the weights' way into
+// LDS (512 -> 512 at 2x128x128 60 us, 284 TOP/s).  Up to KEEP steps, the values stay
+// in registers between the maximum and the codes; beyond, they are read again,
+// four steps at a time.
 template <int NK, Form FORM>
 __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
                                                          const float* __restrict__ scales,

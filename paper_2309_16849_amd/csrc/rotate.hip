@@ -42,10 +42,11 @@ struct RotateGeo {
   int rows, chunks;        // chunks of rows
 };
 
-// 16 bytes an element pair read and as many written: bandwidth bounds it.  A
-// lane keeps its four columns and walks down the rows, so that the angles of a
-// column pair are formed once, those of a row pair once a row, those of a time
-// pair once: 5x64x480x854 q and k, 889 us with a phase per pixel, NNN so.
+// 8 bytes a pair read and as many written: bandwidth bounds it.  A lane keeps its
+// four columns and walks down the rows, kDeep of them in flight, so that the
+// angles of a column pair are formed once, those of a row pair once a row, those
+// of a time pair once: 5x64x480x854 q and k, 889 us with a thread and a phase per
+// pixel, 405 so (5.2 TB/s).
 template <bool WHOLE>
 __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float* k,
                                                      const int64_t* __restrict__ times, Rotary r, RotateGeo g,

@@ -210,7 +210,7 @@ def test_norm_gradient_formula(shape):
         for s in (h, -h):
             z = x.detach().clone()
             z.view(-1)[i] += s
-            f.append(float((R.norm(z, gamma, beta, 1e-5)[0] * gy).sum() + (z * gt).sum()))
+            f.append(float(((R.norm(z, gamma, beta, 1e-5)[0] * gy).sum() + (z * gt).sum()).detach()))
         assert abs((f[0] - f[1]) / (2 * h) - float(gx.reshape(-1)[i])) < 1e-7
 
 
