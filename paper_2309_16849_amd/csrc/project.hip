@@ -291,6 +291,146 @@ __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict
   }
 }
 
+// More channels: the four waves share a group's channels, S steps each, so that
+// every value is loaded once and at once, and join the largest magnitudes and then
+// the codes in LDS; each takes every fourth tile of the weights, whose rows it
+// reads by itself (aligned ones), with no barrier on the way.  A group is 32 * PT
+// pixels or tokens.
+template <int S, int PT, Form FORM>
+__global__ void __launch_bounds__(256, 2) project_wide_kernel(const float* __restrict__ x,
+                                                              const int8_t* __restrict__ w,
+                                                              const float* __restrict__ scales,
+                                                              const float* __restrict__ bias, ProjectGeo g,
+                                                              float* __restrict__ out) {
+  constexpr int NK = 4 * S;
+  constexpr bool TOK = FORM == Form::Tokens;
+  extern __shared__ char lds[];
+  Int4* const shared = reinterpret_cast<Int4*>(lds);                        // codes, in the order of the lanes
+  unsigned* const top = reinterpret_cast<unsigned*>(lds + PT * NK * 1024);  // rows of magnitudes, by waves
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = (g.cout + 31) / 32, t0 = blockIdx.y * g.span, t1 = min(t0 + g.span, tiles);
+  const Walk way = walk<FORM == Form::Odd>(g.groups);
+  for (long long grp = way.first; grp < way.end; grp += way.step) {
+    const long long f = TOK ? 0 : grp / g.per_frame;
+    const long long p0 = (TOK ? grp : grp - f * g.per_frame) * (32 * PT);
+    const int have = (int)min(32LL * PT, (TOK ? g.F : g.P) - p0);
+    const float* const base = TOK ? x + p0 * g.cin : x + f * g.cin * g.P + p0;
+    long long step = TOK ? 1 : g.P;  // from channel to channel
+    if constexpr (!TOK) asm volatile("" : "+s"(step));
+    float v[PT][S][16];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int c = (wv * S + s) * 32, left = g.cin - c - half * 16;
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        const int mine = min(pt * 32 + col, have - 1);  // (a lane without a pixel reads another's)
+        const unsigned at = (TOK ? mine * g.cin + half * 16 : (unsigned)(half * 16 * g.P) + mine) * 4u;
+        const float* from = base + c * step;
+        if (c + 32 <= g.cin) {
+          if constexpr (TOK) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+              load_run<4>(reinterpret_cast<const float*>(reinterpret_cast<const char*>(from + j) + at), 4, v[pt][s] + j);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, from += step) v[pt][s][j] = load_at(from, at);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j, from += step) {
+            v[pt][s][j] = 0.f;
+            if (j < left) v[pt][s][j] = load_at(from, at);
+          }
+        }
+      }
+    }
+    unsigned most[PT] = {};
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) most[pt] = max(most[pt], magnitude(v[pt][s][j]));
+      most[pt] = max(most[pt], (unsigned)__shfl_xor((int)most[pt], 32));
+      top[(wv * PT + pt) * 32 + col] = most[pt];
+    }
+    __syncthreads();
+    float ts[PT];
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) most[pt] = max(most[pt], top[(k * PT + pt) * 32 + col]);
+      const bool ok = most[pt] < kInfBits;
+      const Quant q(most[pt]);
+      ts[pt] = q.s;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        Int4 c;
+        q.codes16(v[pt][s], c);
+        if (!ok) c = Int4{0, 0, 0, 0};
+        shared[(pt * NK + wv * S + s) * 64 + lane] = c;
+      }
+    }
+    __syncthreads();
+    for (int t = t0 + wv; t < t1; t += 4) {
+      const int o0 = t * 32, left = g.cout - o0;
+      Int16 acc[PT] = {};
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        // (a row or a channel past the last is another's: not stored, times 0)
+        const Int4 a = *reinterpret_cast<const Int4*>(
+            w + (long long)min(o0 + col, g.cout - 1) * g.cin + min(ks * 32 + half * 16, g.cin - 16));
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+          const Int4 b = shared[(pt * NK + ks) * 64 + lane];
+          acc[pt] = TOK ? __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, acc[pt], 0, 0, 0)
+                        : __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc[pt], 0, 0, 0);
+        }
+      }
+      // register r: row 8 * (r / 4) + 4 * half + r % 4, column lane mod 32
+      if constexpr (TOK) {
+        const int o = min(o0 + col, g.cout - 1), part = o / g.per;
+        const float sc = scales[o], be = bias ? bias[o] : 0.f;
+        float* const to_row = out + ((long long)part * g.F + p0 + 4 * half) * g.per + (o - part * g.per);
+        const int rows = col < left ? have - 4 * half : 0;
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r / 4) + r % 4;
+            const float s = __shfl(ts[pt], row + 4 * half);
+            if (pt * 32 + row < rows) to_row[(long long)(pt * 32 + row) * g.per] = fmaf((float)acc[pt][r] * s, sc, be);
+          }
+      } else {
+        const int part = o0 / g.per;
+        const bool whole = left >= 32 && have == 32 * PT && o0 + 32 <= (part + 1) * g.per;
+        float* to_px = out + (((long long)part * g.F + f) * g.per + (o0 - part * g.per)) * step + p0;
+        const unsigned lane_at = ((unsigned)(4 * half * g.P) + col) * 4u;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r, to_px += step) {
+            const int o = min(o0 + 8 * n + 4 * half + r, g.cout - 1);
+            const float sc = scales[o], be = bias ? bias[o] : 0.f;
+            const int in = o / g.per;  // the part this channel is in
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+              const float u = fmaf((float)acc[pt][4 * n + r] * ts[pt], sc, be);
+              if (whole)
+                store_at<FORM == Form::Whole>(to_px + pt * 32, lane_at, u);
+              else if (8 * n + 4 * half + r < left && pt * 32 + col < have)
+                out[(((long long)in * g.F + f) * g.per + (o - in * g.per)) * step + p0 + pt * 32 + col] = u;
+            }
+          }
+          to_px += 4 * step;
+        }
+      }
+    }
+    __syncthreads();  // (the codes are read)
+  }
+}
+
 // A wave per output channel.
 __global__ void __launch_bounds__(64) project_pack_kernel(const float* __restrict__ w, int cin,
                                                           int8_t* __restrict__ codes, float* __restrict__ scales) {
@@ -333,20 +473,40 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   const long long want = std::max(1LL, 512 / g.groups);
   const int split = (int)(want < tiles ? want : tiles);
   g.span = (tiles + split - 1) / split;
+  g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
+  const bool whole = pp.pixels % 32 == 0 && !(reinterpret_cast<uintptr_t>(out) & 127);
+  const Form form = tokens ? Form::Tokens : whole ? Form::Whole : Form::Odd;
+  // the waves share the channels: lists of tokens above 192 of them (3,000 of 384
+  // channels to 384: 15.5 us, 28 with a wave a token's channels), frames above 512
+  // (1,024 -> 1,024 at 2x64x64: 53 us and 84; 384 -> 384 at 5x96x96 54 and 48)
+  if (g.aligned && (tokens ? nk >= 8 : nk == 32)) {
+    const int PT = nk <= 12 ? 2 : 1;
+    const long long full = nk == 8 || nk == 16 ? 768 : 512;  // by registers, 3 or 2 a CU
+    g.per_frame = ((tokens ? g.F : g.P) + 32 * PT - 1) / (32 * PT);
+    g.groups = tokens ? g.per_frame : g.per_frame * g.F;
+    const long long share = std::max(1LL, std::min((long long)(tiles + 3) / 4, full / g.groups));
+    g.span = (int)((tiles + share - 1) / share);
+    const dim3 grid((unsigned)std::min(g.groups, 1LL << 20), (unsigned)((tiles + g.span - 1) / g.span));
+    const auto kernel = nk == 8    ? project_wide_kernel<2, 2, Form::Tokens>
+                        : nk == 12 ? project_wide_kernel<3, 2, Form::Tokens>
+                        : nk == 16 ? project_wide_kernel<4, 1, Form::Tokens>
+                        : tokens   ? project_wide_kernel<8, 1, Form::Tokens>
+                        : whole    ? project_wide_kernel<8, 1, Form::Whole>
+                                   : project_wide_kernel<8, 1, Form::Odd>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), PT * (nk * 1024 + 512), s, x, codes, scales, bias, g, out);
+    return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
+  }
   // 60 KB of weights and what goes with them at once, or two buffers of 32 KB, of
   // one tile at least (33 KB with 1,024 channels)
   const int tile = nk * 1024 + 512;
   g.buffers = g.span * tile <= 60 * 1024 ? 1 : 2;
   g.hold = g.buffers == 1 ? g.span : std::max(1, 32 * 1024 / tile);
-  g.aligned = pp.cin % 16 == 0 && !(reinterpret_cast<uintptr_t>(codes) & 15);
   // as many workgroups as the chip holds at once, by registers and by LDS (64 ->
   // 192 channels at 480x854: 90 us, 94 with 5 a CU, where 4 fit; 48 -> 96 at
   // 271x483 73 and 89)
   const int by_regs = nk <= 2 ? 4 : nk == 3 ? 3 : 2, by_lds = 160 * 1024 / (g.buffers * g.hold * tile);
   const dim3 grid((unsigned)std::min(g.groups, 256LL * std::min(by_regs, by_lds)),
                   (unsigned)((tiles + g.span - 1) / g.span));
-  const bool whole = pp.pixels % 32 == 0 && !(reinterpret_cast<uintptr_t>(out) & 127);
-  const Form form = tokens ? Form::Tokens : whole ? Form::Whole : Form::Odd;
   switch (nk) {
     case 1: run_project<1>(x, codes, scales, bias, g, form, grid, out, s); break;
     case 2: run_project<2>(x, codes, scales, bias, g, form, grid, out, s); break;

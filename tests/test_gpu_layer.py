@@ -7,6 +7,7 @@ import torch
 
 from paper_2309_16849_amd import snls as B
 from tests import layer64 as R
+from workloads import small_params
 
 pytestmark = pytest.mark.gpu
 U = R.U
@@ -278,7 +279,8 @@ def test_rotate_points(dev, n, rp, interleaved):
 PROJ = [((1, 1, 1, 1, 1), 1, 1), ((1, 2, 16, 5, 7), 48, 3), ((2, 1, 64, 9, 33), 192, 3), ((1, 1, 48, 11, 12), 33, 1),
         ((1, 1, 33, 3, 41), 66, 2), ((1, 1, 192, 8, 9), 64, 1), ((1, 1, 250, 4, 8), 100, 4), ((1, 1, 256, 8, 8), 256, 2),
         ((1, 1, 300, 5, 5), 31, 1), ((1, 1, 1024, 3, 11), 40, 2), ((2, 3, 100, 1, 3), 70, 2), ((1, 1, 16, 5, 8), 2100, 3), ((1, 2, 384, 4, 32), 390, 2), ((1, 1, 20, 1, 64), 2048, 1),
-        ((1, 3, 240, 8, 16), 96, 3),
+        ((1, 3, 240, 8, 16), 96, 3), ((1, 2, 1024, 8, 8), 200, 2), ((2, 1, 992, 5, 7), 65, 1), ((100, 384), 384, 2),
+        ((33, 512), 129, 1), ((70, 1024), 64, 1), ((65, 208), 36, 3), ((1, 1, 1001, 3, 47), 300, 2), ((40, 1001), 300, 1), ((1, 2, 250, 4, 37), 700, 1),
         ((1, 1), 1, 1), ((1, 192), 576, 3), ((2, 64), 192, 3), ((33, 48), 144, 3), ((65, 20), 34, 2), ((1, 1023), 96, 1),
         ((130, 256), 300, 3), ((1, 1024), 4097, 1), ((1000, 16), 32, 1), ((3, 130), 5, 5)]
 
@@ -354,6 +356,49 @@ def test_results_do_not_depend_on_scheduling(dev):
         assert all(torch.equal(a, b) for a, b in zip(B.snls_norm_backward(gy, x, stats), want))
 
 
+def test_tensors_past_32_bits(dev):
+    """4.4 thousand million elements: the far end of every call."""
+    B_, C, H, W = 2, 68, 5700, 5700
+    if torch.cuda.mem_get_info()[0] < 130e9:
+        pytest.skip("not enough memory")
+    shp = (B_, 1, C, H, W)
+    g = torch.Generator(device=dev).manual_seed(2)
+    x, br = (torch.randn(shp, generator=g, device=dev) for _ in range(2))
+    rng = torch.tensor(RNG, dtype=torch.int64, device=dev)
+    end = (B_ - 1, 0, slice(None), H - 1, slice(W - 300, W))
+    first = ((B_ - 1) * C * H + H - 1) * W + W - 300
+    keep = torch.stack([torch.from_numpy(R.words(first + c * H * W, 300, RNG[0], RNG[1], 3) >= 2 ** 30) for c in range(C)])
+    cut = lambda t: t[end].cpu().double()[:, None, :]  # (C, 1, 300)  # noqa: E731
+    y, total, st = B.snls_norm(x, branch=br, drop=0.25, rng=rng, site=3)
+    add = torch.where(keep[:, None], cut(br) / 0.75, 0.0)
+    want = cut(x) + add
+    err = 2 * U * add.abs() + U * want.abs()
+    _within(total[end][:, None], want, err, "total")
+    _within(y[end][:, None], R.norm(want, None, None, 1e-5)[0], R.norm_bound(want, None, None, 1e-5, err)[0], "y")
+    gx, gb, gg, gbt = B.snls_norm_backward(y, total, st, drop=0.25, rng=rng, site=3, grad_x=x)
+    stats = st[:, B_ - 1, 0, H - 1, W - 300:].cpu()[:, None]
+    (wx, _, _), (ex, _, _) = R.norm_backward(cut(y), cut(total), stats, None, None)
+    _within(gx[end][:, None], wx, ex, "grad_x")
+    assert torch.equal(gb[end].cpu() != 0, keep & (gx[end].cpu() != 0))
+    for c in (0, C - 1):
+        s = y[:, :, c].double().sum().item()
+        # half a million chains of at most 300 roundings, whose errors add up like their number's root
+        assert abs(float(gbt[c]) - s) < 300 * U * float(y[:, :, c].double().abs().sum())
+    del gb, br, x, gx
+    rp = dict(B=B_, T=1, C=C, H=H, W=W, HD=2, pairs=(3, 4, 5), theta=(100.0,) * 3)
+    q, _ = B.snls_rotate(y, None, rp, q_out=total)
+    far = dict(rp, B=1, H=1, W=300, row0=H - 1, col0=W - 300)
+    got, src = q[end][None, None, :, None].cpu(), y[end][None, None, :, None].cpu()
+    _within(got, R.rotate_video(src, torch.zeros(1, 1), far), R.rotate_bound(src, far, src.shape, 6000.0), "rotation")
+    w = torch.randn(9, C, generator=g, device=dev)
+    codes, scales = B.snls_project_pack(w)
+    o = B.snls_project(y, codes, scales)
+    want, err = R.project(y[end][None, None, :, None].cpu(), codes.cpu(), scales.cpu(), None, 1)
+    _within(o[0][B_ - 1, 0, :, H - 1, W - 300:], want[0, 0, 0, :, 0], err[0, 0, 0, :, 0], "projection")
+    del o, y, total, q
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------ as a layer uses them --
 
 def test_training_layer_gradients(dev):
@@ -379,6 +424,76 @@ def test_training_layer_gradients(dev):
     for v, leaf in zip(got, leaves):
         # some 50 roundings of sums of 24 (220 for the weights) terms: far below 1e-5 of the largest
         assert float((v.cpu().double() - leaf.grad).abs().max()) < 1e-5 * float(leaf.grad.abs().max())
+
+
+def _attend64(q, k, v, inds, scale, HD):
+    """Scores of the given neighbours (single pixels), their softmax and the weighted sum, in 64 bits."""
+    B_, T, C, H, W = q.shape
+    Ch = C // HD
+    frame = inds[..., 0].long()
+    hh = torch.arange(H).view(1, 1, 1, H, 1, 1)
+    ww = torch.arange(W).view(1, 1, 1, 1, W, 1)
+    bb = torch.arange(B_).view(B_, 1, 1, 1, 1, 1)
+    hd = torch.arange(HD).view(1, HD, 1, 1, 1, 1)
+    y, x = hh + inds[..., 1].double(), ww + inds[..., 2].double()
+    ok = (frame >= 0) & (frame < T)
+
+    def read(z):
+        z = z.view(B_, T, HD, Ch, H, W).permute(0, 2, 1, 4, 5, 3)  # B HD T H W Ch
+        out = 0
+        for cy in (0, 1):
+            for cx in (0, 1):
+                Y, X = y.floor().long() + cy, x.floor().long() + cx
+                wy = (y - y.floor()) if cy else 1 - (y - y.floor())
+                wx = (x - x.floor()) if cx else 1 - (x - x.floor())
+                on = ok & (Y >= 0) & (Y < H) & (X >= 0) & (X < W)
+                tap = z[bb, hd, frame.clamp(0, T - 1), Y.clamp(0, H - 1), X.clamp(0, W - 1)]
+                out = out + tap * (wy * wx * on)[..., None]
+        return out
+
+    d = (q.view(B_, T, HD, Ch, H, W).permute(0, 2, 1, 4, 5, 3)[..., None, :] * read(k)).sum(-1)
+    logits = torch.where(ok, scale * d, torch.full_like(d, -1e30))
+    out = (torch.softmax(logits, -1)[..., None] * read(v)).sum(-2)  # B HD T H W Ch
+    return out.permute(0, 2, 1, 5, 3, 4).reshape(B_, T, C, H, W)
+
+
+def test_training_layer_with_the_attention(dev):
+    """Residual sum with dropout, norm, rotation, search, aggregation, a second dropout and norm, and back: the
+    gradients against autograd in 64 bits at the neighbours that the search chose."""
+    p = small_params(T=3, C=16, H=13, W=14, HD=2, ws=5, wt=1, ps=1, k=6)
+    rp = dict(B=1, T=3, C=16, H=13, W=14, HD=2, pairs=(1, 1, 2), theta=(100.0, 50.0, 50.0), interleaved=True)
+    shp, scale, drop = B.video_shape(p), 0.3, 0.25
+    g = _gen(77)
+    x, br, go = (torch.randn(shp, generator=g) for _ in range(3))
+    gamma, beta, gamma2 = (1 + 0.3 * torch.randn(16, generator=g) for _ in range(3))
+    flows = 1.3 * torch.randn(B.flow_shape(p), generator=g)
+    times = torch.tensor([[70, 71, 72]])
+    rng = torch.tensor(RNG, dtype=torch.int64, device=dev)
+    xd, bd, gd, td, fd = _to(dev, x, br, go, times, flows)
+    y, total, st = B.snls_norm(xd, gamma.to(dev), beta.to(dev), branch=bd, drop=drop, rng=rng, site=1)
+    q, k = B.snls_rotate(y, y, rp, times=td)
+    d, i = B.snls_search(q, k, fd, p)
+    o = B.snls_aggregate(y, d, i, p, scale)
+    y2, total2, st2 = B.snls_norm(total, gamma2.to(dev), branch=o, drop=drop, rng=rng, site=2)
+    # back
+    gt2, go_o, gg2, _ = B.snls_norm_backward(gd, total2, st2, gamma2.to(dev), drop=drop, rng=rng, site=2)
+    gq, gk, gv, _ = B.snls_backward(q, k, y, fd, d, i, go_o, p, scale)
+    a, b = B.snls_rotate(gq, gk, rp, times=td, inverse=True)
+    gx, gb, gg, gbt = B.snls_norm_backward(a + b + gv, total, st, gamma.to(dev), grad_total=gt2, drop=drop, rng=rng,
+                                           site=1)
+    leaves = [t.double().requires_grad_(True) for t in (x, br, gamma, beta, gamma2)]
+    f = 1 / (1 - R.drop32(drop))
+    tot = leaves[0] + torch.where(R.keep_mask(shp, RNG, drop, 1), leaves[1] * f, 0.0)
+    z = R.norm(tot, leaves[2], leaves[3], 1e-5)[0]
+    qq = R.rotate_video(z, times, rp)
+    out = _attend64(qq, qq, z, i.cpu(), scale, 2)
+    # (the forward pass: some 100 roundings of values of up to 5)
+    assert float((o.cpu().double() - out.detach()).abs().max()) < 100 * U * 5
+    tot2 = tot + torch.where(R.keep_mask(shp, RNG, drop, 2), out * f, 0.0)
+    (R.norm(tot2, leaves[4], None, 1e-5)[0] * go.double()).sum().backward()
+    for v, leaf in zip((gx, gb, gg, gbt, gg2), leaves):
+        # a few hundred roundings, of sums whose parts are up to some ten times the result: below 1e-4 of the largest
+        assert float((v.cpu().double() - leaf.grad).abs().max()) < 1e-4 * float(leaf.grad.abs().max())
 
 
 def _stream_state(dev, seed):
