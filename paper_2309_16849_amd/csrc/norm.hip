@@ -161,7 +161,8 @@ SNLS_DEV float group_sum(float v) {
 }
 
 // Tokens: G lanes take one, four consecutive channels a lane and N times that
-// many; one read.
+// many; one read.  16 lanes up to 128 channels: 64 would stand idle there (100,000
+// tokens of 48 channels 13.1 us with 16, 32.7 with 64; the gradients 21.6 and 50.0).
 template <int G, int N>
 __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const float* branch, Drop d,
                                                          const float* __restrict__ gamma,

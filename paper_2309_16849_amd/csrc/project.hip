@@ -470,6 +470,7 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   g.cin = pp.cin, g.cout = pp.cout, g.per = pp.cout / pp.parts;
   const int tiles = (pp.cout + 31) / 32;
   // few pixels: the output channels are shared out too, until the chip has two workgroups a CU
+  // (64x64 pixels 192 -> 576 12.9 us, 23.1 without; 2,039 tokens 12.6 and 28.0)
   const long long want = std::max(1LL, 512 / g.groups);
   const int split = (int)(want < tiles ? want : tiles);
   g.span = (tiles + split - 1) / split;

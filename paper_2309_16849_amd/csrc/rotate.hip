@@ -5,7 +5,7 @@
 #include "lanes.h"
 
 namespace snls {
-constexpr int kDeep = 4;  // rows a lane has in flight
+constexpr int kRows = 2;  // rows a lane takes, all in flight
 
 // cos and sin of pos * turns turns.  The angle is formed and reduced to the
 // nearest quarter turn in 64 bits, so that what is rounded to fp32 is at most
@@ -43,12 +43,14 @@ struct RotateGeo {
 };
 
 // 8 bytes a pair read and as many written: bandwidth bounds it.  A lane keeps its
-// four columns and walks down the rows, kDeep of them in flight, so that the
-// angles of a column pair are formed once, those of a row pair once a row, those
-// of a time pair once: 5x64x480x854 q and k, 889 us with a thread and a phase per
-// pixel, 405 so (5.2 TB/s).
+// four columns down kRows rows, all in flight, so that the angles of a column
+// pair and of a time pair are formed once, those of a row pair once a row:
+// 5x64x480x854 q and k, 889 us with a thread and a phase per pixel, 378 so
+// (5.6 TB/s).  Short workgroups keep the loads near each other: with 8 rows a lane
+// and 512 lanes the same took 405, 9x32x491x523 243 instead of 205, 720x1280 284
+// instead of 271; with one row a lane 396, 251 and 312.
 template <bool WHOLE>
-__global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float* k,
+__global__ void __launch_bounds__(256) rotate_kernel(const float* q, const float* k,
                                                      const int64_t* __restrict__ times, Rotary r, RotateGeo g,
                                                      float* q_out, float* k_out) {
   const long long HW = (long long)r.H * r.W;
@@ -68,13 +70,13 @@ __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float
         float* const o = dst + (c + at);
         const long long stride = (long long)g.cols * blockDim.x * 4;
         if (src != dst)
-          for (long long i = (blockIdx.x % g.cols * blockDim.x + threadIdx.x) * 4LL; i < n; i += kDeep * stride) {
-            float v[kDeep][4];
+          for (long long i = (blockIdx.x % g.cols * blockDim.x + threadIdx.x) * 4LL; i < n; i += kRows * stride) {
+            float v[kRows][4];
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u)
+            for (int u = 0; u < kRows; ++u)
               if (i + u * stride < n) load_run<4>(a + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u)
+            for (int u = 0; u < kRows; ++u)
               if (i + u * stride < n) put_run<WHOLE, 4>(o + i + u * stride, (int)min(4LL, n - i - u * stride), v[u]);
           }
         continue;
@@ -92,17 +94,18 @@ __global__ void __launch_bounds__(512) rotate_kernel(const float* q, const float
         for (int j = 1; j < 4; ++j) cs[j] = cs[0], sn[j] = sn[0];
       }
       const long long c1 = pr.first * HW + col, c2 = pr.second * HW + col;
-      for (int y = row0 + down; y < row1; y += kDeep * steps) {
-        float a[kDeep][4], b[kDeep][4];
+      // (turns at most once: straight code for the two rows took 421 us where this takes 378)
+      for (int y = row0 + down; y < row1; y += kRows * steps) {
+        float a[kRows][4], b[kRows][4];
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u)
+        for (int u = 0; u < kRows; ++u)
           if (y + u * steps < row1) {
             const long long at = (long long)(y + u * steps) * r.W;
             load_run<4>(src + c1 + at, cnt, a[u]);
             load_run<4>(src + c2 + at, cnt, b[u]);
           }
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u)
+        for (int u = 0; u < kRows; ++u)
           if (y + u * steps < row1) {
             const long long at = (long long)(y + u * steps) * r.W;
             if (pr.axis == 1) {
@@ -166,16 +169,14 @@ snls_status launch_rotate(const float* q, const float* k, const int64_t* times, 
   g.quads = std::min(quads, 256);
   g.cols = (quads + 255) / 256;
   // rows at once: what leaves the fewest lanes of whole waves without a run
-  // (131 runs a row: 2 rows on 320 lanes)
+  // (38 runs a row: 3 rows on 128 lanes)
   g.steps = 1;
   int threads = (g.quads + 63) / 64 * 64;
-  for (int n = 2; n * g.quads <= 512; ++n) {
+  for (int n = 2; n * g.quads <= 128; ++n) {
     const int t = (n * g.quads + 63) / 64 * 64;
     if ((double)n * g.quads / t > (double)g.steps * g.quads / threads + 0.01) g.steps = n, threads = t;
   }
-  // 4,096 workgroups, but up to 8 rows a lane
-  const double lanes = (double)g.heads * (k ? 2 : 1) * g.units * g.cols * ((r.H + g.steps - 1) / g.steps);
-  g.rows = g.steps * (int)std::min(8.0, std::max(1.0, lanes / 4096));
+  g.rows = g.steps * kRows;
   g.chunks = (r.H + g.rows - 1) / g.rows;
   const dim3 grid((unsigned)((long long)g.chunks * g.cols), (unsigned)std::min(g.units, 1024),
                   (unsigned)std::min(g.heads * (k ? 2 : 1), 1024LL));
