@@ -1,6 +1,7 @@
 // project.hip -- projections in 8-bit integers: tokens quantised on the way, a
 // scale per token and per output channel (snls_project, snls_project_pack).
 #include <algorithm>
+#include <type_traits>
 
 #include "lanes.h"
 
@@ -63,6 +64,7 @@ struct ProjectGeo {
   long long P, groups, per_frame;  // pixels of a frame; groups in all, of a frame
   long long F;                     // frames
   int cin, cout, per;              // per: output channels of a part
+  int run;                         // runs of 32 pixels a workgroup takes (project_run_kernel)
   int span, hold, buffers;         // tiles of 32 output channels a workgroup takes, that lie in LDS at a time, in one
                                    // buffer (all of them) or two
   bool aligned;                    // rows of weights at 16 bytes
@@ -96,11 +98,10 @@ SNLS_DEV Int4 weights16(const int8_t* __restrict__ w, int o, int c, const Projec
 // lanes.  NK: steps of 32 channels.  A list of tokens has rows and columns in each
 // other's place, so that stores run along the output channels.
 // 4 bytes an input and an output channel a pixel: up to some hundred channels
-// bandwidth bounds it (64 -> 192 at 480x854 86 us, 4.9 TB/s; 192 -> 576 at
-// 5x152x152 75 us, 4.7), beyond the values' second read and the weights' way into
-// LDS (512 -> 512 at 2x128x128 60 us, 284 TOP/s).  Up to KEEP steps, the values stay
-// in registers between the maximum and the codes; beyond, they are read again,
-// four steps at a time.
+// bandwidth bounds it (24 -> 48 at 9x396x392 73 us, 5.5 TB/s), beyond the values'
+// second read and the weights' way into LDS (512 -> 512 at 2x128x128 60 us, 284
+// TOP/s).  Up to KEEP steps, the values stay in registers between the maximum and
+// the codes; beyond, they are read again, four steps at a time.
 template <int NK, Form FORM>
 __global__ void __launch_bounds__(256, 2) project_kernel(const float* __restrict__ x, const int8_t* __restrict__ w,
                                                          const float* __restrict__ scales,
@@ -431,6 +432,154 @@ __global__ void __launch_bounds__(256, 2) project_wide_kernel(const float* __res
   }
 }
 
+// Frames of up to 192 channels whose tiles of 32 output channels lie in one part,
+// with aligned rows of weights: a workgroup takes a run of pixels, its waves
+// quantise 32 of them at a time into LDS and then share out the products, so that a
+// plane's pixels are stored one after the other.  Planes that do not start a cache
+// line (Odd): the lanes of a row of products exchange places with those of the
+// next 32 pixels, so that every store fills a line all the same; a run's last line
+// takes pixels of the next run, whose first 32 are quantised here too.  Bandwidth
+// bounds it: 64 -> 192 at 480x854 84 us, 5.0 TB/s, at 470x854 92; 192 -> 576 at
+// 5x152x152 72 us, 4.9 TB/s.
+template <int NK, Form FORM>
+__global__ void __launch_bounds__(256, NK <= 4 ? 4 : 3)
+    project_run_kernel(const float* __restrict__ x, const int8_t* __restrict__ w, const float* __restrict__ scales,
+                       const float* __restrict__ bias, ProjectGeo g, float* __restrict__ out) {
+  extern __shared__ char lds[];
+  constexpr bool ODD = FORM == Form::Odd;
+  const int slots = g.run + ODD;
+  Int4* const shared = reinterpret_cast<Int4*>(lds);                      // codes, in the order of the lanes
+  float* const token = reinterpret_cast<float*>(lds + slots * NK * 1024);  // scales of the pixels
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = (g.cout + 31) / 32, t0 = blockIdx.y * g.span, t1 = min(t0 + g.span, tiles);
+  const Walk way = walk<ODD>(g.groups);
+  for (long long grp = way.first; grp < way.end; grp += way.step) {
+    const long long f = grp / g.per_frame, p0 = (grp - f * g.per_frame) * (32 * g.run);
+    const int have = (int)min(32LL * slots, g.P - p0), all = (have + 31) / 32, used = min(all, g.run);
+    long long step = g.P;  // from channel to channel
+    int upper = half * 16;
+    for (int pt = wv; pt < all; pt += 4) {
+      // (else every channel's offset and guard is held in registers across the loop; so below)
+      asm volatile("" : "+s"(step), "+v"(upper));
+      const int mine = min(col, have - pt * 32 - 1);
+      const float* const base = x + f * g.cin * g.P + p0 + pt * 32;
+      const unsigned at = ((unsigned)(half * 16 * g.P) + mine) * 4u;
+      float v[NK * 16];
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        const float* from = base + ks * 32 * step;
+        const int left = g.cin - ks * 32 - upper;
+        if (ks * 32 + 32 <= g.cin) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j, from += step) v[ks * 16 + j] = load_at(from, at);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j, from += step) {
+            v[ks * 16 + j] = 0.f;
+            if (j < left) v[ks * 16 + j] = load_at(from, at);
+          }
+        }
+      }
+      unsigned most = 0;
+#pragma unroll
+      for (int j = 0; j < NK * 16; ++j) most = max(most, magnitude(v[j]));
+      most = max(most, (unsigned)__shfl_xor((int)most, 32));
+      const bool ok = most < kInfBits;
+      const Quant q(most);
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        Int4 c;
+        q.codes16(v + ks * 16, c);
+        if (!ok) c = Int4{0, 0, 0, 0};
+        shared[(pt * NK + ks) * 64 + lane] = c;
+      }
+      token[pt * 32 + col] = q.s;
+    }
+    __syncthreads();
+    const int before = ODD && p0 == 0;  // a frame's first line starts before its first pixel
+    const int lines = used + before, units = (t1 - t0) * lines, last = units * (wv + 1) / 4;
+    for (int u = units * wv / 4; u < last;) {
+      const int t = u / lines, o0 = (t0 + t) * 32, left = g.cout - o0, part = o0 / g.per;
+      const int end = min(last, (t + 1) * lines) - t * lines - before;
+      int pt = u - t * lines - before;
+      u = (t + 1) * lines;
+      Int4 a[NK];
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks)  // (a row or a channel past the last is another's: not stored, times 0)
+        a[ks] = *reinterpret_cast<const Int4*>(w + (long long)min(o0 + col, g.cout - 1) * g.cin +
+                                               min(ks * 32 + upper, g.cin - 16));
+      // register r of a product: row 8 * (r / 4) + 4 * half + r % 4, column lane mod 32
+      float sc[16], be[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int o = min(o0 + 8 * (r / 4) + (upper >> 2) + r % 4, g.cout - 1);
+        sc[r] = scales[o], be[r] = bias ? bias[o] : 0.f;
+      }
+      auto product = [&](int n, float* to) {
+        Int16 acc = {};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+          acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[ks], shared[(n * NK + ks) * 64 + lane], acc, 0, 0, 0);
+        const float ts = token[n * 32 + col];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[r] = fmaf((float)acc[r] * ts, sc[r], be[r]);
+      };
+      const long long plane = ((long long)part * g.F + f) * g.per + (o0 - part * g.per);
+      float* const to = out + plane * step + p0;
+      if constexpr (ODD) {
+        float cur[16] = {}, next[16];
+        if (pt >= 0) product(pt, cur);
+        const unsigned pixels = (unsigned)g.P, first = (unsigned)((uintptr_t)out / 4) + (unsigned)plane * pixels;
+        for (; pt < end; ++pt) {
+          product(min(pt + 1, all - 1), next);
+          asm volatile("" : "+s"(step), "+v"(upper));
+          float* to_px = to + pt * 32;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r, to_px += step) {
+              const int row = 8 * n + (upper >> 2) + r;
+              const int skip = -(int)(first + row * pixels) & 31;  // pixels before the line starts
+              const float give = col < skip ? next[4 * n + r] : cur[4 * n + r];
+              const float v = __int_as_float(__builtin_amdgcn_ds_bpermute(
+                  (((col + skip) & 31) + 2 * upper) * 4, __float_as_int(give)));
+              const int px = pt * 32 + col + skip;
+              const unsigned lane_at = ((upper >> 2) * pixels + col + skip) * 4u;
+              if (row < left && px >= 0 && px < have) store_at<true>(to_px, lane_at, v);
+              cur[4 * n + r] = next[4 * n + r];
+            }
+            to_px += 4 * step;
+          }
+        }
+      } else {
+        auto lines_of = [&](auto count) {
+          constexpr int L = decltype(count)::value;
+          float v[L][16];
+#pragma unroll
+          for (int b = 0; b < L; ++b) product(pt + b, v[b]);
+          asm volatile("" : "+s"(step), "+v"(upper));
+          float* to_px = to + pt * 32;
+          const unsigned lane_at = ((upper >> 2) * (unsigned)g.P + col) * 4u;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r, to_px += step)
+              if (left >= 32 || 8 * n + (upper >> 2) + r < left)
+#pragma unroll
+                for (int b = 0; b < L; ++b) store_at<true>(to_px + b * 32, lane_at, v[b][4 * n + r]);
+            to_px += 4 * step;
+          }
+          pt += L;
+        };
+        while (pt + 2 <= end) lines_of(std::integral_constant<int, 2>());
+        if (pt < end) lines_of(std::integral_constant<int, 1>());
+      }
+    }
+    __syncthreads();  // (the codes are read)
+  }
+}
+
 // A wave per output channel.
 __global__ void __launch_bounds__(64) project_pack_kernel(const float* __restrict__ w, int cin,
                                                           int8_t* __restrict__ codes, float* __restrict__ scales) {
@@ -497,14 +646,41 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
     hipLaunchKernelGGL(kernel, grid, dim3(256), PT * (nk * 1024 + 512), s, x, codes, scales, bias, g, out);
     return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
   }
+  // Runs of pixels, against 128 pixels a workgroup: planes that start a line, 64 ->
+  // 192 at 480x854 84 us and 90, 192 -> 576 at 5x152x152 72 and 77, but 16 -> 384 at
+  // 304x622 63 and 61; planes that do not, 470x854 92 and 123, 32 -> 64 at 9x397x391
+  // 117 and 173, but 16 -> 384 at 305x620 74 and 66, and nothing won or less where
+  // the 256 MB of cache hold the output: 305x622 44 and 45, 271x483 32 and 25.
+  if (!tokens && nk <= 6 && g.aligned && (pp.parts == 1 || g.per % 32 == 0) && pp.cout <= 8 * pp.cin &&
+      (whole || g.F * g.P * g.cout > 1LL << 26)) {
+    // as many workgroups as the chip holds at once, by registers, take the frames in
+    // as few turns as LDS allows, of the same length
+    const int by_regs = nk <= 4 ? 4 : 3, slot = nk * 1024 + 128, odd = form == Form::Odd;
+    const long long all = (g.P + 31) / 32 * g.F, held = 256LL * by_regs;
+    const int most = 160 * 1024 / by_regs / slot - odd;
+    const long long turns = (all + held * most - 1) / (held * most);
+    g.run = (int)((all + held * turns - 1) / (held * turns));
+    g.per_frame = (g.P + 32 * g.run - 1) / (32 * g.run), g.groups = g.per_frame * g.F;
+    const long long share = std::max(1LL, std::min((long long)tiles, 512 / g.groups));
+    g.span = (int)((tiles + share - 1) / share);
+    const dim3 grid((unsigned)std::min(g.groups, held), (unsigned)((tiles + g.span - 1) / g.span));
+#define SNLS_RUN(K) (odd ? project_run_kernel<K, Form::Odd> : project_run_kernel<K, Form::Whole>)
+    const auto kernel = nk == 1   ? SNLS_RUN(1)
+                        : nk == 2 ? SNLS_RUN(2)
+                        : nk == 3 ? SNLS_RUN(3)
+                        : nk == 4 ? SNLS_RUN(4)
+                                  : SNLS_RUN(6);
+#undef SNLS_RUN
+    hipLaunchKernelGGL(kernel, grid, dim3(256), (g.run + odd) * slot, s, x, codes, scales, bias, g, out);
+    return hipGetLastError() == hipSuccess ? SNLS_OK : SNLS_ERR_HIP;
+  }
   // 60 KB of weights and what goes with them at once, or two buffers of 32 KB, of
   // one tile at least (33 KB with 1,024 channels)
   const int tile = nk * 1024 + 512;
   g.buffers = g.span * tile <= 60 * 1024 ? 1 : 2;
   g.hold = g.buffers == 1 ? g.span : std::max(1, 32 * 1024 / tile);
-  // as many workgroups as the chip holds at once, by registers and by LDS (64 ->
-  // 192 channels at 480x854: 90 us, 94 with 5 a CU, where 4 fit; 48 -> 96 at
-  // 271x483 73 and 89)
+  // as many workgroups as the chip holds at once, by registers and by LDS (48 -> 96
+  // channels at 4x271x483 73 us, 89 with 5 a CU, where 4 fit)
   const int by_regs = nk <= 2 ? 4 : nk == 3 ? 3 : 2, by_lds = 160 * 1024 / (g.buffers * g.hold * tile);
   const dim3 grid((unsigned)std::min(g.groups, 256LL * std::min(by_regs, by_lds)),
                   (unsigned)((tiles + g.span - 1) / g.span));

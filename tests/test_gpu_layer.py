@@ -302,6 +302,34 @@ def test_project(dev, case):
         _within(out, want, err, "project")
 
 
+# outputs that no cache holds, of planes that share cache lines: (shape of x, cout, parts, floats before the output)
+BIG = [((1, 1, 32, 470, 855), 200, 1, 0), ((1, 3, 64, 271, 483), 192, 3, 0), ((2, 1, 192, 152, 153), 1536, 2, 1),
+       ((1, 1, 16, 740, 740), 128, 1, 5), ((1, 1, 96, 480, 512), 288, 3, 3), ((8000, 64, 3, 11), 256, 2, 0),
+       ((4400, 128, 1, 31), 512, 4, 31), ((1, 1, 48, 480, 512), 300, 1, 32)]
+
+
+@pytest.mark.parametrize("case", BIG, ids=str)
+def test_project_past_the_caches(dev, case):
+    """The same values as the pixels give as a list of tokens, and nothing beside them."""
+    shape, cout, parts, before = case
+    cin = shape[-3]
+    g = torch.Generator(device=dev).manual_seed(cout)
+    x = torch.randn(shape, generator=g, device=dev)
+    x.view(-1, cin, shape[-2] * shape[-1])[0, 3, 17] = float("nan")
+    codes, scales = B.snls_project_pack(torch.randn(cout, cin, generator=g, device=dev))
+    bias = torch.randn(cout, generator=g, device=dev)
+    n = cout * (x.numel() // cin)
+    room = torch.full((n + before + 64,), -7.5, device=dev)
+    out = room[before:before + n].view((parts,) + shape[:-3] + (cout // parts,) + shape[-2:])
+    B.snls_project(x, codes, scales, bias=bias, parts=parts, out=out)
+    tokens = x.view(-1, cin, shape[-2] * shape[-1]).transpose(1, 2).reshape(-1, cin).contiguous()
+    want = B.snls_project(tokens, codes, scales, bias=bias, parts=parts)
+    want = want.view(parts, -1, shape[-2] * shape[-1], cout // parts).transpose(2, 3)
+    got = out.view(want.shape)
+    assert bool(((got == want) | (got.isnan() & want.isnan())).all()) and int(got.isnan().sum()) == cout
+    assert bool((room[:before] == -7.5).all()) and bool((room[before + n:] == -7.5).all())
+
+
 def test_project_special_tokens(dev):
     """Halves next to their ties, tokens of zeros, of tiny and large values, infinities and NaN."""
     g = _gen(4)
