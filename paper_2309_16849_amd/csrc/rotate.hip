@@ -8,8 +8,10 @@ namespace snls {
 constexpr int kRows = 2;  // rows a lane takes, all in flight
 
 // cos and sin of pos * turns turns.  The angle is formed and reduced to the
-// nearest quarter turn in 64 bits, so that what is rounded to fp32 is at most
-// an eighth of a turn: 2.3e-8 radians, however far the position.
+// nearest quarter turn in 64 bits: turns is off by at most 1.25 * 2^-53 of it, pos
+// (past 2^53) and the product by 2^-53 each, in all less than 2^-51 of the angle,
+// and the reduction is exact.  What is rounded to fp32 is at most an eighth of a
+// turn: 2.3e-8 radians more.
 SNLS_DEV void phase(double pos, double turns, float* c, float* s) {
   const double r = pos * turns * 4.0;
   const double q = rint(r);

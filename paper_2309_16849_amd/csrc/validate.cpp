@@ -142,10 +142,14 @@ snls_status check_rotate(const snls_rotate_params* rp, bool inverse, Rotary* out
   int at = 0;
   for (int a = 0; a < 3; ++a) {
     out->pairs[a] = rp->pairs[a];
-    for (int i = 0; i < rp->pairs[a]; ++i) {
-      const double f = pow((double)rp->theta[a], -(double)i / rp->pairs[a]) / 6.283185307179586476925;
-      out->turns[at++] = inverse ? -f : f;
-    }
+    // theta^(-i/n) / 2 pi as a product of i equal factors, in the 64 bits of a long
+    // double: a factor is off by at most (ln(theta)/n + 2) 2^-64, a product by 2^-64
+    // more, all of them by 2^-55, and the turns, rounded to 53 bits, by 1.25 * 2^-53
+    // (an exponent i/n rounded to 53 bits costs ln(theta) i/n 2^-53: 10 * 2^-51 for
+    // the largest theta).
+    long double f = 1.0L / 6.28318530717958647692528676655900577L;
+    const long double factor = rp->pairs[a] > 0 ? powl((long double)rp->theta[a], -1.0L / rp->pairs[a]) : 1.0L;
+    for (int i = 0; i < rp->pairs[a]; ++i, f *= factor) out->turns[at++] = (double)(inverse ? -f : f);
   }
   return SNLS_OK;
 }
