@@ -537,8 +537,8 @@ snls_status snls_norm(const float* x, const float* branch, const uint64_t* rng, 
  *               0), or both NULL
  *   workspace   device scratch of at least snls_norm_workspace_size(np) bytes,
  *               256-byte aligned; not needed without grad_gamma
- * No sum over pixels chains more than a few hundred additions in fp32 before 64
- * bits take over, and the result does not depend on scheduling.
+ * The sums over frames and pixels are in 64 bits, rounded once; the result does
+ * not depend on scheduling.
  * Errors: as snls_norm; SNLS_ERR_WORKSPACE. */
 snls_status snls_norm_backward(const float* grad_y, const float* grad_total, const float* total, const float* stats,
                                const float* gamma, const uint64_t* rng, const snls_norm_params* np, float* grad_x,

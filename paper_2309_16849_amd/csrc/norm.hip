@@ -119,28 +119,37 @@ __global__ void __launch_bounds__(1024) norm_tile_kernel(const float* x, const f
   }
 }
 
+// v of lane ^ M, M below 16.
+template <int M>
+SNLS_DEV double partner_value(double v, int lane) {
+  return __longlong_as_double((long long)grp_xor64<M>((unsigned long long)__double_as_longlong(v), lane & 15));
+}
+
 // One step of the sum of a list over the lanes: a lane with bit M set goes on
 // with b, the others with a, each plus what its partner (lane ^ M) has of it.
 template <int M>
-SNLS_DEV float halve(float a, float b, int lane) {
+SNLS_DEV double halve(double a, double b, int lane) {
   if constexpr (M >= 16) {
     // the rows of a whose lanes have the bit change places with those of b whose
     // lanes have not
-    const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
-    const auto r = M == 32 ? __builtin_amdgcn_permlane32_swap(ua, ub, false, false)
-                           : __builtin_amdgcn_permlane16_swap(ua, ub, false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto swap = [](unsigned ua, unsigned ub) {
+      return M == 32 ? __builtin_amdgcn_permlane32_swap(ua, ub, false, false)
+                     : __builtin_amdgcn_permlane16_swap(ua, ub, false, false);
+    };
+    const auto lo = swap((unsigned)__double2loint(a), (unsigned)__double2loint(b));
+    const auto hi = swap((unsigned)__double2hiint(a), (unsigned)__double2hiint(b));
+    return __hiloint2double((int)hi[0], (int)lo[0]) + __hiloint2double((int)hi[1], (int)lo[1]);
   } else {
     const bool up = lane & M;
-    const float give = up ? a : b, keep = up ? b : a;
-    return keep + __uint_as_float(grp_xor<M>(__float_as_uint(give), lane & 15));
+    const double give = up ? a : b, keep = up ? b : a;
+    return keep + partner_value<M>(give, lane);
   }
 }
 
 // Sums over 2 M lanes of LEN values each (a power of two up to 2 M): lane l of
 // them returns that of value l / (2 M / LEN).
-template <int LEN, int M = 32>
-SNLS_DEV float list_sum(float* v, int lane) {
+template <int LEN, int M>
+SNLS_DEV double list_sum(double* v, int lane) {
   if constexpr (M == 0) {
     return v[0];
   } else if constexpr (LEN > 1) {
@@ -148,7 +157,7 @@ SNLS_DEV float list_sum(float* v, int lane) {
     for (int i = 0; i < LEN / 2; ++i) v[i] = halve<M>(v[i], v[i + LEN / 2], lane);
     return list_sum<LEN / 2, M / 2>(v, lane);
   } else {
-    v[0] += __uint_as_float(grp_xor<M>(__float_as_uint(v[0]), lane & 15));
+    v[0] += partner_value<M>(v[0], lane);
     return list_sum<1, M / 2>(v, lane);
   }
 }
@@ -264,9 +273,12 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
 // Gradients of frames: tiles, waves and channels as in the forward pass.  Both
 // the scaled gradients and the normalised values stay in registers, one join of
 // two sums a tile.  A workgroup walks every gridDim.x-th tile, at most 64 of them,
-// and a lane adds up its pixels' 2 R terms of the weights' gradients; at the end
-// a wave's lanes are left with one sum each, and a workgroup writes one row of
-// partial sums.
+// and a lane adds up the terms of the weights' gradients of its and its partner's
+// pixels (lane ^ 32), the lower lanes gamma's, the upper lanes beta's; at the end a
+// wave's lanes are left with one sum each, and a workgroup writes one row of
+// partial sums.  Products and sums of these terms are in 64 bits from the start:
+// the vector units have the time (16x64x256x256 163.4 us, 162.5 with sums in 32;
+// 4x48x271x483 66.2 and 66.1).
 template <int R, bool WHOLE>
 __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_y, const float* grad_total,
                                                               const float* __restrict__ total,
@@ -280,7 +292,7 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Philox gen(d);
   const int c0 = wv * g.n, n = min(g.n, g.C - c0);
-  float over[2 * R] = {};  // this lane's sums over the tiles
+  double over[R] = {};  // this lane's sums over the tiles
   int turn = 0;
   const Walk way = walk<!WHOLE>(g.tiles);
   for (long long tile = way.first; tile < way.end; tile += way.step) {
@@ -300,15 +312,17 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
     for (int c = 0; c < R; ++c)
       if (c < n) {
         const float ga = gamma ? gamma[c0 + c] : 1.f;
+        double tg = 0.0, tb = 0.0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           xh[c][j] = (xh[c][j] - mean[j]) * rstd[j];
-          over[c] = fmaf(gy[c][j], xh[c][j], over[c]);
-          over[R + c] += gy[c][j];
+          tg = fma((double)gy[c][j], (double)xh[c][j], tg);
+          tb += (double)gy[c][j];
           gy[c][j] *= ga;
           sum[0][j] += gy[c][j];
           sum[1][j] = fmaf(gy[c][j], xh[c][j], sum[1][j]);
         }
+        over[c] += halve<32>(tg, tb, lane);
       }
     if (waves > 1) {
       float* const rows = part + turn * 2 * waves * V * 64;
@@ -353,16 +367,18 @@ __global__ void __launch_bounds__(1024) norm_grad_tile_kernel(const float* grad_
       }
   }
   if (!sums) return;
-  const double acc = (double)list_sum<2 * R>(over, lane);  // this lane's of the 2 R sums
-  const int which = lane / (32 / R), c = which % R;
-  if (lane % (32 / R) == 0 && c < n) sums[((long long)blockIdx.x * 2 + which / R) * g.C + c0 + c] = acc;
+  const double acc = list_sum<R, 16>(over, lane);  // this lane's of the R sums of its half
+  const int c = (lane & 31) / (32 / R);
+  if (lane % (32 / R) == 0 && c < n) sums[((long long)blockIdx.x * 2 + lane / 32) * g.C + c0 + c] = acc;
 }
 
 // Gradients of frames of many channels: one pixel a lane, L = 64 pixels a tile up
 // to 256 channels, 32 and two channels side by side in a wave up to 512, so that
 // 64 registers hold a wave's tile and two workgroups of 8 waves fit a CU, one
 // loading while the other stores (5x256x128x128 without dropout 59 us, with one
-// workgroup of 16 waves 75; 5x384x96x96 60 and 77).
+// workgroup of 16 waves 75; 5x384x96x96 60 and 77).  The terms of the weights'
+// gradients are multiplied and summed over the pixels in 64 bits; those figures
+// were taken with 32, against which 64 cost 2 us (59.8 -> 62.0, 62.0 -> 64.2).
 template <int L, int R, bool WHOLE>
 __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* grad_y, const float* grad_total,
                                                                 const float* __restrict__ total,
@@ -406,20 +422,19 @@ __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* gra
 #pragma unroll
     for (int k0 = 0; k0 < R; k0 += 8)
       if (k0 < n) {
-        float over[16] = {};
+        double over[8] = {};  // the lower half's lanes gamma's terms, the upper half's beta's
 #pragma unroll
         for (int k = k0; k < k0 + 8; ++k)
           if (k < n) {
             const bool ok = in && k < own;
             gy[k] = ok ? gy[k] : 0.f;
             xh[k] = ok ? (xh[k] - mean) * rstd : 0.f;
-            over[k - k0] = gy[k] * xh[k];
-            over[8 + k - k0] = gy[k];
+            if (sums) over[k - k0] = halve<L / 2>((double)gy[k] * (double)xh[k], (double)gy[k], lane);
             gy[k] *= scale[c0 + k * SIDE + side];
             s0 += gy[k];
             s1 = fmaf(gy[k], xh[k], s1);
           }
-        if (sums) acc[k0 / 8] += (double)list_sum<16, L / 2>(over, lane);
+        if (sums) acc[k0 / 8] += list_sum<8, L / 4>(over, lane);
       }
     if (L == 32) s0 += __shfl_xor(s0, 32), s1 += __shfl_xor(s1, 32);
     float* const rows = part + turn * 2 * waves * 64;
@@ -457,17 +472,18 @@ __global__ void __launch_bounds__(512, 4) norm_grad_wide_kernel(const float* gra
       }
   }
   if (!sums) return;
-  const int which = l / (L / 16);  // of the 16 sums of 8 steps
+  const int which = l / (L / 2), step = l % (L / 2) / (L / 16);  // of the 2 sums of 8 steps
 #pragma unroll
   for (int k0 = 0; k0 < R; k0 += 8) {
-    const int k = k0 + which % 8;
+    const int k = k0 + step;
     if (l % (L / 16) == 0 && k < own)
-      sums[((long long)blockIdx.x * 2 + which / 8) * g.C + c0 + k * SIDE + side] = acc[k0 / 8];
+      sums[((long long)blockIdx.x * 2 + which) * g.C + c0 + k * SIDE + side] = acc[k0 / 8];
   }
 }
 
 // Gradients of tokens: G lanes a token, as in the forward pass; a workgroup
-// walks rows and keeps its channels' sums, joined over its groups at the end.
+// walks rows and keeps its channels' sums in 64 bits, joined over its groups at the
+// end.
 template <int G, int N>
 __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_y, const float* grad_total,
                                                               const float* __restrict__ total,
@@ -475,10 +491,11 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
                                                               const float* __restrict__ gamma, Drop d, NormGeo g,
                                                               float* grad_x, float* grad_branch,
                                                               double* __restrict__ sums) {
-  __shared__ float rows[2][256 / G][G * N * 4];
+  __shared__ double rows[256 / G][G * N * 4];
   const int l = threadIdx.x & (G - 1), group = threadIdx.x / G;
   const Philox gen(d);
-  float acc[2][N][4] = {}, ga[N][4];
+  double acc[2][N][4] = {};
+  float ga[N][4];
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const int c = (k * G + l) * 4, cnt = max(0, min(4, g.C - c));
@@ -502,8 +519,8 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
       for (int j = 0; j < 4; ++j) {
         const bool in = (k * G + l) * 4 + j < g.C;
         xh[k][j] = in ? (xh[k][j] - mean) * rstd : 0.f;
-        acc[0][k][j] = fmaf(gy[k][j], xh[k][j], acc[0][k][j]);
-        acc[1][k][j] += gy[k][j];
+        acc[0][k][j] = fma((double)gy[k][j], (double)xh[k][j], acc[0][k][j]);
+        acc[1][k][j] += (double)gy[k][j];
         gy[k][j] *= ga[k][j];
         s0 += gy[k][j];
         s1 = fmaf(gy[k][j], xh[k][j], s1);
@@ -534,18 +551,18 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
   }
   if (!sums) return;
 #pragma unroll
-  for (int k = 0; k < N; ++k)
+  for (int which = 0; which < 2; ++which) {
+    if (which) __syncthreads();  // (the first sums are read)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      rows[0][group][(k * G + l) * 4 + j] = acc[0][k][j];
-      rows[1][group][(k * G + l) * 4 + j] = acc[1][k][j];
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rows[group][(k * G + l) * 4 + j] = acc[which][k][j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < g.C; c += 256) {
+      double s = 0.0;
+      for (int k = 0; k < 256 / G; ++k) s += rows[k][c];
+      sums[((long long)blockIdx.x * 2 + which) * g.C + c] = s;
     }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 2 * g.C; i += 256) {
-    const int which = i >= g.C, c = i - which * g.C;
-    double s = 0.0;
-    for (int k = 0; k < 256 / G; ++k) s += (double)rows[which][k][c];
-    sums[(long long)blockIdx.x * 2 * g.C + i] = s;
   }
 }
 
@@ -594,7 +611,7 @@ __global__ void __launch_bounds__(256) norm_weights_kernel(const float* __restri
   for (long long i = blockIdx.y * 256LL + threadIdx.x; i < px; i += gridDim.y * 256LL) {
     const long long f = i / P, e = (f * C + c) * P + (i - f * P);
     const float g = grad_y[e];
-    sg += (double)(g * ((total[e] - stats[i]) * stats[px + i]));
+    sg += (double)g * (double)((total[e] - stats[i]) * stats[px + i]);
     sb += (double)g;
   }
   sums[0][threadIdx.x] = sg, sums[1][threadIdx.x] = sb;
