@@ -503,8 +503,9 @@ typedef struct {
  * + eps) over the C channels of a pixel of total (of x without branch), y =
  * (total - mean) * rstd * gamma + beta (NaN where eps is 0 and a pixel's channels
  * are all alike).  The variance is the mean of the squared
- * differences from the mean.  Sums of C values and of their squares stay in
- * fp32: |x| * C and (x - mean)^2 * C have to stay in its range.
+ * differences from the mean.  No lane adds up more than 32 channels in fp32 (where
+ * one adds up more it does in 64 bits): |x| * C and (x - mean)^2 * C have to stay in
+ * fp32's range.
  *   x       device, (frames, C, pixels)
  *   branch  device, as x, or NULL (then total is not written; drop must be 0)
  *   rng     device, 2 x uint64 (seed, step); may be NULL when drop == 0

@@ -229,7 +229,10 @@ __global__ void __launch_bounds__(256) norm_token_kernel(const float* x, const f
 }
 
 // More channels than registers hold: a thread per pixel (or token) that reads
-// them again.
+// them again.  One lane adds up all of them, up to 65,535, so in 64 bits
+// (4x600x96x96 558 us, 546 with sums in 32).  Not tuned: a thread's loads wait for
+// each other, and for tokens the lanes' loads are C floats apart (64 tokens of 4,096
+// channels 1.6 ms, 4,000 2.4 ms; the gradients 1.8 and 3.4 ms).
 __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* branch, Drop d,
                                                    const float* __restrict__ gamma, const float* __restrict__ beta,
                                                    long long frames, int C, long long P, float eps, float* total,
@@ -238,7 +241,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
   const long long px = frames * P;
   for (long long i = blockIdx.x * 256LL + threadIdx.x; i < px; i += gridDim.x * 256LL) {
     const long long f = i / P, at = f * C * P + (i - f * P);
-    float sum = 0.f;
+    double sum = 0.0;
     for (int c = 0; c < C; ++c) {
       const long long e = at + c * P;
       float v = x[e];
@@ -252,16 +255,16 @@ __global__ void __launch_bounds__(256) norm_kernel(const float* x, const float* 
         v += b;
         total[e] = v;
       }
-      sum += v;
+      sum += (double)v;
     }
     const float* from = branch ? total : x;
-    const float mean = sum / C;
-    float sq = 0.f;
+    const float mean = (float)(sum / C);
+    double sq = 0.0;
     for (int c = 0; c < C; ++c) {
-      const float t = from[at + c * P] - mean;
-      sq = fmaf(t, t, sq);
+      const double t = (double)(from[at + c * P] - mean);
+      sq = fma(t, t, sq);
     }
-    const float rstd = 1.f / sqrtf(sq / C + eps);
+    const float rstd = 1.f / sqrtf((float)(sq / C) + eps);
     for (int c = 0; c < C; ++c) {
       const float t = (from[at + c * P] - mean) * rstd;
       y[at + c * P] = fmaf(t, gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
@@ -566,7 +569,8 @@ __global__ void __launch_bounds__(256) norm_grad_token_kernel(const float* grad_
   }
 }
 
-// More channels than registers hold: a thread per pixel, gradients of the input and the branch.
+// More channels than registers hold: a thread per pixel, gradients of the input and
+// the branch; sums over the channels in 64 bits, as above.
 __global__ void __launch_bounds__(256) norm_grad_kernel(const float* grad_y, const float* grad_total,
                                                         const float* __restrict__ total,
                                                         const float* __restrict__ stats,
@@ -577,13 +581,13 @@ __global__ void __launch_bounds__(256) norm_grad_kernel(const float* grad_y, con
   for (long long i = blockIdx.x * 256LL + threadIdx.x; i < px; i += gridDim.x * 256LL) {
     const long long f = i / P, at = f * C * P + (i - f * P);
     const float mean = stats[i], rstd = stats[px + i];
-    float sg = 0.f, sgx = 0.f;
+    double over = 0.0, over_x = 0.0;
     for (int c = 0; c < C; ++c) {
       const float g = grad_y[at + c * P] * (gamma ? gamma[c] : 1.f), xh = (total[at + c * P] - mean) * rstd;
-      sg += g;
-      sgx = fmaf(g, xh, sgx);
+      over += (double)g;
+      over_x = fma((double)g, (double)xh, over_x);
     }
-    sg /= C, sgx /= C;
+    const float sg = (float)(over / C), sgx = (float)(over_x / C);
     for (int c = 0; c < C; ++c) {
       const long long e = at + c * P;
       const float g = grad_y[e] * (gamma ? gamma[c] : 1.f), xh = (total[e] - mean) * rstd;
