@@ -676,6 +676,21 @@ def _features(t, name):
     return frames, s[-3], s[-2] * s[-1], tuple(s[:-3]) + tuple(s[-2:])
 
 
+def dropout_site(site: int) -> int:
+    """A dropout's number; a C field would take it modulo 2^32, and two sites share a mask."""
+    site = int(site)
+    if not 0 <= site < 1 << 32:
+        raise ValueError("site must be a whole number of 32 bits, got %d" % site)
+    return site
+
+
+_MOST = (1 << 31) - 1  # channels beyond stay more than the library takes
+
+
+def norm_params(C: int, frames: int, pixels: int, eps: float, drop: float, site: int) -> SnlsNormParams:
+    return SnlsNormParams(_NORM_SIZE, min(C, _MOST), frames, pixels, float(eps), float(drop), dropout_site(site))
+
+
 def _per_channel(C, **tensors):
     for n, t in tensors.items():
         if t is not None:
@@ -707,7 +722,7 @@ def snls_norm(x, gamma=None, beta=None, eps: float = 1e-5, branch=None, drop: fl
     y = _like(x, y, "y", stream)
     stats = _dev(stats, "stats", (2,) + px) if stats is not None else _new((2,) + px, x, stream)
     _here(x, gamma, beta, branch, rng, y, total, stats)
-    prm = SnlsNormParams(_NORM_SIZE, C, frames, pixels or 1, float(eps), float(drop), int(site))
+    prm = norm_params(C, frames, pixels or 1, eps, drop, site)
     if pixels:
         _check(lib.snls_norm(_ptr(x), _ptr(branch), _rng(rng, drop), _ptr(gamma), _ptr(beta), ctypes.byref(prm),
                              _ptr(total), _ptr(y), _ptr(stats), _stream(stream)), "snls_norm")
@@ -728,7 +743,7 @@ def snls_norm_backward(grad_y, total, stats, gamma=None, grad_total=None, drop: 
     grad_x = _like(total, grad_x, "grad_x", stream)
     if grad_branch is not None or drop > 0:
         grad_branch = _like(total, grad_branch, "grad_branch", stream)
-    prm = SnlsNormParams(_NORM_SIZE, C, frames if pixels else 0, pixels or 1, 0.0, float(drop), int(site))
+    prm = norm_params(C, frames if pixels else 0, pixels or 1, 0.0, drop, site)
     gg, gb, room = None, None, (None, 0)
     if weights:
         gg, gb = _new((C,), total, stream), _new((C,), total, stream)
@@ -754,8 +769,8 @@ def snls_dropout(x, rng, drop: float, site: int = 0, residual=None, out=None, st
         _dev(residual, "residual", x.shape)
     out = _like(x, out, "out", stream)
     _here(x, residual, rng, out)
-    _check(lib.snls_dropout(_ptr(x), _ptr(residual), _rng(rng, drop), x.numel(), float(drop), int(site), _ptr(out),
-                            _stream(stream)), "snls_dropout")
+    _check(lib.snls_dropout(_ptr(x), _ptr(residual), _rng(rng, drop), x.numel(), float(drop), dropout_site(site),
+                            _ptr(out), _stream(stream)), "snls_dropout")
     return out
 
 
@@ -767,9 +782,11 @@ _ROTATE_SIZE, _Int3, _Float3 = ctypes.sizeof(SnlsRotateParams), ctypes.c_int32 *
 def rotate_from_dict(rp: dict) -> SnlsRotateParams:
     if len(rp["pairs"]) != 3 or len(rp["theta"]) != 3:
         raise ValueError("pairs and theta have three entries: time, row, column")
-    return SnlsRotateParams(_ROTATE_SIZE, int(rp["B"]), int(rp["T"]), int(rp["C"]), int(rp["H"]), int(rp["W"]),
-                            int(rp["HD"]), _Int3(*rp["pairs"]), _Float3(*rp["theta"]),
-                            int(rp.get("interleaved", 0)), int(rp.get("row0", 0)), int(rp.get("col0", 0)))
+    n = (int(rp["B"]), int(rp["T"]), int(rp["C"]), int(rp["H"]), int(rp["W"]), int(rp["HD"]), *rp["pairs"],
+         int(rp.get("interleaved", 0)), int(rp.get("row0", 0)), int(rp.get("col0", 0)))
+    if min(n) < -1 << 31 or max(n) >= 1 << 31:
+        raise ValueError("sizes, pairs and origins must be whole numbers of 32 bits")
+    return SnlsRotateParams(_ROTATE_SIZE, *n[:6], _Int3(*n[6:9]), _Float3(*rp["theta"]), *n[9:])
 
 
 def snls_rotate(q, k, rp: dict, times=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
@@ -815,6 +832,10 @@ def snls_rotate_points(q, points, rp: dict, times=None, inverse: bool = False, o
 _PROJECT_SIZE = ctypes.sizeof(SnlsProjectParams)
 
 
+def project_params(cin: int, cout: int, parts: int, frames: int, pixels: int) -> SnlsProjectParams:
+    return SnlsProjectParams(_PROJECT_SIZE, min(cin, _MOST), min(cout, _MOST), parts, frames, pixels)
+
+
 def snls_project_pack(w, codes=None, scales=None, stream=None):
     """Weights (cout, cin) as int8 codes and a scale per output channel: (codes, scales)."""
     lib = load_library()
@@ -829,7 +850,7 @@ def snls_project_pack(w, codes=None, scales=None, stream=None):
     _dev_as(codes, "codes", w.shape, (torch.int8,))
     scales = _dev(scales, "scales", (cout,)) if scales is not None else _new((cout,), w, stream)
     _here(w, codes, scales)
-    prm = SnlsProjectParams(_PROJECT_SIZE, cin, cout, 1, 0, 1)
+    prm = project_params(cin, cout, 1, 0, 1)
     _check(lib.snls_project_pack(_ptr(w), ctypes.byref(prm), _ptr(codes), _ptr(scales), _stream(stream)),
            "snls_project_pack")
     return codes, scales
@@ -851,7 +872,7 @@ def snls_project(x, codes, scales, bias=None, parts: int = 1, out=None, stream=N
     shp = (parts,) + tuple(x.shape[:-3] if x.dim() > 2 else x.shape[:1]) + tail
     out = _dev(out, "out", shp) if out is not None else _new(shp, x, stream)
     _here(x, codes, scales, bias, out)
-    prm = SnlsProjectParams(_PROJECT_SIZE, cin, cout, parts, frames, pixels or 1)
+    prm = project_params(cin, cout, parts, frames, pixels or 1)
     if pixels:
         _check(lib.snls_project(_ptr(x), _ptr(codes), _ptr(scales), _ptr(bias), ctypes.byref(prm), _ptr(out),
                                 _stream(stream)), "snls_project")
