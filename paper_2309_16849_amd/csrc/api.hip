@@ -4,7 +4,7 @@
 // state is kept between calls.
 #include <cmath>
 
-#include "snls_internal.h"
+#include "layer.h"
 
 using namespace snls;
 

@@ -2,7 +2,7 @@
 // (device side), at any 4-byte address.
 #pragma once
 
-#include "snls_internal.h"
+#include "layer.h"
 
 #ifdef __HIPCC__
 

@@ -8,7 +8,7 @@
 // they straddle a border.
 #pragma once
 
-#include "snls_internal.h"
+#include "layer.h"
 
 #ifdef __HIPCC__
 

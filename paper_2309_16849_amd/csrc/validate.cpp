@@ -4,7 +4,7 @@
 #include <limits.h>
 #include <math.h>
 
-#include "snls_internal.h"
+#include "layer.h"
 
 namespace snls {
 
