@@ -26,6 +26,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -776,17 +777,18 @@ def snls_dropout(x, rng, drop: float, site: int = 0, residual=None, out=None, st
 
 # ------------------------------------------------------------- rotary positions --
 
-_ROTATE_SIZE, _Int3, _Float3 = ctypes.sizeof(SnlsRotateParams), ctypes.c_int32 * 3, ctypes.c_float * 3
+_ROTATE_SIZE, _pack_rotate = ctypes.sizeof(SnlsRotateParams), struct.Struct("=I9i3f3i").pack  # the struct's fields
 
 
 def rotate_from_dict(rp: dict) -> SnlsRotateParams:
     if len(rp["pairs"]) != 3 or len(rp["theta"]) != 3:
         raise ValueError("pairs and theta have three entries: time, row, column")
-    n = (int(rp["B"]), int(rp["T"]), int(rp["C"]), int(rp["H"]), int(rp["W"]), int(rp["HD"]), *rp["pairs"],
-         int(rp.get("interleaved", 0)), int(rp.get("row0", 0)), int(rp.get("col0", 0)))
-    if min(n) < -1 << 31 or max(n) >= 1 << 31:
-        raise ValueError("sizes, pairs and origins must be whole numbers of 32 bits")
-    return SnlsRotateParams(_ROTATE_SIZE, *n[:6], _Int3(*n[6:9]), _Float3(*rp["theta"]), *n[9:])
+    try:  # (packing looks at the numbers' ranges, which ctypes fields do not, and takes half their time)
+        return SnlsRotateParams.from_buffer_copy(_pack_rotate(
+            _ROTATE_SIZE, int(rp["B"]), int(rp["T"]), int(rp["C"]), int(rp["H"]), int(rp["W"]), int(rp["HD"]),
+            *rp["pairs"], *rp["theta"], int(rp.get("interleaved", 0)), int(rp.get("row0", 0)), int(rp.get("col0", 0))))
+    except (struct.error, OverflowError) as e:
+        raise ValueError("sizes, pairs and origins must be whole numbers of 32 bits, theta of fp32's range: %s" % e)
 
 
 def snls_rotate(q, k, rp: dict, times=None, inverse: bool = False, q_out=None, k_out=None, stream=None):

@@ -1,5 +1,6 @@
 """Numbers that a C field does not hold are refused, not taken modulo its size."""
 import pytest
+import torch
 
 from paper_2309_16849_amd import snls as B
 
@@ -47,3 +48,10 @@ def test_channels_past_32_bits_stay_too_many():
     for prm in (B.project_params(many, 4, 1, 1, 1), B.project_params(4, many, 1, 1, 1)):
         assert lib.snls_project(*[0x1000] * 4, prm, 0x1000, None) == B.SNLS_ERR_UNSUPPORTED
         assert lib.snls_project_pack(0x1000, prm, 0x1000, 0x1000, None) == B.SNLS_ERR_UNSUPPORTED
+
+
+def test_theta_past_fp32():
+    with pytest.raises(ValueError):
+        B.rotate_from_dict(dict(ROT, theta=(1e39, 1.0, 1.0)))
+    assert [float(t) for t in B.rotate_from_dict(dict(ROT, theta=(1e4, 0.1, 3e38))).theta] == [
+        1e4, float(torch.tensor(0.1)), float(torch.tensor(3e38))]
