@@ -567,10 +567,13 @@ snls_status snls_dropout(const float* x, const float* residual, const uint64_t* 
  * are.  Pair i of an axis with n pairs is its channels 2i and 2i+1
  * (interleaved) or i and n+i (not), and is turned by the angle position *
  * theta^(-i/n): (a, b) -> (a cos - b sin, a sin + b cos).  Inner products of
- * turned queries and keys depend on the difference of their positions.
- * Positions are the frame's time, row0 + row and col0 + column.  Angles are
- * formed and reduced in 64 bits: off by at most |angle| * 2^-51 radians and
- * 2^-24 more.  struct_size must be sizeof(snls_rotate_params). */
+ * turned queries and keys depend on the difference of their positions: of keys
+ * that are read at whole pixels.  A search or an aggregation with fractional shifts
+ * interpolates turned keys, and halfway between two pixels a pair of w radians a
+ * pixel keeps cos(w / 2) of its length (an axis's first pair, whose w is 1 whatever
+ * theta is, 0.88).  Positions are the frame's time, row0 + row and col0 + column.
+ * Angles are formed and reduced in 64 bits: off by at most |angle| * 2^-51 radians
+ * and 2^-24 more.  struct_size must be sizeof(snls_rotate_params). */
 #define SNLS_ROTATE_MAX_PAIRS 128 /* largest sum of pairs */
 typedef struct {
   uint32_t struct_size;

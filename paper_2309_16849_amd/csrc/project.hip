@@ -650,7 +650,11 @@ snls_status launch_project(const float* x, const int8_t* codes, const float* sca
   // 192 at 480x854 84 us and 90, 192 -> 576 at 5x152x152 72 and 77, but 16 -> 384 at
   // 304x622 63 and 61; planes that do not, 470x854 92 and 123, 32 -> 64 at 9x397x391
   // 117 and 173, but 16 -> 384 at 305x620 74 and 66, and nothing won or less where
-  // the 256 MB of cache hold the output: 305x622 44 and 45, 271x483 32 and 25.
+  // the 256 MB of cache hold all: 271x483 32 and 25, 96 -> 96 at 435x437 39 and 37.
+  // The border of 268 MB of output is a coarse one: below it runs are the faster from
+  // about 190,000 odd pixels on on inputs that no cache holds (64 -> 192 at 305x622 45
+  // and 56, 438x795 83 and 110; 32 -> 64 at 700x1003 60 and 75; 96 -> 96 at 600x667 77
+  // and 80, 192 -> 192 at 300x601 82 and 75).
   if (!tokens && nk <= 6 && g.aligned && (pp.parts == 1 || g.per % 32 == 0) && pp.cout <= 8 * pp.cin &&
       (whole || g.F * g.P * g.cout > 1LL << 26)) {
     // as many workgroups as the chip holds at once, by registers, take the frames in
